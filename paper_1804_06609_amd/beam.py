@@ -1,0 +1,261 @@
+"""The operators of include/dba_beam.h on torch tensors: marshalling and device-memory plumbing only.
+
+`select` (the new beam from logits), `reorder` (states follow the back-pointers), `append` (keys and values into a paged
+cache, rotated on the way) and `attend` (a tree's nodes over that cache).  All enqueue their work on the current stream of
+the current device, where their tensors have to be, and return without waiting; workspaces come from torch's allocator on that
+stream.  A tensor that was made on another stream is the caller's to wait for, as with any torch operator.
+Nothing of the methods runs here, and there is no fallback: without the built library the calls raise.
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import Optional, Sequence
+
+import torch
+
+from . import binding as _b
+
+_P, _I, _L, _Z = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_size_t
+
+
+class _State(ctypes.Structure):
+    _fields_ = [("dst", _P), ("src", _P)] + [(f, _L) for f in (
+        "dst_sent", "dst_row", "dst_seg", "src_sent", "src_row", "src_seg", "segs", "seg_bytes")]
+
+
+class _Cache(ctypes.Structure):
+    _fields_ = [("k", _P), ("v", _P), ("table", _P), ("table_stride", _L), ("page_stride", _L), ("token_stride", _L),
+                ("head_stride", _L), ("format", _I), ("n_pages", _I), ("page_size", _I), ("max_pages", _I), ("heads", _I), ("head_dim", _I)]
+
+
+class _Heads(ctypes.Structure):
+    _fields_ = [("data", _P), ("sent_stride", _L), ("token_stride", _L), ("head_stride", _L)]
+
+
+_SIGNATURES = {
+    "dba_beam_select_workspace_bytes": (_Z, [_I] * 5),
+    "dba_beam_select": (_I, [_I] * 6 + [_P, _I, _L, _L] + [_P] * 6 + [_P, _Z, _P]),
+    "dba_beam_reorder": (_I, [_I, _I, _P, _P, _I, _P]),
+    "dba_cache_append": (_I, [_I, _I, _P, _P, _P, _I] + [_P] * 6 + [_I, _I, _P]),
+    "dba_tree_attend_workspace_bytes": (_Z, [_I, _I, _I, _P, _I]),
+    "dba_tree_attend": (_I, [_I, _I, _I] + [_P] * 5 + [_I, _I, ctypes.c_float] + [_P] * 3 + [_Z, _P]),
+}
+_FORMATS = {torch.float32: _b.DBA_LOGP_F32, torch.float16: _b.DBA_LOGP_F16, torch.bfloat16: _b.DBA_LOGP_BF16}
+
+_lib = None
+
+
+def load() -> ctypes.CDLL:
+    """The built library with these operators' signatures; raises if it has not been built."""
+    global _lib
+    if _lib is None:
+        lib = _b.load()
+        for name, (res, args) in _SIGNATURES.items():
+            fn = getattr(lib, name)
+            fn.restype = res
+            fn.argtypes = args
+        _lib = lib
+    return _lib
+
+
+def _fail(text: str):
+    raise _b.DbaError(_b.DBA_EINVAL, text)
+
+
+def _stream(x: torch.Tensor) -> int:
+    if not x.is_cuda:
+        _fail("tensors must be on the GPU")
+    if x.device.index != torch.cuda.current_device():
+        _fail("tensors must be on the current device")
+    return torch.cuda.current_stream().cuda_stream
+
+
+def _ints(name: str, x: Optional[torch.Tensor], shape, like: torch.Tensor) -> Optional[int]:
+    """Address of a dense int32 tensor of this shape (None where it may be left out)."""
+    if x is None:
+        return None
+    if x.dtype is not torch.int32 or x.shape != shape or x.device != like.device or not x.is_contiguous():
+        _fail(f"{name} must be a contiguous int32 tensor {tuple(shape)} on the device of the others")
+    return x.data_ptr()
+
+
+def _workspace(nbytes: int, like: torch.Tensor):
+    """(tensor, address): torch's allocations start on 512 bytes."""
+    if not nbytes:
+        return None, None
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=like.device)
+    return ws, ws.data_ptr()
+
+
+def select(logits: torch.Tensor, score: torch.Tensor, flags: Optional[torch.Tensor], k_out: int, eos_id: int, pad_id: int,
+           out: Optional[Sequence[torch.Tensor]] = None):
+    """The new beam from logits [B, k_in, V] (fp32, fp16 or bf16; last axis dense), score [B, k_in] fp32 and flags [B, k_in] uint8 or
+    None: (token, backptr, score, flags), each [B, k_out] as dba_step writes them.  `out`: four tensors to write to."""
+    lib = load()
+    if logits.dim() != 3 or logits.dtype not in _FORMATS or (logits.shape[2] > 1 and logits.stride(2) != 1):
+        _fail("logits must be [B, k, V] of fp32, fp16 or bf16 with a dense last axis")
+    B, k, V = logits.shape
+    stream = _stream(logits)
+    for name, x, dtype in (("score", score, torch.float32), ("flags", flags, torch.uint8)):
+        if x is not None and (x.dtype is not dtype or x.shape != (B, k) or not x.is_contiguous() or x.device != logits.device):
+            _fail(f"{name} must be a contiguous {dtype} tensor [B, k] on the device of the logits")
+    if out is None:
+        dev = logits.device
+        out = (torch.empty((B, k_out), dtype=torch.int32, device=dev), torch.empty((B, k_out), dtype=torch.int32, device=dev),
+               torch.empty((B, k_out), dtype=torch.float32, device=dev), torch.empty((B, k_out), dtype=torch.uint8, device=dev))
+    else:
+        for x, dtype in zip(out, (torch.int32, torch.int32, torch.float32, torch.uint8), strict=True):
+            if x.dtype is not dtype or x.shape != (B, k_out) or not x.is_contiguous() or x.device != logits.device:
+                _fail("out must be four contiguous tensors [B, k_out]: int32, int32, fp32, uint8")
+    fmt = _FORMATS[logits.dtype]
+    nbytes = lib.dba_beam_select_workspace_bytes(B, k, k_out, V, fmt)
+    ws, at = _workspace(nbytes, logits)
+    _b._check(lib.dba_beam_select(B, k, k_out, V, eos_id, pad_id, logits.data_ptr(), fmt, logits.stride(0), logits.stride(1),
+                                  score.data_ptr(), None if flags is None else flags.data_ptr(), out[0].data_ptr(), out[1].data_ptr(),
+                                  out[2].data_ptr(), out[3].data_ptr(), at, nbytes, stream))
+    return tuple(out)
+
+
+def _pieces(x: torch.Tensor):
+    """[B, k, ...] as (sent, row, seg strides in bytes, pieces, bytes of a piece); the axes behind the second fold into two."""
+    e = x.element_size()
+    shape, strides = list(x.shape[2:]), list(x.stride()[2:])
+    seg, dense = 1, 1                                  # dense: elements of a piece so far
+    while shape and (shape[-1] == 1 or strides[-1] == dense):
+        dense *= shape.pop()
+        strides.pop()
+    seg_stride = 0
+    while shape:
+        n, s = shape.pop(), strides.pop()
+        if n == 1:
+            continue
+        if seg == 1:
+            seg_stride = s
+        elif s != seg_stride * seg:
+            return None
+        seg *= n
+    return x.stride(0) * e, x.stride(1) * e, seg_stride * e, seg, dense * e
+
+
+def reorder(backptr: torch.Tensor, states: Sequence[torch.Tensor], out: Optional[Sequence[torch.Tensor]] = None):
+    """Every state [B, k, ...] (any type) follows backptr [B, k] int32: out[b, h] = state[b, backptr[b, h]], rows of a
+    back-pointer outside [0, k) cleared.  out None: in place.  Views of the places in use do: behind the
+    second axis a state may have one more that is not dense (e.g. [B, k, heads, capacity, width][:, :, :, :t]).  Returns `out`."""
+    lib = load()
+    if backptr.dim() != 2:
+        _fail("backptr must be [B, k]")
+    B, k = backptr.shape
+    stream = _stream(backptr)
+    back = _ints("backptr", backptr, backptr.shape, backptr)
+    out = states if out is None else out
+    if len(out) != len(states):
+        _fail("as many tensors out as states")
+    table = (_State * len(states))()
+    for row, s, d in zip(table, states, out):
+        if s.shape[:2] != (B, k) or s.shape != d.shape or s.dtype is not d.dtype or s.device != backptr.device or d.device != backptr.device:
+            _fail("states and out must be [B, k, ...] tensors alike in shape and type, on the device of backptr")
+        a, c = _pieces(s), _pieces(d)
+        if a is None or c is None:
+            _fail("a state's axes behind the second must fold into pieces of one stride")
+        if a[3:] != c[3:]:                             # one side is more finely cut: the smaller piece serves both
+            piece = min(a[4], c[4])
+            if max(a[4], c[4]) % piece or (a[3] > 1 and c[3] > 1):
+                _fail("the axes of a state and its out must fold alike")
+            a, c = ((x[0], x[1], piece if x[4] > piece else x[2], x[3] * x[4] // piece, piece) for x in (a, c))
+        row.dst, row.dst_sent, row.dst_row, row.dst_seg = d.data_ptr(), *c[:3]
+        row.src, row.src_sent, row.src_row, row.src_seg = s.data_ptr(), *a[:3]
+        row.segs, row.seg_bytes = a[3], a[4]
+    _b._check(lib.dba_beam_reorder(B, k, back, table, len(states), stream))
+    return out
+
+
+def _cache(k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor, like: torch.Tensor) -> _Cache:
+    strides = [[st if size > 1 else 0 for st, size in zip(x.stride(), x.shape)] for x in (k_pages, v_pages)]
+    if k_pages.dim() != 4 or v_pages.shape != k_pages.shape or strides[0] != strides[1] or strides[0][3] != 1:
+        _fail("k_pages and v_pages must be [pages, page_size, heads, head_dim], laid out alike, with a dense last axis")
+    if k_pages.dtype not in _FORMATS or v_pages.dtype is not k_pages.dtype or k_pages.dtype is not like.dtype:
+        _fail("keys, values, queries and pages must be of one type: fp32, fp16 or bf16")
+    if table.dtype is not torch.int32 or table.dim() != 2 or table.stride(1) != 1 or table.shape[0] != like.shape[0]:
+        _fail("table must be an int32 tensor [B, max_pages] with a dense last axis")
+    if k_pages.device != like.device or v_pages.device != like.device or table.device != like.device:
+        _fail("tensors must be on one device")
+    n_pages, page, heads, D = k_pages.shape
+    s = strides[0]
+    return _Cache(k_pages.data_ptr(), v_pages.data_ptr(), table.data_ptr(), table.stride(0), s[0], s[1], s[2],
+                  _FORMATS[k_pages.dtype], n_pages, page, table.shape[1], heads, D)
+
+
+def _heads(name: str, x: torch.Tensor, B: int, n: int, heads: Optional[int], D: int, like: torch.Tensor) -> _Heads:
+    if x.dim() != 4 or x.shape[0] != B or x.shape[1] != n or (heads is not None and x.shape[2] != heads) or x.shape[3] != D:
+        _fail(f"{name} must be [B, n, heads, head_dim]")
+    if x.dtype is not like.dtype or x.device != like.device or x.stride(3) != 1:
+        _fail(f"{name} must be of the type and on the device of the others, with a dense last axis")
+    # the stride of an axis of one is never used; torch gives it any value
+    s = [st if size > 1 else 0 for st, size in zip(x.stride(), x.shape)]
+    return _Heads(x.data_ptr(), s[0], s[1], s[2])
+
+
+def append(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor, first: torch.Tensor,
+           count: Optional[torch.Tensor] = None, *, position: Optional[torch.Tensor] = None, inv_freq: Optional[torch.Tensor] = None,
+           interleaved: bool = False, q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """k, v [B, n, heads, head_dim] become tokens first[b] .. of the cache (count[b] of them, or n), k rotated by its position ([B, n]
+    int32, or first[b] + i) and inv_freq (fp32; None: no rotation).  q [B, n, q_heads, head_dim] is rotated alike into q_out (a new
+    tensor if None; q itself is allowed), which is returned."""
+    lib = load()
+    stream = _stream(k)
+    if k.dim() != 4:
+        _fail("k must be [B, n, heads, head_dim]")
+    B, n, heads, D = k.shape
+    cache = _cache(k_pages, v_pages, table, k)
+    if (cache.heads, cache.head_dim) != (heads, D):
+        _fail("k has other heads than the cache")
+    kh, vh = _heads("k", k, B, n, heads, D, k), _heads("v", v, B, n, heads, D, k)
+    qh = oh = None
+    if q is not None:
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        qh, oh = ctypes.byref(_heads("q", q, B, n, None, D, k)), ctypes.byref(_heads("q_out", q_out, B, n, q.shape[2], D, k))
+    if inv_freq is not None and (inv_freq.dtype is not torch.float32 or inv_freq.dim() != 1 or not inv_freq.is_contiguous() or inv_freq.device != k.device):
+        _fail("inv_freq must be a contiguous fp32 tensor [rot_dim / 2]")
+    rot = 0 if inv_freq is None else 2 * inv_freq.shape[0]
+    _b._check(lib.dba_cache_append(B, n, ctypes.byref(cache), ctypes.byref(kh), ctypes.byref(vh), 0 if q is None else q.shape[2], qh, oh,
+                                   _ints("first", first, (B,), k), _ints("count", count, (B,), k), _ints("position", position, (B, n), k),
+                                   inv_freq.data_ptr() if rot else None, rot, int(interleaved), stream))
+    return q_out
+
+
+def attend(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor, prefix: torch.Tensor,
+           tree: Optional[torch.Tensor] = None, mask: Optional[torch.Tensor] = None, *, scale: Optional[float] = None,
+           max_len: Optional[int] = None, out: Optional[torch.Tensor] = None, return_lse: bool = False):
+    """q [B, n, q_heads, head_dim] over the cache: node i of sentence b sees its prefix[b] first tokens and, of the tree[b] behind
+    them, those whose bit is set in mask [B, n, words] (int64, 64 tokens a word, lowest bit first); without a mask the n nodes are
+    the last n tokens of a chain.  scale: head_dim ** -0.5 if None.  max_len: no sentence has more tokens (the table's capacity
+    if None; a close bound makes a better launch).  Returns out, or (out, lse [B, n, q_heads] fp32)."""
+    lib = load()
+    stream = _stream(q)
+    if q.dim() != 4:
+        _fail("q must be [B, n, q_heads, head_dim]")
+    B, n, heads, D = q.shape
+    cache = _cache(k_pages, v_pages, table, q)
+    if cache.head_dim != D:
+        _fail("q has another head_dim than the cache")
+    if out is None:
+        out = torch.empty((B, n, heads, D), dtype=q.dtype, device=q.device)
+    words = 0
+    if mask is not None:
+        if mask.dtype is not torch.int64 or mask.dim() != 3 or mask.shape[:2] != (B, n) or not mask.is_contiguous() or mask.device != q.device:
+            _fail("mask must be a contiguous int64 tensor [B, n, words] on the device of the others")
+        words = mask.shape[2]
+        if not words:                                  # a mask without a bit: nothing of the tree is seen
+            tree = None
+    qh, oh = _heads("q", q, B, n, heads, D, q), _heads("out", out, B, n, heads, D, q)
+    lse = torch.empty((B, n, heads), dtype=torch.float32, device=q.device) if return_lse else None
+    if max_len is None:
+        max_len = min(cache.max_pages * cache.page_size, 2**31 - 1)
+    nbytes = lib.dba_tree_attend_workspace_bytes(B, n, heads, ctypes.byref(cache), max_len)
+    ws, at = _workspace(nbytes, q)
+    _b._check(lib.dba_tree_attend(B, n, heads, ctypes.byref(qh), ctypes.byref(cache), _ints("prefix", prefix, (B,), q),
+                                  _ints("tree", tree, (B,), q), mask.data_ptr() if words else None, words, max_len,
+                                  D ** -0.5 if scale is None else float(scale), ctypes.byref(oh), lse.data_ptr() if return_lse else None,
+                                  at, nbytes, stream))
+    return (out, lse) if return_lse else out

@@ -8,13 +8,16 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdba.so")
-SOURCES = [os.path.join(CSRC, "dba.hip")]
-DEPS = SOURCES + [os.path.join(CSRC, f) for f in ("dba_kernels.hpp", "wave_topk.hpp", "host_blocks.hpp")] + [
-    os.path.join(os.path.dirname(HERE), "include", f) for f in ("dba.h", "dba_debug.h")]
+OBJ = os.path.join(HERE, "build")
+SOURCES = [os.path.join(CSRC, f) for f in ("dba.hip", "dba_beam.hip")]
+DEPS = SOURCES + [os.path.join(CSRC, f) for f in (
+    "dba_kernels.hpp", "wave_topk.hpp", "host_blocks.hpp", "entry.hpp", "paged.hpp", "beam_select.hpp", "beam_reorder.hpp",
+    "cache_append.hpp", "tree_attend.hpp")] + [
+    os.path.join(os.path.dirname(HERE), "include", f) for f in ("dba.h", "dba_debug.h", "dba_beam.h")]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
-    "--offload-arch=gfx950", "-O3", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden",
+    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden",
     # packed fp32 VALU forms are kept off on the test machines
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wall", "-Wno-unused-function",
@@ -27,8 +30,13 @@ def build(force: bool = True, extra=()) -> str:
     stale = force or not os.path.exists(LIB) or any(
         os.path.getmtime(LIB) < os.path.getmtime(d) for d in DEPS)
     if stale:
-        cmd = [HIPCC] + FLAGS + list(extra) + SOURCES + ["-o", LIB]
-        subprocess.check_call(cmd)
+        os.makedirs(OBJ, exist_ok=True)
+        objects = [os.path.join(OBJ, os.path.basename(s) + ".o") for s in SOURCES]
+        compiles = [subprocess.Popen([HIPCC] + FLAGS + list(extra) + ["-c", s, "-o", o]) for s, o in zip(SOURCES, objects)]
+        failed = [c.args for c in compiles if c.wait() != 0]     # (all are waited for)
+        if failed:
+            raise subprocess.CalledProcessError(1, failed[0])
+        subprocess.check_call([HIPCC, "--offload-arch=gfx950", "-shared"] + objects + ["-o", LIB])
     return LIB
 
 

@@ -1,0 +1,375 @@
+// Selection over beams and vocabulary from logits: kernels.
+//
+// The score of an extension, score[h] + x - lse[h], falls with the logit x inside a row, so a row's best are known
+// before its normaliser is.  One pass over the logits therefore does both: a workgroup takes a part of a row
+// into registers, sums the exponentials, and hands on the part's k_out greatest logits (and a few more).
+// A second launch, one workgroup per sentence, puts the normalisers together and ranks what has been handed on.
+#pragma once
+#include "wave_topk.hpp"
+
+namespace dba {
+
+// What a part of a row leaves behind: its greatest logit, the sum of exp(x - top) and how many keys it has handed on.
+struct SelectPart {
+    double sum;
+    float top;
+    int count;
+};
+
+struct SelectParams {
+    const float *score;
+    const uint8_t *flags;              // null: all rows live
+    int32_t *out_token, *out_backptr;
+    float *out_score;
+    uint8_t *out_flags;
+    SelectPart *parts;                 // [B, k_in, nparts]
+    u64 *keys;                         // [B, k_in, nparts, cap]
+    int64_t sent_stride, row_stride;   // elements
+    int k_in, k_out, V, nparts, cap, part_chunks, eos, pad;
+};
+
+constexpr int kSelectThreads = 256;    // of the first launch
+constexpr int kSelectChunks = 8;       // 16-byte chunks a thread keeps in registers
+constexpr int kSelectFinal = 512;      // keys the second launch ranks by counting
+// log2 e in two parts: a one-part product is off by 1.3e-8 of itself in the same direction for every x, which shows in the sum
+constexpr float kLog2eHi = 1.44269502162933349609375f;
+constexpr float kLog2eLo = (float)(1.442695040888963407359924681 - 1.44269502162933349609375);
+
+// exp(x - top); the difference comes first, so that logits at the type's lowest value do no harm
+__device__ __forceinline__ float exp_below(float x, float top)
+{
+    const float d = x - top;
+    return __builtin_amdgcn_exp2f(fmaf(d, kLog2eHi, d * kLog2eLo));
+}
+
+template <int FMT> struct Chunk;       // 16 bytes of logits
+template <> struct Chunk<0> {
+    static constexpr int N = 4;
+    typedef float elem_t;
+    static __device__ __forceinline__ float get(const uint4 &c, int e) { return __uint_as_float(((const uint32_t *)&c)[e]); }
+    static __device__ __forceinline__ uint32_t bits(const float *p) { return __float_as_uint(*p); }
+    static constexpr uint32_t kNone = 0xFF800000u;
+};
+template <> struct Chunk<1> {
+    static constexpr int N = 8;
+    typedef uint16_t elem_t;
+    static __device__ __forceinline__ float get(const uint4 &c, int e)
+    {
+        const uint32_t w = ((const uint32_t *)&c)[e >> 1];
+        const uint16_t h = (uint16_t)((e & 1) ? w >> 16 : w);
+        return (float)__builtin_bit_cast(_Float16, h);
+    }
+    static __device__ __forceinline__ uint32_t bits(const uint16_t *p) { return *p; }
+    static constexpr uint32_t kNone = 0xFC00u;
+};
+template <> struct Chunk<2> {
+    static constexpr int N = 8;
+    typedef uint16_t elem_t;
+    static __device__ __forceinline__ float get(const uint4 &c, int e)
+    {
+        const uint32_t w = ((const uint32_t *)&c)[e >> 1];
+        return __uint_as_float((e & 1) ? w & 0xFFFF0000u : w << 16);
+    }
+    static __device__ __forceinline__ uint32_t bits(const uint16_t *p) { return *p; }
+    static constexpr uint32_t kNone = 0xFF80u;
+};
+
+__device__ __forceinline__ float wave_max_float(float v)
+{
+#pragma unroll
+    for (int d = 32; d; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
+    return v;
+}
+__device__ __forceinline__ double wave_sum_double(double v)
+{
+#pragma unroll
+    for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
+    return v;
+}
+
+// Sum of `v` over the workgroup, in every thread.  `room`: one int per wave; ends with a barrier.
+template <int THREADS>
+__device__ __forceinline__ int block_sum(int v, int *room)
+{
+#pragma unroll
+    for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
+    if (lane_id() == 0) room[threadIdx.x / kWave] = v;
+    __syncthreads();
+    int s = 0;
+    for (int w = 0; w < THREADS / kWave; ++w) s += room[w];
+    __syncthreads();
+    return s;
+}
+
+// One part of one row.  Bound: HBM (the logits are read once); the exponentials take about a quarter of
+// the VALU's time at that rate.
+template <int FMT>
+__global__ __launch_bounds__(kSelectThreads) void dba_select_part_kernel(const void *logits, SelectParams p)
+{
+    typedef Chunk<FMT> C;
+    typedef typename C::elem_t elem_t;
+    constexpr int T = kSelectThreads, R = kSelectChunks, N = C::N, NW = T / kWave;
+    __shared__ uint32_t s_max[T];
+    __shared__ double s_sum[NW];
+    __shared__ int s_int[NW];
+    __shared__ int s_count;
+    __shared__ u64 s_keys[2 * DBA_MAX_BEAM];
+    const int t = (int)threadIdx.x;
+    const int part = (int)blockIdx.x % p.nparts, h = (int)blockIdx.x / p.nparts, b = (int)blockIdx.y;
+    const int row = b * p.k_in + h;
+    const size_t list = (size_t)row * p.nparts + part;
+    SelectPart *out = p.parts + list;
+    u64 *out_keys = p.keys + list * p.cap;
+    const float score = p.score[row];
+    const int flags = p.flags ? p.flags[row] : 0;
+    if ((flags & (DBA_FLAG_FINISHED | DBA_FLAG_DEAD)) || !(fabsf(score) < INFINITY)) {
+        // a completed hypothesis goes on with pad_id at its own score; the others offer nothing
+        const bool goes_on = part == 0 && (flags & DBA_FLAG_FINISHED) && !(flags & DBA_FLAG_DEAD) && fabsf(score) < INFINITY;
+        if (t == 0) {
+            if (goes_on) out_keys[0] = make_key(0.0f, (uint32_t)p.pad);
+            *out = SelectPart{goes_on ? 1.0 : 0.0, 0.0f, goes_on ? 1 : 0};
+        }
+        return;
+    }
+    const elem_t *src = static_cast<const elem_t *>(logits) + ((int64_t)b * p.sent_stride + (int64_t)h * p.row_stride);
+    // chunks lie on the 16-byte grid of memory; the first starts `shift` elements before the row
+    const int shift = (int)((reinterpret_cast<uintptr_t>(src) & 15) / sizeof(elem_t));
+    const int c0 = part * p.part_chunks, c1 = c0 + p.part_chunks;
+    uint4 raw[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int c = c0 + t + r * T;
+        const int64_t v0 = (int64_t)c * N - shift;
+        if (c < c1 && v0 >= 0 && v0 + N <= p.V) {
+            raw[r] = *reinterpret_cast<const uint4 *>(src + v0);
+        } else {
+            uint32_t w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = N == 4 ? C::kNone : C::kNone | (C::kNone << 16);
+            if (c < c1) {
+#pragma unroll
+                for (int e = 0; e < N; ++e)
+                    if (v0 + e >= 0 && v0 + e < p.V) {
+                        const uint32_t x = C::bits(src + v0 + e);
+                        if (N == 4) w[e] = x;
+                        else w[e >> 1] = (e & 1) ? (w[e >> 1] & 0xFFFFu) | (x << 16) : (w[e >> 1] & 0xFFFF0000u) | x;
+                    }
+            }
+            raw[r] = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    }
+    float top = -INFINITY;
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int e = 0; e < N; ++e) top = fmaxf(top, C::get(raw[r], e));
+    s_max[t] = top > -INFINITY ? ord_from_float(top) : 0u;
+    if (t == 0) s_count = 0;
+    __syncthreads();
+    // k_out threads hold something that reaches the k_out-th greatest of the threads' maxima: so does
+    // everything that can be among the part's k_out greatest
+    uint32_t r4[T / kWave];
+    uint32_t most = 0;
+#pragma unroll
+    for (int j = 0; j < T / kWave; ++j) {
+        r4[j] = s_max[j * kWave + lane_id()];
+        most = most > r4[j] ? most : r4[j];
+    }
+    most = wave_max_u32(most);
+    int reached;
+    const uint32_t bar_ord = kth_greatest<T / kWave>(r4, p.k_out, reached);
+    const float bar = bar_ord ? float_from_ord(bar_ord) : -INFINITY;
+    const float most_x = most ? float_from_ord(most) : 0.0f;
+    // the sum: a few dozen terms a thread in fp32 (each is off by 1e-7 of itself, either way), the threads' in 64 bits
+    float sum = 0.0f;
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const float x = C::get(raw[r], e);
+            sum += exp_below(x, most_x);
+            if (x >= bar && x > -INFINITY) {
+                const int at = atomicAdd(&s_count, 1);
+                const int c = c0 + t + r * T;
+                if (at < p.cap) s_keys[at] = make_key(x, (uint32_t)(c * N - shift + e));
+            }
+        }
+    const double total = wave_sum_double((double)sum);
+    if (lane_id() == 0) s_sum[t / kWave] = total;
+    __syncthreads();
+    int count = s_count;
+    if (count > p.cap) {
+        // many equal logits, or few threads with any: exactly k_out, by bisection on the keys, which all differ
+        auto each = [&](auto f) {
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    const float x = C::get(raw[r], e);
+                    if (x >= bar && x > -INFINITY) f(make_key(x, (uint32_t)((c0 + t + r * T) * N - shift + e)));
+                }
+        };
+        u64 lo = 1, hi = ~0ull;
+        while (lo < hi) {
+            const u64 mid = lo + ((hi - lo) >> 1) + 1;
+            int n = 0;
+            each([&](u64 key) { n += key >= mid; });
+            n = block_sum<T>(n, s_int);
+            if (n >= p.k_out) lo = mid;
+            else hi = mid - 1;
+            if (n == p.k_out) break;
+        }
+        if (t == 0) s_count = 0;
+        __syncthreads();
+        each([&](u64 key) {
+            if (key >= lo) {
+                const int at = atomicAdd(&s_count, 1);
+                if (at < p.cap) s_keys[at] = key;
+            }
+        });
+        __syncthreads();
+        count = min(s_count, p.cap);
+    }
+    for (int i = t; i < count; i += T) out_keys[i] = s_keys[i];
+    if (t == 0) {
+        double s = 0.0;
+        for (int w = 0; w < NW; ++w) s += s_sum[w];
+        *out = SelectPart{s, most_x, count};
+    }
+}
+
+__device__ __forceinline__ u64 ord_from_double(double s)
+{
+    const u64 u = (u64)__double_as_longlong(s + 0.0);
+    return (u >> 63) ? ~u : (u | 0x8000000000000000ull);
+}
+
+// One sentence: normalisers, then the k_out best of what its rows have handed on.  Bound: latency.
+template <int T>
+__global__ __launch_bounds__(T) void dba_select_sentence_kernel(SelectParams p)
+{
+    constexpr int NW = T / kWave;
+    __shared__ double s_base[DBA_MAX_BEAM];       // score - log sum exp(x - top); NaN where the row offers nothing
+    __shared__ float s_top[DBA_MAX_BEAM];
+    __shared__ uint32_t s_max[T];
+    __shared__ int s_int[NW];
+    __shared__ int s_count;
+    __shared__ u64 s_ord[kSelectFinal];
+    __shared__ uint32_t s_flat[kSelectFinal];
+    __shared__ double s_score[kSelectFinal];
+    const int t = (int)threadIdx.x, b = (int)blockIdx.x;
+    const SelectPart *parts = p.parts + (size_t)b * p.k_in * p.nparts;
+    const u64 *keys = p.keys + (size_t)b * p.k_in * p.nparts * p.cap;
+    if (t < p.k_in) {
+        const int flags = p.flags ? p.flags[b * p.k_in + t] : 0;
+        const double score = (double)p.score[b * p.k_in + t];
+        double base = score;
+        float most = 0.0f;
+        if (!(flags & DBA_FLAG_FINISHED)) {
+            most = -INFINITY;
+            for (int i = 0; i < p.nparts; ++i)
+                if (parts[t * p.nparts + i].sum != 0.0) most = fmaxf(most, parts[t * p.nparts + i].top);
+            double sum = 0.0;
+            for (int i = 0; i < p.nparts; ++i) {
+                const SelectPart q = parts[t * p.nparts + i];
+                if (q.sum != 0.0) sum += q.sum * exp((double)q.top - (double)most);
+            }
+            base = score - log(sum);
+        }
+        s_top[t] = most;
+        s_base[t] = fabs(base) < INFINITY ? base : __longlong_as_double(0x7FF8000000000000ll);
+    }
+    if (t == 0) s_count = 0;
+    __syncthreads();
+    const int places = p.k_in * p.nparts * p.cap;
+    auto each = [&](auto f) {
+        for (int i = t; i < places; i += T) {
+            const int list = i / p.cap;
+            if (i - list * p.cap >= parts[list].count) continue;
+            const int h = list / p.nparts;
+            const u64 key = keys[i];
+            const double s = s_base[h] + ((double)float_from_ord((uint32_t)(key >> 32)) - (double)s_top[h]);
+            if (s == s) f(s, (uint32_t)h * (uint32_t)p.V + key_flat(key));
+        }
+    };
+    uint32_t top = 0;
+    each([&](double s, uint32_t) {
+        const uint32_t o = ord_from_float((float)s);
+        top = top > o ? top : o;
+    });
+    s_max[t] = top;
+    __syncthreads();
+    uint32_t r[NW];
+#pragma unroll
+    for (int j = 0; j < NW; ++j) r[j] = s_max[j * kWave + lane_id()];
+    int reached;
+    const uint32_t bar = kth_greatest<NW>(r, p.k_out, reached);
+    auto put = [&](double s, uint32_t flat) {
+        const int at = atomicAdd(&s_count, 1);
+        if (at < kSelectFinal) {
+            s_ord[at] = ord_from_double(s);
+            s_flat[at] = flat;
+            s_score[at] = s;
+        }
+    };
+    each([&](double s, uint32_t flat) {
+        if (ord_from_float((float)s) >= bar) put(s, flat);
+    });
+    __syncthreads();
+    int count = s_count;
+    if (count > kSelectFinal) {
+        // the k_out-th greatest score by bisection, then of its equals the first coordinates
+        u64 lo = 0, hi = ~0ull;
+        while (lo < hi) {
+            const u64 mid = lo + ((hi - lo) >> 1) + 1;
+            int n = 0;
+            each([&](double s, uint32_t) { n += ord_from_double(s) >= mid; });
+            n = block_sum<T>(n, s_int);
+            if (n >= p.k_out) lo = mid;
+            else hi = mid - 1;
+        }
+        int more = 0;
+        each([&](double s, uint32_t) { more += ord_from_double(s) > lo; });
+        more = block_sum<T>(more, s_int);
+        uint32_t first = 0, last = ~0u;            // the least coordinate up to which enough of the equals lie
+        while (first < last) {
+            const uint32_t mid = first + ((last - first) >> 1);
+            int n = 0;
+            each([&](double s, uint32_t flat) { n += ord_from_double(s) == lo && flat <= mid; });
+            n = block_sum<T>(n, s_int);
+            if (n >= p.k_out - more) last = mid;
+            else first = mid + 1;
+        }
+        if (t == 0) s_count = 0;
+        __syncthreads();
+        each([&](double s, uint32_t flat) {
+            const u64 o = ord_from_double(s);
+            if (o > lo || (o == lo && flat <= last)) put(s, flat);
+        });
+        __syncthreads();
+        count = min(s_count, kSelectFinal);
+    }
+    int32_t *token = p.out_token + (size_t)b * p.k_out, *back = p.out_backptr + (size_t)b * p.k_out;
+    float *score = p.out_score + (size_t)b * p.k_out;
+    uint8_t *flags = p.out_flags + (size_t)b * p.k_out;
+    for (int i = t; i < count; i += T) {
+        const u64 o = s_ord[i];
+        const uint32_t f = s_flat[i];
+        int rank = 0;
+        for (int j = 0; j < count; ++j) rank += s_ord[j] > o || (s_ord[j] == o && s_flat[j] < f);
+        if (rank >= p.k_out) continue;
+        const int h = (int)(f / (uint32_t)p.V), w = (int)(f - (uint32_t)h * (uint32_t)p.V);
+        token[rank] = w;
+        back[rank] = h;
+        score[rank] = (float)s_score[i];
+        flags[rank] = w == p.eos || (p.flags && (p.flags[b * p.k_in + h] & DBA_FLAG_FINISHED)) ? DBA_FLAG_FINISHED : 0;
+    }
+    for (int i = count + t; i < p.k_out; i += T) {
+        token[i] = p.pad;
+        back[i] = -1;
+        score[i] = -INFINITY;
+        flags[i] = DBA_FLAG_DEAD;
+    }
+}
+
+}  // namespace dba

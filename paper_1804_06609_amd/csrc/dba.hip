@@ -14,6 +14,7 @@
 #include "../../include/dba.h"
 #include "../../include/dba_debug.h"
 #include "dba_kernels.hpp"
+#include "entry.hpp"
 #include "host_blocks.hpp"
 
 using namespace dba;
@@ -887,6 +888,19 @@ int fail(dba_ctx *ctx, int code, const char *fmt, ...)
     va_end(ap);
     return code;
 }
+
+}  // namespace
+
+int dba::set_error(int code, const char *fmt, ...)
+{
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(g_init_error, sizeof g_init_error, fmt, ap);
+    va_end(ap);
+    return code;
+}
+
+namespace {
 
 bool shape_ok(int B, int k, int V, int N, int max_cons)
 {

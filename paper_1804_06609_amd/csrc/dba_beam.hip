@@ -1,0 +1,371 @@
+// libdba: the operators next to the selection step (see include/dba_beam.h), host side.
+#include <hip/hip_runtime.h>
+#include <math.h>
+
+#include <algorithm>
+
+#include "../../include/dba_beam.h"
+#include "beam_reorder.hpp"
+#include "beam_select.hpp"
+#include "cache_append.hpp"
+#include "entry.hpp"
+#include "tree_attend.hpp"
+
+using namespace dba;
+
+namespace {
+
+constexpr size_t align256(size_t x) { return (x + 255) / 256 * 256; }
+constexpr int kMostRows = 1 << 22;          // tokens, or heads of tokens, of one sentence in a call
+
+int launched(const char *who)
+{
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? DBA_OK : set_error(DBA_EHIP, "%s: launch failed: %s", who, hipGetErrorString(e));
+}
+
+// ---- selection ----------------------------------------------------------------------------------------------------
+
+struct SelectPlan {
+    int nparts, part_chunks, cap;
+    size_t keys_at, total;
+};
+
+bool select_shape_ok(int B, int k_in, int k_out, int V, int format)
+{
+    return B >= 1 && B <= 65535 && k_in >= 1 && k_in <= DBA_MAX_BEAM && k_out >= 1 && k_out <= DBA_MAX_BEAM && V >= 1 &&
+           V <= (1 << 24) && format_ok(format);
+}
+
+SelectPlan select_plan(int B, int k_in, int k_out, int V, int format)
+{
+    SelectPlan s;
+    const int per_chunk = 16 / (int)elem_bytes(format);
+    const int chunks = (V + per_chunk - 1) / per_chunk + 1;        // a row that starts inside a chunk may touch one more
+    const int most = kSelectThreads * kSelectChunks;
+    s.nparts = (chunks + most - 1) / most;
+    s.part_chunks = (chunks + s.nparts - 1) / s.nparts;
+    s.cap = std::max(32, 2 * k_out);
+    const size_t lists = (size_t)B * k_in * s.nparts;
+    s.keys_at = align256(lists * sizeof(SelectPart));
+    s.total = align256(s.keys_at + lists * s.cap * sizeof(u64));
+    return s;
+}
+
+// ---- caches -------------------------------------------------------------------------------------------------------
+
+const char *cache_fault(const dba_cache *c)
+{
+    if (!c) return "the cache is NULL";
+    if (!format_ok(c->format)) return "unknown format";
+    if (!c->k || !c->v || !c->table) return "a pointer of the cache is NULL";
+    if (c->heads < 1 || c->heads > 1024) return "1 <= heads <= 1024";
+    if (c->head_dim < 8 || c->head_dim > 256 || c->head_dim % 8) return "head_dim must be a multiple of 8, 8 to 256";
+    if (c->page_size < 1 || c->page_size > 65536 || (c->page_size & (c->page_size - 1))) return "page_size must be a power of two, at most 65536";
+    if (c->n_pages < 1 || c->max_pages < 1) return "n_pages and max_pages must be at least 1";
+    if ((int64_t)c->max_pages * c->page_size > INT32_MAX) return "max_pages * page_size must be below 2^31";
+    if (c->table_stride < c->max_pages) return "table_stride is less than max_pages";
+    const int unit = 16 / (int)elem_bytes(c->format);
+    if (misaligned(c->k, 16) || misaligned(c->v, 16) || c->page_stride % unit || c->token_stride % unit || c->head_stride % unit ||
+        c->page_stride < 0 || c->token_stride < 0 || c->head_stride < 0)
+        return "k, v and the strides of pages, tokens and heads must be multiples of 16 bytes, none negative";
+    return nullptr;
+}
+
+const char *heads_fault(const dba_heads *h, int format)
+{
+    if (!h || !h->data) return "a tensor is NULL";
+    const int unit = 16 / (int)elem_bytes(format);
+    if (misaligned(h->data, 16) || h->sent_stride % unit || h->token_stride % unit || h->head_stride % unit || h->sent_stride < 0 ||
+        h->token_stride < 0 || h->head_stride < 0)
+        return "tensors and their strides must be multiples of 16 bytes, none negative";
+    return nullptr;
+}
+
+Paged paged_of(const dba_cache &c)
+{
+    Paged p;
+    p.table = c.table;
+    p.table_stride = c.table_stride;
+    p.page_stride = c.page_stride;
+    p.token_stride = c.token_stride;
+    p.head_stride = c.head_stride;
+    p.n_pages = c.n_pages;
+    p.page_shift = __builtin_ctz((unsigned)c.page_size);
+    p.max_pages = c.max_pages;
+    return p;
+}
+
+HeadsAt heads_of(const dba_heads *h)
+{
+    if (!h) return HeadsAt{nullptr, 0, 0, 0};
+    return HeadsAt{static_cast<unsigned char *>(h->data), h->sent_stride, h->token_stride, h->head_stride};
+}
+
+// the two launches of a selection
+template <int FMT>
+void select_launch(const SelectParams &p, int B, const void *logits, hipStream_t stream)
+{
+    dba_select_part_kernel<FMT><<<dim3((unsigned)(p.nparts * p.k_in), (unsigned)B), kSelectThreads, 0, stream>>>(logits, p);
+}
+
+}  // namespace
+
+extern "C" {
+
+DBA_API size_t dba_beam_select_workspace_bytes(int B, int k_in, int k_out, int V, int logits_format)
+{
+    return select_shape_ok(B, k_in, k_out, V, logits_format) ? select_plan(B, k_in, k_out, V, logits_format).total : 0;
+}
+
+DBA_API int dba_beam_select(int B, int k_in, int k_out, int V, int eos_id, int pad_id, const void *logits_dev, int logits_format,
+                            int64_t sent_stride, int64_t row_stride, const float *score_dev, const uint8_t *flags_dev,
+                            int32_t *out_token_dev, int32_t *out_backptr_dev, float *out_score_dev, uint8_t *out_flags_dev,
+                            void *workspace_dev, size_t workspace_bytes, void *hip_stream)
+{
+    if (!select_shape_ok(B, k_in, k_out, V, logits_format))
+        return set_error(DBA_EINVAL, "dba_beam_select: need 1 <= B <= 65535, 1 <= k_in, k_out <= %d, 1 <= V <= 2^24 and a known format",
+                         DBA_MAX_BEAM);
+    if (pad_id < 0 || pad_id >= V || eos_id < -1 || eos_id >= V || eos_id == pad_id)
+        return set_error(DBA_EINVAL, "dba_beam_select: eos_id/pad_id must be distinct ids in [0,V) (eos_id may be -1)");
+    if (!logits_dev || !score_dev || !out_token_dev || !out_backptr_dev || !out_score_dev || !out_flags_dev)
+        return set_error(DBA_EINVAL, "dba_beam_select: a pointer is NULL");
+    if (misaligned(logits_dev, elem_bytes(logits_format)))
+        return set_error(DBA_EINVAL, "dba_beam_select: logits_dev must be aligned to its element size");
+    if ((k_in > 1 && row_stride < V) || (B > 1 && sent_stride < 0))
+        return set_error(DBA_EINVAL, "dba_beam_select: row_stride must be at least V and sent_stride not negative");
+    const SelectPlan plan = select_plan(B, k_in, k_out, V, logits_format);
+    if (!workspace_dev || misaligned(workspace_dev, 256))
+        return set_error(DBA_EINVAL, "dba_beam_select: workspace_dev must be 256-byte aligned");
+    if (workspace_bytes < plan.total)
+        return set_error(DBA_ENOMEM, "dba_beam_select: workspace has %zu bytes, %zu needed", workspace_bytes, plan.total);
+    SelectParams p;
+    p.score = score_dev;
+    p.flags = flags_dev;
+    p.out_token = out_token_dev;
+    p.out_backptr = out_backptr_dev;
+    p.out_score = out_score_dev;
+    p.out_flags = out_flags_dev;
+    p.parts = static_cast<SelectPart *>(workspace_dev);
+    p.keys = reinterpret_cast<u64 *>(static_cast<unsigned char *>(workspace_dev) + plan.keys_at);
+    p.sent_stride = sent_stride;
+    p.row_stride = row_stride;
+    p.k_in = k_in;
+    p.k_out = k_out;
+    p.V = V;
+    p.nparts = plan.nparts;
+    p.cap = plan.cap;
+    p.part_chunks = plan.part_chunks;
+    p.eos = eos_id;
+    p.pad = pad_id;
+    const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    (void)hipGetLastError();
+    switch (logits_format) {
+        case DBA_LOGP_F32: select_launch<0>(p, B, logits_dev, stream); break;
+        case DBA_LOGP_F16: select_launch<1>(p, B, logits_dev, stream); break;
+        default: select_launch<2>(p, B, logits_dev, stream); break;
+    }
+    const int rc = launched("dba_beam_select");
+    if (rc != DBA_OK) return rc;
+    if (k_in * plan.nparts * plan.cap <= 4096) dba_select_sentence_kernel<256><<<B, 256, 0, stream>>>(p);
+    else dba_select_sentence_kernel<1024><<<B, 1024, 0, stream>>>(p);
+    return launched("dba_beam_select");
+}
+
+DBA_API int dba_beam_reorder(int B, int k, const int32_t *backptr_dev, const dba_state *states_host, int n_states, void *hip_stream)
+{
+    if (B < 1 || B > 65535 || k < 1 || k > DBA_MAX_BEAM || n_states < 0)
+        return set_error(DBA_EINVAL, "dba_beam_reorder: need 1 <= B <= 65535, 1 <= k <= %d, n_states >= 0", DBA_MAX_BEAM);
+    if (!backptr_dev || (n_states > 0 && !states_host)) return set_error(DBA_EINVAL, "dba_beam_reorder: a pointer is NULL");
+    // everything is looked at before anything is launched
+    for (int i = 0; i < n_states; ++i) {
+        const dba_state &s = states_host[i];
+        if (s.segs < 0 || s.seg_bytes < 0) return set_error(DBA_EINVAL, "dba_beam_reorder: state %d has a negative size", i);
+        if (s.segs == 0 || s.seg_bytes == 0) continue;
+        if (!s.dst || !s.src) return set_error(DBA_EINVAL, "dba_beam_reorder: a pointer of state %d is NULL", i);
+        const int64_t count[3] = {B, k, s.segs};
+        const int64_t ds[3] = {s.dst_sent, s.dst_row, s.dst_seg}, ss[3] = {s.src_sent, s.src_row, s.src_seg};
+        __int128 d_end = s.seg_bytes, s_end = s.seg_bytes;
+        int order[3] = {0, 1, 2};
+        std::sort(order, order + 3, [&](int x, int y) { return ds[x] < ds[y]; });
+        for (int x = 0; x < 3; ++x) {
+            const int o = order[x];
+            if (count[o] == 1) continue;
+            if (ds[o] < d_end) return set_error(DBA_EINVAL, "dba_beam_reorder: pieces of state %d's dst overlap", i);
+            d_end += (__int128)ds[o] * (count[o] - 1);
+        }
+        for (int x = 0; x < 3; ++x) {
+            if (count[x] == 1) continue;
+            if (ss[x] < 0) return set_error(DBA_EINVAL, "dba_beam_reorder: state %d has a negative stride", i);
+            s_end += (__int128)ss[x] * (count[x] - 1);
+        }
+        if (d_end > ((__int128)1 << 62) || s_end > ((__int128)1 << 62))
+            return set_error(DBA_EINVAL, "dba_beam_reorder: state %d is larger than memory", i);
+        const unsigned char *d = static_cast<unsigned char *>(s.dst), *c = static_cast<const unsigned char *>(s.src);
+        if (d == c) {
+            for (int x = 0; x < 3; ++x)
+                if (count[x] > 1 && ds[x] != ss[x])
+                    return set_error(DBA_EINVAL, "dba_beam_reorder: state %d is reordered in place with two sets of strides", i);
+        } else if (d < c + (int64_t)s_end && c < d + (int64_t)d_end) {
+            return set_error(DBA_EINVAL, "dba_beam_reorder: dst and src of state %d overlap", i);
+        }
+        if ((__int128)s.segs * s.seg_bytes > ((__int128)1 << 31))
+            return set_error(DBA_EINVAL, "dba_beam_reorder: a row of state %d has more than 2 GB", i);
+    }
+    const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    (void)hipGetLastError();
+    ReorderParams p;
+    p.back = backptr_dev;
+    p.k = k;
+    p.n_states = 0;
+    uint32_t blocks = 0;
+    const auto flush = [&]() -> int {
+        if (!p.n_states) return DBA_OK;
+        const dim3 grid(blocks, (unsigned)B);
+        if (k <= 4) dba_reorder_kernel<4><<<grid, kReorderThreads, 0, stream>>>(p);
+        else if (k <= 8) dba_reorder_kernel<8><<<grid, kReorderThreads, 0, stream>>>(p);
+        else if (k <= 16) dba_reorder_kernel<16><<<grid, kReorderThreads, 0, stream>>>(p);
+        else if (k <= 32) dba_reorder_kernel<32><<<grid, kReorderThreads, 0, stream>>>(p);
+        else dba_reorder_kernel<64><<<grid, kReorderThreads, 0, stream>>>(p);
+        p.n_states = 0;
+        blocks = 0;
+        return launched("dba_beam_reorder");
+    };
+    for (int i = 0; i < n_states; ++i) {
+        dba_state s = states_host[i];
+        if (s.segs == 0 || s.seg_bytes == 0) continue;
+        if (s.segs > 1 && s.dst_seg == s.seg_bytes && s.src_seg == s.seg_bytes) {
+            s.seg_bytes *= s.segs;
+            s.segs = 1;
+        }
+        uintptr_t bits = reinterpret_cast<uintptr_t>(s.dst) | reinterpret_cast<uintptr_t>(s.src) | (uintptr_t)s.seg_bytes;
+        if (B > 1) bits |= (uintptr_t)(s.dst_sent | s.src_sent);
+        if (k > 1) bits |= (uintptr_t)(s.dst_row | s.src_row);
+        if (s.segs > 1) bits |= (uintptr_t)(s.dst_seg | s.src_seg);
+        const uint32_t widest = k > 32 ? 8 : 16;       // 64 columns of 16 bytes are more than a thread has registers for
+        const uint32_t col = std::min<uint32_t>(widest, (uint32_t)(bits & (~bits + 1)) ? (uint32_t)std::min<uintptr_t>(bits & (~bits + 1), 16) : 16u);
+        const uint64_t columns = (uint64_t)(s.segs * s.seg_bytes) / col;
+        const uint32_t more = (uint32_t)((columns + kReorderThreads - 1) / kReorderThreads);
+        if (p.n_states == kReorderStates || (uint64_t)blocks + more > (1u << 23)) {
+            const int rc = flush();
+            if (rc != DBA_OK) return rc;
+        }
+        ReorderState &r = p.s[p.n_states++];
+        r.dst = static_cast<unsigned char *>(s.dst);
+        r.src = static_cast<const unsigned char *>(s.src);
+        r.dst_sent = s.dst_sent;
+        r.dst_row = s.dst_row;
+        r.dst_seg = s.dst_seg;
+        r.src_sent = s.src_sent;
+        r.src_row = s.src_row;
+        r.src_seg = s.src_seg;
+        r.segs = (uint32_t)s.segs;
+        r.per_seg = (uint32_t)(s.seg_bytes / col);
+        r.col_bytes = col;
+        r.first_block = blocks;
+        blocks += more;
+    }
+    return flush();
+}
+
+DBA_API int dba_cache_append(int B, int n, const dba_cache *cache, const dba_heads *k, const dba_heads *v, int q_heads, const dba_heads *q,
+                             const dba_heads *q_out, const int32_t *first_dev, const int32_t *count_dev, const int32_t *position_dev,
+                             const float *inv_freq_dev, int rot_dim, int interleaved, void *hip_stream)
+{
+    const char *fault = cache_fault(cache);
+    if (fault) return set_error(DBA_EINVAL, "dba_cache_append: %s", fault);
+    if (B < 1 || B > 65535 || n < 1 || n > kMostRows) return set_error(DBA_EINVAL, "dba_cache_append: need 1 <= B <= 65535, 1 <= n <= 2^22");
+    if ((fault = heads_fault(k, cache->format)) || (fault = heads_fault(v, cache->format)))
+        return set_error(DBA_EINVAL, "dba_cache_append: %s", fault);
+    if ((q != nullptr) != (q_out != nullptr)) return set_error(DBA_EINVAL, "dba_cache_append: q and q_out go together");
+    if (q) {
+        if ((fault = heads_fault(q, cache->format)) || (fault = heads_fault(q_out, cache->format)))
+            return set_error(DBA_EINVAL, "dba_cache_append: %s", fault);
+        if (q_heads < 1 || q_heads > 8192) return set_error(DBA_EINVAL, "dba_cache_append: 1 <= q_heads <= 8192");
+        if (q->data == q_out->data && (q->sent_stride != q_out->sent_stride || q->token_stride != q_out->token_stride || q->head_stride != q_out->head_stride))
+            return set_error(DBA_EINVAL, "dba_cache_append: q is rotated in place with two sets of strides");
+    }
+    if (!first_dev) return set_error(DBA_EINVAL, "dba_cache_append: first_dev is NULL");
+    if (rot_dim < 0 || rot_dim > cache->head_dim || rot_dim % 16) return set_error(DBA_EINVAL, "dba_cache_append: rot_dim must be a multiple of 16, at most head_dim");
+    if (rot_dim && !inv_freq_dev) return set_error(DBA_EINVAL, "dba_cache_append: inv_freq_dev is NULL");
+    AppendParams p;
+    p.cache = paged_of(*cache);
+    p.k_pages = static_cast<unsigned char *>(cache->k);
+    p.v_pages = static_cast<unsigned char *>(cache->v);
+    p.q = heads_of(q);
+    p.q_out = heads_of(q_out);
+    p.k = heads_of(k);
+    p.v = heads_of(v);
+    p.first = first_dev;
+    p.count = count_dev;
+    p.position = position_dev;
+    p.inv_freq = inv_freq_dev;
+    p.n = n;
+    p.heads = cache->heads;
+    p.q_heads = q ? q_heads : 0;
+    p.D = cache->head_dim;
+    p.rot = rot_dim;
+    p.interleaved = interleaved != 0;
+    const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    const dim3 grid((unsigned)n, (unsigned)B);
+    (void)hipGetLastError();
+    switch (cache->format) {
+        case DBA_LOGP_F32: dba_append_kernel<0><<<grid, kAppendThreads, 0, stream>>>(p); break;
+        case DBA_LOGP_F16: dba_append_kernel<1><<<grid, kAppendThreads, 0, stream>>>(p); break;
+        default: dba_append_kernel<2><<<grid, kAppendThreads, 0, stream>>>(p); break;
+    }
+    return launched("dba_cache_append");
+}
+
+DBA_API size_t dba_tree_attend_workspace_bytes(int B, int n, int q_heads, const dba_cache *cache, int max_len)
+{
+    (void)B, (void)n, (void)q_heads, (void)cache, (void)max_len;
+    return 0;
+}
+
+DBA_API int dba_tree_attend(int B, int n, int q_heads, const dba_heads *q, const dba_cache *cache, const int32_t *prefix_dev,
+                            const int32_t *tree_dev, const uint64_t *mask_dev, int mask_words, int max_len, float scale,
+                            const dba_heads *out, float *out_lse_dev, void *workspace_dev, size_t workspace_bytes, void *hip_stream)
+{
+    (void)workspace_dev, (void)workspace_bytes;
+    const char *fault = cache_fault(cache);
+    if (fault) return set_error(DBA_EINVAL, "dba_tree_attend: %s", fault);
+    if (B < 1 || B > 65535 || n < 1 || q_heads < 1 || q_heads > 8192 || (int64_t)n * q_heads > kMostRows)
+        return set_error(DBA_EINVAL, "dba_tree_attend: need 1 <= B <= 65535, 1 <= q_heads <= 8192, n >= 1, n * q_heads <= 2^22");
+    if (q_heads % cache->heads) return set_error(DBA_EINVAL, "dba_tree_attend: q_heads must be a multiple of the cache's heads");
+    if ((fault = heads_fault(q, cache->format)) || (fault = heads_fault(out, cache->format)))
+        return set_error(DBA_EINVAL, "dba_tree_attend: %s", fault);
+    if (!prefix_dev) return set_error(DBA_EINVAL, "dba_tree_attend: prefix_dev is NULL");
+    if (mask_words < 0 || (mask_dev && !tree_dev)) return set_error(DBA_EINVAL, "dba_tree_attend: a mask needs tree_dev and mask_words >= 0");
+    if (max_len < 1 || max_len > cache->max_pages * cache->page_size)
+        return set_error(DBA_EINVAL, "dba_tree_attend: need 1 <= max_len <= max_pages * page_size");
+    if (!(fabsf(scale) < INFINITY)) return set_error(DBA_EINVAL, "dba_tree_attend: scale is not a finite number");
+    AttendParams p;
+    p.cache = paged_of(*cache);
+    p.k_pages = static_cast<const unsigned char *>(cache->k);
+    p.v_pages = static_cast<const unsigned char *>(cache->v);
+    p.q = heads_of(q);
+    p.out = heads_of(out);
+    p.prefix = prefix_dev;
+    p.tree = tree_dev;
+    p.mask = reinterpret_cast<const unsigned long long *>(mask_dev);
+    p.lse = out_lse_dev;
+    p.n = n;
+    p.q_heads = q_heads;
+    p.heads = cache->heads;
+    p.D = cache->head_dim;
+    p.mask_words = mask_words;
+    p.max_len = max_len;
+    p.scale = scale;
+    const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    const dim3 grid((unsigned)(n * q_heads), (unsigned)B);
+    (void)hipGetLastError();
+    switch (cache->format) {
+        case DBA_LOGP_F32: dba_attend_simple_kernel<0><<<grid, 256, 0, stream>>>(p); break;
+        case DBA_LOGP_F16: dba_attend_simple_kernel<1><<<grid, 256, 0, stream>>>(p); break;
+        default: dba_attend_simple_kernel<2><<<grid, 256, 0, stream>>>(p); break;
+    }
+    return launched("dba_tree_attend");
+}
+
+}  // extern "C"
