@@ -9,10 +9,11 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdba.so")
 OBJ = os.path.join(HERE, "build")
-SOURCES = [os.path.join(CSRC, f) for f in ("dba.hip", "dba_beam.hip")]
+SOURCES = [os.path.join(CSRC, f) for f in (
+    "dba.hip", "dba_beam.hip", "dba_attend_f32.hip", "dba_attend_f16.hip", "dba_attend_bf16.hip")]
 DEPS = SOURCES + [os.path.join(CSRC, f) for f in (
     "dba_kernels.hpp", "wave_topk.hpp", "host_blocks.hpp", "entry.hpp", "paged.hpp", "beam_select.hpp", "beam_reorder.hpp",
-    "cache_append.hpp", "tree_attend.hpp")] + [
+    "cache_append.hpp", "tree_attend.hpp", "tree_attend_launch.hpp")] + [
     os.path.join(os.path.dirname(HERE), "include", f) for f in ("dba.h", "dba_debug.h", "dba_beam.h")]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

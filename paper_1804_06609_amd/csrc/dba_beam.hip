@@ -13,6 +13,12 @@
 
 using namespace dba;
 
+namespace dba {
+extern template hipError_t attend_launch<0>(const AttendParams &, const AttendPlan &, int, hipStream_t);
+extern template hipError_t attend_launch<1>(const AttendParams &, const AttendPlan &, int, hipStream_t);
+extern template hipError_t attend_launch<2>(const AttendParams &, const AttendPlan &, int, hipStream_t);
+}  // namespace dba
+
 namespace {
 
 constexpr size_t align256(size_t x) { return (x + 255) / 256 * 256; }
@@ -101,6 +107,41 @@ HeadsAt heads_of(const dba_heads *h)
     if (!h) return HeadsAt{nullptr, 0, 0, 0};
     return HeadsAt{static_cast<unsigned char *>(h->data), h->sent_stride, h->token_stride, h->head_stride};
 }
+
+AttendPlan attend_plan(int B, int n, int q_heads, const dba_cache &c, int max_len)
+{
+    AttendPlan a;
+    const int rows = n * (q_heads / c.heads);
+    a.DP = c.head_dim <= 64 ? 64 : c.head_dim <= 128 ? 128 : 256;
+    const int widest = a.DP <= 128 ? 4 : 2;            // 16-row tiles a wave has registers for
+    a.shared = rows > 16 * widest;
+    a.QT = a.shared ? (rows > 128 ? widest : 2) : rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+    a.tile_rows = (a.shared ? 64 : 16) * a.QT;
+    a.row_tiles = (rows + a.tile_rows - 1) / a.tile_rows;
+    a.tile = a.shared ? 64 : c.format == DBA_LOGP_F32 ? 16 : 32;
+    const int tiles = (max_len + a.tile - 1) / a.tile + 1;         // (the prefix and the tree each end in a tile of their own)
+    const int64_t groups = (int64_t)B * c.heads * a.row_tiles;
+    const int64_t want = std::max<int64_t>(1, (1024 + groups - 1) / groups);
+    const int least = a.shared ? 4 : 8;
+    int64_t chunk = std::max<int64_t>(least, (tiles + want - 1) / want);
+    chunk = (chunk + 3) / 4 * 4;
+    a.chunk = (int)chunk;
+    a.splits = (int)((tiles + chunk - 1) / chunk);
+    return a;
+}
+
+const char *attend_fault(int B, int n, int q_heads, const dba_cache *cache, int max_len)
+{
+    const char *fault = cache_fault(cache);
+    if (fault) return fault;
+    if (B < 1 || B > 65535 || n < 1 || q_heads < 1 || q_heads > 8192 || (int64_t)n * q_heads > kMostRows)
+        return "need 1 <= B <= 65535, 1 <= q_heads <= 8192, n >= 1, n * q_heads <= 2^22";
+    if (q_heads % cache->heads) return "q_heads must be a multiple of the cache's heads";
+    if (max_len < 1 || max_len > cache->max_pages * cache->page_size) return "need 1 <= max_len <= max_pages * page_size";
+    return nullptr;
+}
+
+size_t attend_rows_of(int B, int n, int q_heads, const AttendPlan &a) { return (size_t)B * n * q_heads * a.splits; }
 
 // the two launches of a selection
 template <int FMT>
@@ -319,27 +360,30 @@ DBA_API int dba_cache_append(int B, int n, const dba_cache *cache, const dba_hea
 
 DBA_API size_t dba_tree_attend_workspace_bytes(int B, int n, int q_heads, const dba_cache *cache, int max_len)
 {
-    (void)B, (void)n, (void)q_heads, (void)cache, (void)max_len;
-    return 0;
+    if (attend_fault(B, n, q_heads, cache, max_len)) return 0;
+    const AttendPlan a = attend_plan(B, n, q_heads, *cache, max_len);
+    if (a.splits == 1) return 0;
+    const size_t rows = attend_rows_of(B, n, q_heads, a);
+    return align256(rows * cache->head_dim * 4) + align256(rows * 8);
 }
 
 DBA_API int dba_tree_attend(int B, int n, int q_heads, const dba_heads *q, const dba_cache *cache, const int32_t *prefix_dev,
                             const int32_t *tree_dev, const uint64_t *mask_dev, int mask_words, int max_len, float scale,
                             const dba_heads *out, float *out_lse_dev, void *workspace_dev, size_t workspace_bytes, void *hip_stream)
 {
-    (void)workspace_dev, (void)workspace_bytes;
-    const char *fault = cache_fault(cache);
+    const char *fault = attend_fault(B, n, q_heads, cache, max_len);
     if (fault) return set_error(DBA_EINVAL, "dba_tree_attend: %s", fault);
-    if (B < 1 || B > 65535 || n < 1 || q_heads < 1 || q_heads > 8192 || (int64_t)n * q_heads > kMostRows)
-        return set_error(DBA_EINVAL, "dba_tree_attend: need 1 <= B <= 65535, 1 <= q_heads <= 8192, n >= 1, n * q_heads <= 2^22");
-    if (q_heads % cache->heads) return set_error(DBA_EINVAL, "dba_tree_attend: q_heads must be a multiple of the cache's heads");
     if ((fault = heads_fault(q, cache->format)) || (fault = heads_fault(out, cache->format)))
         return set_error(DBA_EINVAL, "dba_tree_attend: %s", fault);
     if (!prefix_dev) return set_error(DBA_EINVAL, "dba_tree_attend: prefix_dev is NULL");
     if (mask_words < 0 || (mask_dev && !tree_dev)) return set_error(DBA_EINVAL, "dba_tree_attend: a mask needs tree_dev and mask_words >= 0");
-    if (max_len < 1 || max_len > cache->max_pages * cache->page_size)
-        return set_error(DBA_EINVAL, "dba_tree_attend: need 1 <= max_len <= max_pages * page_size");
-    if (!(fabsf(scale) < INFINITY)) return set_error(DBA_EINVAL, "dba_tree_attend: scale is not a finite number");
+    if (!(fabsf(scale) <= 1e30f)) return set_error(DBA_EINVAL, "dba_tree_attend: scale is not a number between -1e30 and 1e30");
+    const AttendPlan plan = attend_plan(B, n, q_heads, *cache, max_len);
+    const size_t need = dba_tree_attend_workspace_bytes(B, n, q_heads, cache, max_len);
+    if (need) {
+        if (!workspace_dev || misaligned(workspace_dev, 256)) return set_error(DBA_EINVAL, "dba_tree_attend: workspace_dev must be 256-byte aligned");
+        if (workspace_bytes < need) return set_error(DBA_ENOMEM, "dba_tree_attend: workspace has %zu bytes, %zu needed", workspace_bytes, need);
+    }
     AttendParams p;
     p.cache = paged_of(*cache);
     p.k_pages = static_cast<const unsigned char *>(cache->k);
@@ -357,15 +401,17 @@ DBA_API int dba_tree_attend(int B, int n, int q_heads, const dba_heads *q, const
     p.mask_words = mask_words;
     p.max_len = max_len;
     p.scale = scale;
+    p.row_tiles = plan.row_tiles;
+    p.tile_rows = plan.tile_rows;
+    p.splits = plan.splits;
+    p.chunk = plan.chunk;
+    p.part_o = static_cast<float *>(workspace_dev);
+    p.part_ml = reinterpret_cast<float *>(static_cast<unsigned char *>(workspace_dev) + align256(attend_rows_of(B, n, q_heads, plan) * cache->head_dim * 4));
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    const dim3 grid((unsigned)(n * q_heads), (unsigned)B);
     (void)hipGetLastError();
-    switch (cache->format) {
-        case DBA_LOGP_F32: dba_attend_simple_kernel<0><<<grid, 256, 0, stream>>>(p); break;
-        case DBA_LOGP_F16: dba_attend_simple_kernel<1><<<grid, 256, 0, stream>>>(p); break;
-        default: dba_attend_simple_kernel<2><<<grid, 256, 0, stream>>>(p); break;
-    }
-    return launched("dba_tree_attend");
+    const hipError_t e = cache->format == DBA_LOGP_F32 ? attend_launch<0>(p, plan, B, stream)
+                       : cache->format == DBA_LOGP_F16 ? attend_launch<1>(p, plan, B, stream) : attend_launch<2>(p, plan, B, stream);
+    return e == hipSuccess ? DBA_OK : set_error(DBA_EHIP, "dba_tree_attend: launch failed: %s", hipGetErrorString(e));
 }
 
 }  // extern "C"

@@ -1,4 +1,14 @@
 // Attention of a tree's nodes over a paged cache: kernels.
+//
+// For one sentence and one head of the cache, the queries that read it are rows: row r is node r / G, query head r % G of the
+// G that share the head.  With x = scale log2 e (q . k), a row's output is sum 2^(x_t - m) v_t / sum 2^(x_t - m) over the tokens it
+// sees, m being the running maximum; parts of the token axis are joined by their maxima and sums.
+//
+// Both products run on the matrix units, transposed: S^T = K Q^T leaves lane (g, c) of a wave (c = lane % 16, g = lane / 16) with
+// four consecutive tokens 4g .. 4g+3 of row c, which is what the second product O^T = V^T P^T takes as its right operand: the
+// probabilities never leave the registers, the softmax's statistics are one number a lane, and joining a row's
+// lanes takes two exchanges.  V^T, its left operand, comes out of LDS through the transposing read.  The order of tokens
+// inside a product's sum is arbitrary as long as both sides have the same.
 #pragma once
 #include "cache_append.hpp"
 #include "paged.hpp"
@@ -12,68 +22,574 @@ struct AttendParams {
     const int32_t *prefix, *tree;
     const unsigned long long *mask;
     float *lse;
+    float *part_o, *part_ml;           // of split launches: [B, heads, splits, rows, D] and [.., 2]
     int n, q_heads, heads, D, mask_words, max_len;
+    int row_tiles, tile_rows;          // workgroups along the rows, rows of each
+    int splits, chunk;                 // workgroups along the token axis, tiles of each
     float scale;
 };
 
-// One query head of one node a workgroup, a token a wave at a time, the running maximum and sum of the softmax in fp32.
-template <int FMT>
-__global__ __launch_bounds__(256) void dba_attend_simple_kernel(AttendParams p)
+// Tokens of a sentence that the workgroup of row r looks at: of a chain those up to tree - n + its last node.
+__device__ __forceinline__ Span span_of_rows(const AttendParams &p, int b, int row_tile, int G, int &tree_all)
 {
-    typedef typename Elem<FMT>::type E;
-    __shared__ float s_m[4], s_l[4], s_o[4][256];
-    const int t = (int)threadIdx.x, lane = t & 63, wave = t >> 6;
-    const int h = (int)blockIdx.x % p.q_heads, i = (int)blockIdx.x / p.q_heads, b = (int)blockIdx.y;
-    const int64_t kv_head = (int64_t)(h / (p.q_heads / p.heads)) * p.cache.head_stride;
-    const Span span = span_of(p.prefix[b], p.tree ? p.tree[b] : 0, p.max_len);
-    const int tree = p.tree ? max(p.tree[b], 0) : 0;
-    const E *q = reinterpret_cast<const E *>(p.q.data) + (b * p.q.sent + i * p.q.token + h * p.q.head);
-    float x[4], o[4] = {0.0f, 0.0f, 0.0f, 0.0f}, m = -INFINITY, l = 0.0f;
+    tree_all = p.tree ? max(p.tree[b], 0) : 0;
+    Span s = span_of(p.prefix[b], tree_all, p.max_len);
+    if (!p.mask) {
+        const int last = min((row_tile + 1) * p.tile_rows, p.n * G) - 1;
+        s.end = min(s.end, s.prefix + max(0, tree_all - p.n + last / G + 1));
+    }
+    return s;
+}
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLn2f = 0.69314718055994530942f;
+
+// Eight elements of a row along the contraction: 16 bytes, or 32 in fp32.
+template <int FMT> struct Frag {
+    static constexpr int C = FMT == 0 ? 2 : 1;
+    uint4 c[C];
+};
+
+// c += a b^T of 16 rows each over 32 elements; lane (g, i) gives elements 8g .. 8g+7 of row i of a and of b.  In fp32 the products come four
+// at a time, one of each lane's eight.
+template <int FMT>
+__device__ __forceinline__ f32x4 mfma32(const Frag<FMT> &a, const Frag<FMT> &b, f32x4 c)
+{
+    if constexpr (FMT == 0) {
+        const float *x = reinterpret_cast<const float *>(&a), *y = reinterpret_cast<const float *>(&b);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) x[j] = lane + 64 * j < p.D ? (float)q[lane + 64 * j] * p.scale : 0.0f;
-    for (int tok = wave; tok < span.end; tok += 4) {
-        if (tok >= span.prefix) {
-            const int j = tok - span.prefix;
-            if (!p.mask) {
-                if (j > tree - p.n + i) continue;
-            } else if (j >= 64 * p.mask_words || !((p.mask[((int64_t)b * p.n + i) * p.mask_words + (j >> 6)] >> (j & 63)) & 1)) {
-                continue;
+        for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[j], y[j], c, 0, 0, 0);
+        return c;
+    } else if constexpr (FMT == 1) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a.c[0]), __builtin_bit_cast(f16x8, b.c[0]), c, 0, 0, 0);
+    } else {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a.c[0]), __builtin_bit_cast(bf16x8, b.c[0]), c, 0, 0, 0);
+    }
+}
+
+template <int FMT>
+__device__ __forceinline__ uint32_t pack2(float a, float b)
+{
+    if constexpr (FMT == 1) {
+        typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+        const h2 v = {(_Float16)a, (_Float16)b};
+        return __builtin_bit_cast(uint32_t, v);
+    } else {
+        typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+        const b2 v = {(__bf16)a, (__bf16)b};
+        return __builtin_bit_cast(uint32_t, v);
+    }
+}
+
+// Which of a chunk's elements are not finite are made 0; true if there were any.
+template <int FMT>
+__device__ __forceinline__ bool make_finite(uint4 &c)
+{
+    uint32_t *w = reinterpret_cast<uint32_t *>(&c);
+    bool found = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (FMT == 0) {
+            if ((w[i] & 0x7F800000u) == 0x7F800000u) w[i] = 0, found = true;
+        } else {
+            constexpr uint32_t E = FMT == 1 ? 0x7C00u : 0x7F80u;
+            if ((w[i] & E) == E) w[i] &= 0xFFFF0000u, found = true;
+            if ((w[i] & (E << 16)) == (E << 16)) w[i] &= 0xFFFFu, found = true;
+        }
+    }
+    return found;
+}
+
+__device__ __forceinline__ float max_over_groups(float v)      // over the four lanes of a row
+{
+    v = fmaxf(v, __shfl_xor(v, 16));
+    return fmaxf(v, __shfl_xor(v, 32));
+}
+__device__ __forceinline__ float sum_over_groups(float v)
+{
+    v += __shfl_xor(v, 16);
+    return v + __shfl_xor(v, 32);
+}
+
+// How a kernel's LDS is laid out.  ROWS: the four waves have rows of their own and share tiles of 64 tokens, keys and values both in LDS;
+// else they have all rows and tiles of their own (32 tokens, 16 in fp32), keys straight in registers, values in LDS.
+template <int FMT, int DP, int QT, bool ROWS>
+struct AttendShape {
+    static constexpr int ES = FMT == 0 ? 4 : 2;
+    static constexpr int KS = DP / 32;                  // steps of 32 elements
+    static constexpr int DT = DP / 16;                  // tiles of 16 elements
+    static constexpr int NT = ROWS || FMT == 0 ? 1 : 2; // 16-token tiles a wave loads at a time
+    static constexpr int CT = ROWS ? 4 : NT;            // and works on at a time
+    static constexpr int TT = 16 * CT;
+    static constexpr int ROW = DP * ES;                 // bytes
+    static constexpr int CH = ROW / 16;
+    static constexpr int RK = CH >= 16 ? 1 : 16 / CH;   // tokens whose rows share 256 bytes
+    static constexpr int TILE = TT * ROW;
+    static constexpr int BUFS = ROWS ? (4 * TILE <= 131072 ? 2 : 1) : 1;
+    static constexpr int LOOP = ROWS ? 2 * TILE * BUFS : 4 * TILE;
+    static constexpr int JOIN = ROWS ? 0 : 4 * QT * (DT / 4) * 1024;
+    static constexpr int LDS = LOOP > JOIN ? LOOP : JOIN;
+    static constexpr int REGS = QT * (DT * 4 + KS * 4 * (FMT == 0 ? 2 : 1)) + 2 * NT * KS * 4 * (FMT == 0 ? 2 : 1) + CT * QT * 4;
+    static constexpr int PER_SIMD = REGS <= 190 ? 2 : 1;
+
+    // A row's chunks are rotated, so that 16 lanes that read one chunk of 16 rows (keys), or 32 lanes that read 32 bytes of eight
+    // rows (values; 64 of four in fp32), meet all 64 banks.
+    static __device__ __forceinline__ int key_at(int token, int chunk)
+    {
+        return token * ROW + ((chunk + (token % 16) / RK) & (CH - 1)) * 16;
+    }
+    static __device__ __forceinline__ int value_at(int token, int chunk)
+    {
+        if constexpr (FMT == 0) return token * ROW + (((chunk >> 2) + (token >> 2)) & (CH / 4 - 1)) * 64 + (chunk & 3) * 16;
+        else return token * ROW + (((chunk >> 1) + (token % 16) / RK) & (CH / 2 - 1)) * 32 + (chunk & 1) * 16;
+    }
+};
+
+// Grid: x = row tile + row_tiles * split, y = head of the cache, z = sentence.
+template <int FMT, int DP, int QT, bool ROWS>
+__global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) void dba_attend_kernel(AttendParams p)
+{
+    typedef AttendShape<FMT, DP, QT, ROWS> A;
+    typedef typename Elem<FMT>::type E;
+    constexpr int KS = A::KS, DT = A::DT, NT = A::NT, CT = A::CT, TT = A::TT, FC = Frag<FMT>::C, NE = 16 / A::ES;
+    extern __shared__ unsigned char s_mem[];
+    __shared__ float s_ml[4][16 * QT][2];
+    __shared__ unsigned long long s_bad[2][4], s_live[2][4];
+    const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int c = lane & 15, g = lane >> 4;
+    const int row_tile = (int)blockIdx.x % p.row_tiles, split = (int)blockIdx.x / p.row_tiles;
+    const int head = (int)blockIdx.y, b = (int)blockIdx.z;
+    const int G = p.q_heads / p.heads, rows = p.n * G;
+    const int row0 = (ROWS ? row_tile * 4 + wave : row_tile) * 16 * QT;
+
+    int tree_all;
+    const Span span = span_of_rows(p, b, row_tile, G, tree_all);
+    const int tree = span.end - span.prefix;
+    const int prefix_tiles = (span.prefix + TT - 1) / TT, tiles = prefix_tiles + (tree + TT - 1) / TT;
+    const int u0 = split * p.chunk, u1 = min(tiles, u0 + p.chunk);
+    if (u0 >= tiles && split > 0) return;              // (the join does not ask for it; the first split is always there)
+
+    // the queries, and what rows they are
+    Frag<FMT> q[QT][KS];
+    const unsigned long long *mask_row[QT];
+    int chain[QT];                                     // the last tree token a row of a chain sees
+    const float qsign = p.scale < 0.0f ? -1.0f : 1.0f;
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+        const int r = row0 + t * 16 + c, node = min(r, rows - 1) / G, h = head * G + min(r, rows - 1) % G;
+        const E *src = reinterpret_cast<const E *>(p.q.data) + ((int64_t)b * p.q.sent + (int64_t)node * p.q.token + (int64_t)h * p.q.head);
+        mask_row[t] = p.mask ? p.mask + ((int64_t)b * p.n + node) * p.mask_words : nullptr;
+        chain[t] = tree_all - p.n + node;
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+#pragma unroll
+            for (int f = 0; f < FC; ++f) {
+                const int d = k * 32 + g * 8 + f * NE;
+                uint4 v = make_uint4(0, 0, 0, 0);
+                if (r < rows && d < p.D && p.scale != 0.0f) v = *reinterpret_cast<const uint4 *>(src + d);
+                if (qsign < 0.0f) {
+                    uint32_t *w = reinterpret_cast<uint32_t *>(&v);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) w[i] ^= FMT == 0 ? 0x80000000u : 0x80008000u;
+                }
+                q[t][k].c[f] = v;
             }
         }
-        const int64_t at = token_offset(p.cache, b, tok);
-        if (at < 0) continue;
-        const E *k = reinterpret_cast<const E *>(p.k_pages) + (at + kv_head), *v = reinterpret_cast<const E *>(p.v_pages) + (at + kv_head);
-        float s = 0.0f;
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (lane + 64 * j < p.D) s += x[j] * (float)k[lane + 64 * j];
-#pragma unroll
-        for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
-        const float m1 = fmaxf(m, s);
-        const float keep = m1 == m ? 1.0f : __expf(m - m1), w = __expf(s - m1);
-        m = m1;
-        l = l * keep + w;
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (lane + 64 * j < p.D) o[j] = o[j] * keep + w * (float)v[lane + 64 * j];
     }
-    if (lane == 0) {
-        s_m[wave] = m;
-        s_l[wave] = l;
-    }
+    const float sl2 = p.scale != 0.0f ? fabsf(p.scale) * kLog2e : 1.0f;    // (without a scale the queries are 0)
+
+    // tokens of tile u that this wave loads: 16 * (ROWS ? wave : 0) + 16 t + c
+    const int load0 = ROWS ? wave * 16 : 0;
+    const int step = ROWS ? 1 : 4, first = ROWS ? u0 : u0 + wave;
+    auto page_of = [&](int u, int t) -> int {          // -1: no such token
+        const bool in_tree = u >= prefix_tiles;
+        const int pos = (in_tree ? span.prefix + (u - prefix_tiles) * TT : u * TT) + load0 + t * 16 + c;
+        const int lim = in_tree ? span.prefix + tree : span.prefix;
+        int page = -1;
+        if (u < u1 && pos < lim) page = p.cache.table[(int64_t)b * p.cache.table_stride + (pos >> p.cache.page_shift)];
+        return (uint32_t)page < (uint32_t)p.cache.n_pages ? page : -1;
+    };
+    const int64_t head_at = (int64_t)head * p.cache.head_stride;
+    auto offset_of = [&](int u, int t, int page) -> int64_t {      // of a token that is not there: of one that is
+        if (page < 0) return head_at;
+        const int pos = (u >= prefix_tiles ? span.prefix + (u - prefix_tiles) * TT : u * TT) + load0 + t * 16 + c;
+        return (int64_t)page * p.cache.page_stride + (int64_t)(pos & ((1 << p.cache.page_shift) - 1)) * p.cache.token_stride + head_at;
+    };
+    uint4 kr[NT][KS][FC], vr[NT][KS][FC];
+    // a chunk behind the head's end is read as its first: the queries have 0 there, and nobody asks for those outputs
+    auto load = [&](const unsigned char *pool, uint4 (&to)[KS][FC], int64_t at) {
+        const E *src = reinterpret_cast<const E *>(pool) + at;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) s_o[wave][lane + 64 * j] = o[j];
-    __syncthreads();
-    float top = -INFINITY, sum = 0.0f, y = 0.0f;
-    for (int w = 0; w < 4; ++w) top = fmaxf(top, s_m[w]);
-    for (int w = 0; w < 4; ++w) {
-        const float f = s_l[w] != 0.0f ? __expf(s_m[w] - top) : 0.0f;     // (a NaN is not nothing)
-        sum += s_l[w] * f;
-        if (t < p.D && f != 0.0f) y += s_o[w][t] * f;
+        for (int k = 0; k < KS; ++k)
+#pragma unroll
+            for (int f = 0; f < FC; ++f) {
+                const int d = k * 32 + g * 8 + f * NE;
+                to[k][f] = *reinterpret_cast<const uint4 *>(src + (d < p.D ? d : 0));
+            }
+    };
+
+    f32x4 o[QT][DT];
+    float m[QT], l[QT];
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+        m[t] = -INFINITY;
+        l[t] = 0.0f;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[t][d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
-    E *out = reinterpret_cast<E *>(p.out.data) + (b * p.out.sent + i * p.out.token + h * p.out.head);
-    if (t < p.D) out[t] = (E)(sum != 0.0f ? y / sum : 0.0f);
-    if (t == 0 && p.lse) p.lse[((int64_t)b * p.n + i) * p.q_heads + h] = sum != 0.0f ? top + __logf(sum) : -INFINITY;
+
+    unsigned char *const s_v = s_mem + (ROWS ? A::TILE * A::BUFS : wave * A::TILE);
+    int page[NT], page_next[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        page[t] = page_of(first, t);
+        page_next[t] = page_of(first + step, t);
+    }
+    if (first < u1) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const int64_t at = offset_of(first, t, page[t]);
+            load(p.k_pages, kr[t], at);
+            load(p.v_pages, vr[t], at);
+        }
+    }
+
+    int buf = 0;
+    for (int u = first; u < u1; u += step) {
+        const bool in_tree = u >= prefix_tiles;
+        const int j0 = (u - prefix_tiles) * TT;        // of a tile of the tree
+        unsigned char *const kb = s_mem + buf * A::TILE, *const vb = s_v + (ROWS ? buf * A::TILE : 0);
+        // which rows see which tokens of the tile (bit t: token t)
+        unsigned long long seen[QT];
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+            seen[t] = ~0ull;
+            if (in_tree) {
+                if (p.mask) {
+                    seen[t] = (j0 >> 6) < p.mask_words ? mask_row[t][j0 >> 6] >> (j0 & 63) : 0;
+                } else {
+                    const int last = chain[t] - j0;
+                    seen[t] = last < 0 ? 0 : last >= 63 ? ~0ull : (2ull << last) - 1;
+                }
+            }
+        }
+        // this wave's tokens of the tile: values into LDS, where those that are not there, and in the tree what is not finite,
+        // become 0 (a weight of 0 would not keep them out of the product)
+        unsigned long long live = 0, bad = 0;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const unsigned long long here = __ballot(page[t] >= 0) & 0xFFFF;
+            live |= here << (load0 + t * 16);
+            if (here != 0xFFFF) {
+#pragma unroll
+                for (int k = 0; k < KS; ++k)
+#pragma unroll
+                    for (int f = 0; f < FC; ++f)
+                        if (page[t] < 0) vr[t][k][f] = make_uint4(0, 0, 0, 0);
+            }
+            if (in_tree) {
+                bool found = false;
+#pragma unroll
+                for (int k = 0; k < KS; ++k)
+#pragma unroll
+                    for (int f = 0; f < FC; ++f) found |= make_finite<FMT>(vr[t][k][f]);
+                unsigned long long who = __ballot(found);
+                who = (who | (who >> 16) | (who >> 32) | (who >> 48)) & 0xFFFF;
+                bad |= who << (load0 + t * 16);
+            }
+#pragma unroll
+            for (int k = 0; k < KS; ++k)
+#pragma unroll
+                for (int f = 0; f < FC; ++f) {
+                    const int token = load0 + t * 16 + c, chunk = (k * 4 + g) * FC + f;
+                    *reinterpret_cast<uint4 *>(vb + A::value_at(token, chunk)) = vr[t][k][f];
+                    if constexpr (ROWS) *reinterpret_cast<uint4 *>(kb + A::key_at(token, chunk)) = kr[t][k][f];
+                }
+        }
+        if constexpr (ROWS) {
+            if (lane == 0) {
+                s_bad[buf][wave] = bad;
+                s_live[buf][wave] = live;
+            }
+            __syncthreads();
+            live = bad = 0;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                live |= s_live[buf][w];
+                bad |= s_bad[buf][w];
+            }
+        }
+        // the next tile's values, and in this form its keys, are asked for now
+        int64_t at[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            page[t] = page_next[t];
+            at[t] = offset_of(u + step, t, page[t]);
+            page_next[t] = page_of(u + 2 * step, t);
+            load(p.v_pages, vr[t], at[t]);
+            if constexpr (ROWS) load(p.k_pages, kr[t], at[t]);
+        }
+        // S^T
+        f32x4 s[CT][QT];
+#pragma unroll
+        for (int t = 0; t < CT; ++t) {
+#pragma unroll
+            for (int j = 0; j < QT; ++j) s[t][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+                Frag<FMT> kf;
+#pragma unroll
+                for (int f = 0; f < FC; ++f) {
+                    if constexpr (ROWS) kf.c[f] = *reinterpret_cast<const uint4 *>(kb + A::key_at(t * 16 + c, (k * 4 + g) * FC + f));
+                    else kf.c[f] = kr[t][k][f];
+                }
+#pragma unroll
+                for (int j = 0; j < QT; ++j) s[t][j] = mfma32<FMT>(kf, q[j][k], s[t][j]);
+            }
+        }
+        if constexpr (!ROWS) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t) load(p.k_pages, kr[t], at[t]);
+        }
+        // softmax, one row a lane
+        constexpr unsigned long long kAll = TT == 64 ? ~0ull : (1ull << (TT & 63)) - 1;
+#pragma unroll
+        for (int j = 0; j < QT; ++j) {
+            const unsigned long long sees = seen[j] & live;
+            if (__any((sees & kAll) != kAll)) {
+#pragma unroll
+                for (int t = 0; t < CT; ++t) {
+                    const uint32_t four = (uint32_t)(sees >> (t * 16 + g * 4));
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (!((four >> i) & 1)) s[t][j][i] = -INFINITY;
+                }
+            }
+            float top = s[0][j][0];
+#pragma unroll
+            for (int t = 0; t < CT; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) top = fmaxf(top, s[t][j][i]);
+            top = max_over_groups(top) * sl2;
+            if (__any(top > m[j])) {                   // (a maximum stays as it is in most tiles)
+                const float m1 = fmaxf(m[j], top);
+                const float keep = m1 == m[j] ? 1.0f : __builtin_amdgcn_exp2f(m[j] - m1);
+                m[j] = m1;
+                l[j] *= keep;
+#pragma unroll
+                for (int d = 0; d < DT; ++d) o[j][d] *= keep;
+            }
+            const float base = m[j] == -INFINITY ? 0.0f : m[j];
+            float sum = 0.0f;
+#pragma unroll
+            for (int t = 0; t < CT; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    s[t][j][i] = __builtin_amdgcn_exp2f(fmaf(s[t][j][i], sl2, -base));
+                    sum += s[t][j][i];
+                }
+            l[j] += sum;
+        }
+        // O^T += V^T P^T
+        if constexpr (FMT == 0) {
+#pragma unroll
+            for (int t = 0; t < CT; ++t)
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float v = *reinterpret_cast<const float *>(vb + A::value_at(t * 16 + 4 * g + i, d * 4 + (c >> 2)) + (c & 3) * 4);
+#pragma unroll
+                        for (int j = 0; j < QT; ++j) o[j][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, s[t][j][i], o[j][d], 0, 0, 0);
+                    }
+        } else {
+            typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+#pragma unroll
+            for (int t = 0; t < CT; t += 2) {
+                // weights in 16 bits, as the matrix units take them: each is off by half a step of itself, either way
+                Frag<FMT> w[QT];
+#pragma unroll
+                for (int j = 0; j < QT; ++j)
+                    w[j].c[0] = make_uint4(pack2<FMT>(s[t][j][0], s[t][j][1]), pack2<FMT>(s[t][j][2], s[t][j][3]),
+                                           pack2<FMT>(s[t + 1][j][0], s[t + 1][j][1]), pack2<FMT>(s[t + 1][j][2], s[t + 1][j][3]));
+#pragma unroll
+                for (int d = 0; d < DT; ++d) {
+                    // lane (g, i) of 16 points at elements 4 (i % 4) .. of token 4g + i / 4 and receives element i of tokens 4g .. 4g+3
+                    struct { i16x4 lo, hi; } v;
+                    const int token = 4 * g + (c >> 2), in = (c & 3) * 8;
+                    v.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(vb + A::value_at(t * 16 + token, d * 2 + (in >> 4)) + (in & 15)));
+                    v.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(vb + A::value_at(t * 16 + 16 + token, d * 2 + (in >> 4)) + (in & 15)));
+                    Frag<FMT> vf;
+                    vf.c[0] = __builtin_bit_cast(uint4, v);
+#pragma unroll
+                    for (int j = 0; j < QT; ++j) o[j][d] = mfma32<FMT>(vf, w[j], o[j][d]);
+                }
+            }
+        }
+        // values that are not finite: for the rows that see them, one at a time
+        while (bad) {
+            const int t = __ffsll(bad) - 1;
+            bad &= bad - 1;
+            const int64_t where = token_offset(p.cache, b, (int64_t)span.prefix + j0 + t);
+            const E *src = reinterpret_cast<const E *>(p.v_pages) + (where < 0 ? 0 : where) + head_at;
+#pragma unroll
+            for (int j = 0; j < QT; ++j) {
+                float w = 0.0f;
+#pragma unroll
+                for (int x = 0; x < CT; ++x)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float y = __shfl(s[x][j][i], ((t & 15) >> 2) * 16 + c);
+                        if (t == x * 16 + ((t & 15) & ~3) + i) w = y;
+                    }
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int e = d * 16 + g * 4 + i;
+                        const float v = (float)src[e < p.D ? e : 0];
+                        if (w != 0.0f && !(fabsf(v) < INFINITY)) o[j][d][i] += w * v;
+                    }
+            }
+        }
+        if constexpr (ROWS) {
+            if (A::BUFS == 1) __syncthreads();
+            else buf ^= 1;
+        }
+    }
+
+    // results: [rows, D] of the output, or this split's part
+    const size_t part = (((size_t)b * p.heads + head) * p.splits + split) * rows;
+    auto put_row = [&](int r, float mm, float ll) {    // statistics of a row
+        if (p.splits > 1) {
+            p.part_ml[(part + r) * 2] = mm;
+            p.part_ml[(part + r) * 2 + 1] = ll;
+        } else if (p.lse) {
+            p.lse[((int64_t)b * p.n + r / G) * p.q_heads + head * G + r % G] = ll != 0.0f ? (mm + __builtin_amdgcn_logf(ll)) * kLn2f : -INFINITY;
+        }
+    };
+    auto put = [&](int r, int d, float ll, f32x4 v) {  // four elements of a row
+        if (p.splits > 1) {
+            *reinterpret_cast<f32x4 *>(p.part_o + (part + r) * p.D + d) = v;
+            return;
+        }
+        const float f = ll != 0.0f ? 1.0f / ll : 0.0f; // (a sum that is not a number is not nothing)
+        E *to = reinterpret_cast<E *>(p.out.data) + ((int64_t)b * p.out.sent + (int64_t)(r / G) * p.out.token + (int64_t)(head * G + r % G) * p.out.head + d);
+        v *= f;
+        if constexpr (FMT == 0) *reinterpret_cast<f32x4 *>(to) = v;
+        else *reinterpret_cast<uint2 *>(to) = make_uint2(pack2<FMT>(v[0], v[1]), pack2<FMT>(v[2], v[3]));
+    };
+#pragma unroll
+    for (int j = 0; j < QT; ++j) l[j] = sum_over_groups(l[j]);
+    if constexpr (ROWS) {
+#pragma unroll
+        for (int j = 0; j < QT; ++j) {
+            const int r = row0 + j * 16 + c;
+            if (r >= rows) continue;
+            if (g == 0) put_row(r, m[j], l[j]);
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+                if (d * 16 + g * 4 < p.D) put(r, d * 16 + g * 4, l[j], o[j][d]);
+        }
+    } else {
+        // the four waves' parts: each on the common maximum, then added up from LDS
+        if (g == 0)
+#pragma unroll
+            for (int j = 0; j < QT; ++j) {
+                s_ml[wave][j * 16 + c][0] = m[j];
+                s_ml[wave][j * 16 + c][1] = l[j];
+            }
+        __syncthreads();                               // (and nobody reads values any more)
+        float top[QT], sum[QT], f[QT];
+#pragma unroll
+        for (int j = 0; j < QT; ++j) {
+            top[j] = -INFINITY;
+            sum[j] = 0.0f;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) top[j] = fmaxf(top[j], s_ml[w][j * 16 + c][0]);
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const float mw = s_ml[w][j * 16 + c][0], lw = s_ml[w][j * 16 + c][1];
+                sum[j] += mw == -INFINITY ? lw : lw * __builtin_amdgcn_exp2f(mw - top[j]);
+            }
+            f[j] = m[j] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[j] - top[j]);
+            const int r = row0 + j * 16 + c;
+            if (wave == 0 && g == 0 && r < rows) put_row(r, top[j], sum[j]);
+        }
+        f32x4 *const s_o = reinterpret_cast<f32x4 *>(s_mem);       // [wave][j][d of this round][lane]
+        constexpr int DR = DT / 4;
+#pragma unroll
+        for (int round = 0; round < 4; ++round) {
+            if (round) __syncthreads();
+#pragma unroll
+            for (int j = 0; j < QT; ++j)
+#pragma unroll
+                for (int d = 0; d < DR; ++d) s_o[((wave * QT + j) * DR + d) * 64 + lane] = o[j][round * DR + d] * f[j];
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < QT; ++j)
+#pragma unroll
+                for (int d = 0; d < DR; ++d) {
+                    if ((j * DR + d) % 4 != wave) continue;
+                    f32x4 v = s_o[(j * DR + d) * 64 + lane];
+#pragma unroll
+                    for (int w = 1; w < 4; ++w) v += s_o[((w * QT + j) * DR + d) * 64 + lane];
+                    const int r = row0 + j * 16 + c, e = (round * DR + d) * 16 + g * 4;
+                    if (r < rows && e < p.D) put(r, e, sum[j], v);
+                }
+        }
+    }
 }
+
+// Joins the splits of a row: one wave a row, four elements a lane.
+template <int FMT>
+__global__ __launch_bounds__(256) void dba_attend_join_kernel(AttendParams p, int tile)
+{
+    typedef typename Elem<FMT>::type E;
+    const int lane = (int)threadIdx.x & 63, b = (int)blockIdx.z, head = (int)blockIdx.y;
+    const int G = p.q_heads / p.heads, rows = p.n * G, r = (int)blockIdx.x * 4 + ((int)threadIdx.x >> 6);
+    if (r >= rows) return;
+    int tree_all;
+    const Span span = span_of_rows(p, b, r / p.tile_rows, G, tree_all);
+    const int tree = span.end - span.prefix;
+    const int tiles = (span.prefix + tile - 1) / tile + (tree + tile - 1) / tile;
+    const int live = max(1, min(p.splits, (tiles + p.chunk - 1) / p.chunk));
+    const size_t part = ((size_t)b * p.heads + head) * p.splits * rows + r;
+    float top = -INFINITY;
+    for (int s = 0; s < live; ++s) top = fmaxf(top, p.part_ml[(part + (size_t)s * rows) * 2]);
+    float sum = 0.0f;
+    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+    const int d = lane * 4;
+    for (int s = 0; s < live; ++s) {
+        const size_t at = part + (size_t)s * rows;
+        const float ms = p.part_ml[at * 2], ls = p.part_ml[at * 2 + 1];
+        if (ls == 0.0f) continue;
+        const float f = ms == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ms - top);
+        sum += ls * f;
+        if (d < p.D) v += *reinterpret_cast<const f32x4 *>(p.part_o + at * p.D + d) * f;
+    }
+    const int64_t row = ((int64_t)b * p.n + r / G) * p.q_heads + head * G + r % G;
+    if (lane == 0 && p.lse) p.lse[row] = sum != 0.0f ? (top + __builtin_amdgcn_logf(sum)) * kLn2f : -INFINITY;
+    if (d < p.D) {
+        v *= sum != 0.0f ? 1.0f / sum : 0.0f;
+        E *to = reinterpret_cast<E *>(p.out.data) + ((int64_t)b * p.out.sent + (int64_t)(r / G) * p.out.token + (int64_t)(head * G + r % G) * p.out.head + d);
+        if constexpr (FMT == 0) *reinterpret_cast<f32x4 *>(to) = v;
+        else *reinterpret_cast<uint2 *>(to) = make_uint2(pack2<FMT>(v[0], v[1]), pack2<FMT>(v[2], v[3]));
+    }
+}
+
+// How a call is laid out: which kernel, how many workgroups along the rows and the token axis.
+struct AttendPlan {
+    int DP, QT;
+    bool shared;                       // the waves have rows of their own (ROWS)
+    int tile, tile_rows, row_tiles, splits, chunk;
+};
+
+template <int FMT> hipError_t attend_launch(const AttendParams &p, const AttendPlan &plan, int B, hipStream_t stream);
 
 }  // namespace dba

@@ -1,0 +1,46 @@
+// Launches of the attention kernels of one format; each format is a source file of its own, which compile side by side.
+#pragma once
+#include "tree_attend.hpp"
+
+namespace dba {
+
+template <int FMT, int DP, int QT, bool ROWS>
+hipError_t attend_one(const AttendParams &p, int B, hipStream_t stream)
+{
+    constexpr int lds = AttendShape<FMT, DP, QT, ROWS>::LDS;
+    static_assert(lds + 4 * 16 * QT * 8 + 256 <= 160 * 1024, "LDS of a compute unit");
+    if constexpr (lds > 65536) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&dba_attend_kernel<FMT, DP, QT, ROWS>),
+                                                 hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        if (e != hipSuccess) return e;
+    }
+    dba_attend_kernel<FMT, DP, QT, ROWS><<<dim3((unsigned)(p.row_tiles * p.splits), (unsigned)p.heads, (unsigned)B), 256, lds, stream>>>(p);
+    return hipGetLastError();
+}
+
+template <int FMT, int DP>
+hipError_t attend_rows(const AttendParams &p, const AttendPlan &plan, int B, hipStream_t stream)
+{
+    if (plan.shared) {
+        if constexpr (DP <= 128)
+            if (plan.QT == 4) return attend_one<FMT, DP, 4, true>(p, B, stream);
+        return attend_one<FMT, DP, 2, true>(p, B, stream);
+    }
+    if constexpr (DP <= 128)
+        if (plan.QT == 4) return attend_one<FMT, DP, 4, false>(p, B, stream);
+    return plan.QT == 2 ? attend_one<FMT, DP, 2, false>(p, B, stream) : attend_one<FMT, DP, 1, false>(p, B, stream);
+}
+
+template <int FMT>
+hipError_t attend_launch(const AttendParams &p, const AttendPlan &plan, int B, hipStream_t stream)
+{
+    hipError_t e = plan.DP == 64 ? attend_rows<FMT, 64>(p, plan, B, stream)
+                 : plan.DP == 128 ? attend_rows<FMT, 128>(p, plan, B, stream) : attend_rows<FMT, 256>(p, plan, B, stream);
+    if (e == hipSuccess && p.splits > 1) {
+        dba_attend_join_kernel<FMT><<<dim3((unsigned)((p.n * (p.q_heads / p.heads) + 3) / 4), (unsigned)p.heads, (unsigned)B), 256, 0, stream>>>(p, plan.tile);
+        e = hipGetLastError();
+    }
+    return e;
+}
+
+}  // namespace dba
