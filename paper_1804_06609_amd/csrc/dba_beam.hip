@@ -113,12 +113,13 @@ AttendPlan attend_plan(int B, int n, int q_heads, const dba_cache &c, int max_le
     AttendPlan a;
     const int rows = n * (q_heads / c.heads);
     a.DP = c.head_dim <= 64 ? 64 : c.head_dim <= 128 ? 128 : 256;
-    const int widest = a.DP <= 128 ? 4 : 2;            // 16-row tiles a wave has registers for
+    const bool f32 = c.format == DBA_LOGP_F32;
+    const int widest = a.DP == 64 ? kAttendWidest<1, 64> : a.DP == 256 ? kAttendWidest<1, 256> : f32 ? kAttendWidest<0, 128> : kAttendWidest<1, 128>;
     a.shared = rows > 16 * widest;
-    a.QT = a.shared ? (rows > 128 ? widest : 2) : rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+    a.QT = a.shared ? (a.DP <= 128 ? 2 : 1) : rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
     a.tile_rows = (a.shared ? 64 : 16) * a.QT;
     a.row_tiles = (rows + a.tile_rows - 1) / a.tile_rows;
-    a.tile = a.shared ? 64 : c.format == DBA_LOGP_F32 ? 16 : 32;
+    a.tile = a.shared ? 64 : f32 ? 16 : 32;
     const int tiles = (max_len + a.tile - 1) / a.tile + 1;         // (the prefix and the tree each end in a tile of their own)
     const int64_t groups = (int64_t)B * c.heads * a.row_tiles;
     const int64_t want = std::max<int64_t>(1, (1024 + groups - 1) / groups);

@@ -44,6 +44,7 @@ __device__ __forceinline__ Span span_of_rows(const AttendParams &p, int b, int r
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.44269504088896340736f;
@@ -52,7 +53,7 @@ constexpr float kLn2f = 0.69314718055994530942f;
 // Eight elements of a row along the contraction: 16 bytes, or 32 in fp32.
 template <int FMT> struct Frag {
     static constexpr int C = FMT == 0 ? 2 : 1;
-    uint4 c[C];
+    u32x4 c[C];
 };
 
 // c += a b^T of 16 rows each over 32 elements; lane (g, i) gives elements 8g .. 8g+7 of row i of a and of b.  In fp32 the products come four
@@ -61,9 +62,9 @@ template <int FMT>
 __device__ __forceinline__ f32x4 mfma32(const Frag<FMT> &a, const Frag<FMT> &b, f32x4 c)
 {
     if constexpr (FMT == 0) {
-        const float *x = reinterpret_cast<const float *>(&a), *y = reinterpret_cast<const float *>(&b);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[j], y[j], c, 0, 0, 0);
+        for (int j = 0; j < 8; ++j)
+            c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.c[j / 4][j % 4]), __uint_as_float(b.c[j / 4][j % 4]), c, 0, 0, 0);
         return c;
     } else if constexpr (FMT == 1) {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a.c[0]), __builtin_bit_cast(f16x8, b.c[0]), c, 0, 0, 0);
@@ -86,22 +87,26 @@ __device__ __forceinline__ uint32_t pack2(float a, float b)
     }
 }
 
-// Which of a chunk's elements are not finite are made 0; true if there were any.
+// Elements that are not finite are made 0.
 template <int FMT>
-__device__ __forceinline__ bool make_finite(uint4 &c)
+__device__ __forceinline__ uint32_t finite_of(uint32_t w)
 {
-    uint32_t *w = reinterpret_cast<uint32_t *>(&c);
-    bool found = false;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if constexpr (FMT == 0) {
-            if ((w[i] & 0x7F800000u) == 0x7F800000u) w[i] = 0, found = true;
-        } else {
-            constexpr uint32_t E = FMT == 1 ? 0x7C00u : 0x7F80u;
-            if ((w[i] & E) == E) w[i] &= 0xFFFF0000u, found = true;
-            if ((w[i] & (E << 16)) == (E << 16)) w[i] &= 0xFFFFu, found = true;
-        }
+    if constexpr (FMT == 0) {
+        return (w & 0x7F800000u) == 0x7F800000u ? 0u : w;
+    } else {
+        constexpr uint32_t E = FMT == 1 ? 0x7C00u : 0x7F80u;
+        w = (w & E) == E ? w & 0xFFFF0000u : w;
+        return (w & (E << 16)) == (E << 16) ? w & 0xFFFFu : w;
     }
+}
+
+// The same of a chunk; true if there were any.
+template <int FMT>
+__device__ __forceinline__ bool make_finite(u32x4 &c)
+{
+    const u32x4 f = u32x4{finite_of<FMT>(c.x), finite_of<FMT>(c.y), finite_of<FMT>(c.z), finite_of<FMT>(c.w)};
+    const bool found = f.x != c.x || f.y != c.y || f.z != c.z || f.w != c.w;
+    c = f;
     return found;
 }
 
@@ -157,9 +162,10 @@ __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) vo
     typedef AttendShape<FMT, DP, QT, ROWS> A;
     typedef typename Elem<FMT>::type E;
     constexpr int KS = A::KS, DT = A::DT, NT = A::NT, CT = A::CT, TT = A::TT, FC = Frag<FMT>::C, NE = 16 / A::ES;
-    extern __shared__ unsigned char s_mem[];
+    extern __shared__ __align__(16) unsigned char s_mem[];
     __shared__ float s_ml[4][16 * QT][2];
-    __shared__ unsigned long long s_bad[2][4], s_live[2][4];
+    __shared__ unsigned long long s_live[2][4];
+    __shared__ int s_bad;
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int c = lane & 15, g = lane >> 4;
     const int row_tile = (int)blockIdx.x % p.row_tiles, split = (int)blockIdx.x / p.row_tiles;
@@ -178,7 +184,7 @@ __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) vo
     Frag<FMT> q[QT][KS];
     const unsigned long long *mask_row[QT];
     int chain[QT];                                     // the last tree token a row of a chain sees
-    const float qsign = p.scale < 0.0f ? -1.0f : 1.0f;
+    const uint32_t sign = p.scale < 0.0f ? (FMT == 0 ? 0x80000000u : 0x80008000u) : 0u;    // a negative scale turns the queries round
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
         const int r = row0 + t * 16 + c, node = min(r, rows - 1) / G, h = head * G + min(r, rows - 1) % G;
@@ -190,14 +196,9 @@ __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) vo
 #pragma unroll
             for (int f = 0; f < FC; ++f) {
                 const int d = k * 32 + g * 8 + f * NE;
-                uint4 v = make_uint4(0, 0, 0, 0);
-                if (r < rows && d < p.D && p.scale != 0.0f) v = *reinterpret_cast<const uint4 *>(src + d);
-                if (qsign < 0.0f) {
-                    uint32_t *w = reinterpret_cast<uint32_t *>(&v);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) w[i] ^= FMT == 0 ? 0x80000000u : 0x80008000u;
-                }
-                q[t][k].c[f] = v;
+                u32x4 v = u32x4{0, 0, 0, 0};
+                if (r < rows && d < p.D && p.scale != 0.0f) v = *reinterpret_cast<const u32x4 *>(src + d);
+                q[t][k].c[f] = v ^ sign;
             }
         }
     }
@@ -220,16 +221,18 @@ __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) vo
         const int pos = (u >= prefix_tiles ? span.prefix + (u - prefix_tiles) * TT : u * TT) + load0 + t * 16 + c;
         return (int64_t)page * p.cache.page_stride + (int64_t)(pos & ((1 << p.cache.page_shift) - 1)) * p.cache.token_stride + head_at;
     };
-    uint4 kr[NT][KS][FC], vr[NT][KS][FC];
+    bool bad = false;                                  // this lane has met a value that is not finite
+    if (threadIdx.x == 0) s_bad = 0;
+    u32x4 kr[NT][KS][FC], vr[NT][KS][FC];
     // a chunk behind the head's end is read as its first: the queries have 0 there, and nobody asks for those outputs
-    auto load = [&](const unsigned char *pool, uint4 (&to)[KS][FC], int64_t at) {
+    auto load = [&](const unsigned char *pool, u32x4 (&to)[KS][FC], int64_t at) {
         const E *src = reinterpret_cast<const E *>(pool) + at;
 #pragma unroll
         for (int k = 0; k < KS; ++k)
 #pragma unroll
             for (int f = 0; f < FC; ++f) {
                 const int d = k * 32 + g * 8 + f * NE;
-                to[k][f] = *reinterpret_cast<const uint4 *>(src + (d < p.D ? d : 0));
+                to[k][f] = *reinterpret_cast<const u32x4 *>(src + (d < p.D ? d : 0));
             }
     };
 
@@ -280,7 +283,7 @@ __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) vo
         }
         // this wave's tokens of the tile: values into LDS, where those that are not there, and in the tree what is not finite,
         // become 0 (a weight of 0 would not keep them out of the product)
-        unsigned long long live = 0, bad = 0;
+        unsigned long long live = 0;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             const unsigned long long here = __ballot(page[t] >= 0) & 0xFFFF;
@@ -290,39 +293,27 @@ __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) vo
                 for (int k = 0; k < KS; ++k)
 #pragma unroll
                     for (int f = 0; f < FC; ++f)
-                        if (page[t] < 0) vr[t][k][f] = make_uint4(0, 0, 0, 0);
+                        if (page[t] < 0) vr[t][k][f] = u32x4{0, 0, 0, 0};
             }
             if (in_tree) {
-                bool found = false;
 #pragma unroll
                 for (int k = 0; k < KS; ++k)
 #pragma unroll
-                    for (int f = 0; f < FC; ++f) found |= make_finite<FMT>(vr[t][k][f]);
-                unsigned long long who = __ballot(found);
-                who = (who | (who >> 16) | (who >> 32) | (who >> 48)) & 0xFFFF;
-                bad |= who << (load0 + t * 16);
+                    for (int f = 0; f < FC; ++f) bad |= make_finite<FMT>(vr[t][k][f]);
             }
 #pragma unroll
             for (int k = 0; k < KS; ++k)
 #pragma unroll
                 for (int f = 0; f < FC; ++f) {
                     const int token = load0 + t * 16 + c, chunk = (k * 4 + g) * FC + f;
-                    *reinterpret_cast<uint4 *>(vb + A::value_at(token, chunk)) = vr[t][k][f];
-                    if constexpr (ROWS) *reinterpret_cast<uint4 *>(kb + A::key_at(token, chunk)) = kr[t][k][f];
+                    *reinterpret_cast<u32x4 *>(vb + A::value_at(token, chunk)) = vr[t][k][f];
+                    if constexpr (ROWS) *reinterpret_cast<u32x4 *>(kb + A::key_at(token, chunk)) = kr[t][k][f];
                 }
         }
         if constexpr (ROWS) {
-            if (lane == 0) {
-                s_bad[buf][wave] = bad;
-                s_live[buf][wave] = live;
-            }
+            if (lane == 0) s_live[buf][wave] = live;
             __syncthreads();
-            live = bad = 0;
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                live |= s_live[buf][w];
-                bad |= s_bad[buf][w];
-            }
+            live = s_live[buf][0] | s_live[buf][1] | s_live[buf][2] | s_live[buf][3];
         }
         // the next tile's values, and in this form its keys, are asked for now
         int64_t at[NT];
@@ -345,7 +336,7 @@ __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) vo
                 Frag<FMT> kf;
 #pragma unroll
                 for (int f = 0; f < FC; ++f) {
-                    if constexpr (ROWS) kf.c[f] = *reinterpret_cast<const uint4 *>(kb + A::key_at(t * 16 + c, (k * 4 + g) * FC + f));
+                    if constexpr (ROWS) kf.c[f] = *reinterpret_cast<const u32x4 *>(kb + A::key_at(t * 16 + c, (k * 4 + g) * FC + f));
                     else kf.c[f] = kr[t][k][f];
                 }
 #pragma unroll
@@ -415,8 +406,8 @@ __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) vo
                 Frag<FMT> w[QT];
 #pragma unroll
                 for (int j = 0; j < QT; ++j)
-                    w[j].c[0] = make_uint4(pack2<FMT>(s[t][j][0], s[t][j][1]), pack2<FMT>(s[t][j][2], s[t][j][3]),
-                                           pack2<FMT>(s[t + 1][j][0], s[t + 1][j][1]), pack2<FMT>(s[t + 1][j][2], s[t + 1][j][3]));
+                    w[j].c[0] = u32x4{pack2<FMT>(s[t][j][0], s[t][j][1]), pack2<FMT>(s[t][j][2], s[t][j][3]),
+                                      pack2<FMT>(s[t + 1][j][0], s[t + 1][j][1]), pack2<FMT>(s[t + 1][j][2], s[t + 1][j][3])};
 #pragma unroll
                 for (int d = 0; d < DT; ++d) {
                     // lane (g, i) of 16 points at elements 4 (i % 4) .. of token 4g + i / 4 and receives element i of tokens 4g .. 4g+3
@@ -425,36 +416,10 @@ __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) vo
                     v.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(vb + A::value_at(t * 16 + token, d * 2 + (in >> 4)) + (in & 15)));
                     v.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(vb + A::value_at(t * 16 + 16 + token, d * 2 + (in >> 4)) + (in & 15)));
                     Frag<FMT> vf;
-                    vf.c[0] = __builtin_bit_cast(uint4, v);
+                    vf.c[0] = __builtin_bit_cast(u32x4, v);
 #pragma unroll
                     for (int j = 0; j < QT; ++j) o[j][d] = mfma32<FMT>(vf, w[j], o[j][d]);
                 }
-            }
-        }
-        // values that are not finite: for the rows that see them, one at a time
-        while (bad) {
-            const int t = __ffsll(bad) - 1;
-            bad &= bad - 1;
-            const int64_t where = token_offset(p.cache, b, (int64_t)span.prefix + j0 + t);
-            const E *src = reinterpret_cast<const E *>(p.v_pages) + (where < 0 ? 0 : where) + head_at;
-#pragma unroll
-            for (int j = 0; j < QT; ++j) {
-                float w = 0.0f;
-#pragma unroll
-                for (int x = 0; x < CT; ++x)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float y = __shfl(s[x][j][i], ((t & 15) >> 2) * 16 + c);
-                        if (t == x * 16 + ((t & 15) & ~3) + i) w = y;
-                    }
-#pragma unroll
-                for (int d = 0; d < DT; ++d)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int e = d * 16 + g * 4 + i;
-                        const float v = (float)src[e < p.D ? e : 0];
-                        if (w != 0.0f && !(fabsf(v) < INFINITY)) o[j][d][i] += w * v;
-                    }
             }
         }
         if constexpr (ROWS) {
@@ -544,6 +509,30 @@ __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) vo
                 }
         }
     }
+
+    // Values of the tree that are not finite have been left out.  Whatever its weight, such a value makes an element of the rows that
+    // see it an infinity or a NaN: those elements are written once more.  (Slow, and only where there is one.)
+    if (__any(bad) && lane == 0) s_bad = 1;
+    __syncthreads();
+    if (!s_bad) return;
+    const int t0 = max(0, u0 - prefix_tiles) * TT, t1 = min(tree, (u1 - prefix_tiles) * TT);
+    const int r0 = row_tile * p.tile_rows, r1 = min(rows, r0 + p.tile_rows);
+    for (int x = (int)threadIdx.x; x < (r1 - r0) * p.D; x += 256) {
+        const int r = r0 + x / p.D, e = x % p.D, node = r / G;
+        float v = 0.0f;
+        for (int t = t0; t < t1; ++t) {
+            if (p.mask ? (t >> 6) >= p.mask_words || !((p.mask[((int64_t)b * p.n + node) * p.mask_words + (t >> 6)] >> (t & 63)) & 1)
+                       : t > tree_all - p.n + node)
+                continue;
+            const int64_t at = token_offset(p.cache, b, (int64_t)span.prefix + t);
+            if (at < 0) continue;
+            const float y = (float)reinterpret_cast<const E *>(p.v_pages)[at + head_at + e];
+            if (!(fabsf(y) < INFINITY)) v += y;
+        }
+        if (v == 0.0f) continue;
+        if (p.splits > 1) p.part_o[(part + r) * p.D + e] = v;
+        else reinterpret_cast<E *>(p.out.data)[(int64_t)b * p.out.sent + (int64_t)node * p.out.token + (int64_t)(head * G + r % G) * p.out.head + e] = (E)v;
+    }
 }
 
 // Joins the splits of a row: one wave a row, four elements a lane.
@@ -582,6 +571,9 @@ __global__ __launch_bounds__(256) void dba_attend_join_kernel(AttendParams p, in
         else *reinterpret_cast<uint2 *>(to) = make_uint2(pack2<FMT>(v[0], v[1]), pack2<FMT>(v[2], v[3]));
     }
 }
+
+// The most 16-row tiles a wave has registers for where it holds all rows of a head.
+template <int FMT, int DP> constexpr int kAttendWidest = DP == 64 ? 4 : DP == 128 ? (FMT == 0 ? 2 : 4) : 1;
 
 // How a call is laid out: which kernel, how many workgroups along the rows and the token axis.
 struct AttendPlan {

@@ -21,14 +21,12 @@ hipError_t attend_one(const AttendParams &p, int B, hipStream_t stream)
 template <int FMT, int DP>
 hipError_t attend_rows(const AttendParams &p, const AttendPlan &plan, int B, hipStream_t stream)
 {
-    if (plan.shared) {
-        if constexpr (DP <= 128)
-            if (plan.QT == 4) return attend_one<FMT, DP, 4, true>(p, B, stream);
-        return attend_one<FMT, DP, 2, true>(p, B, stream);
-    }
-    if constexpr (DP <= 128)
+    if (plan.shared) return attend_one<FMT, DP, (DP <= 128 ? 2 : 1), true>(p, B, stream);
+    if constexpr (kAttendWidest<FMT, DP> >= 4)
         if (plan.QT == 4) return attend_one<FMT, DP, 4, false>(p, B, stream);
-    return plan.QT == 2 ? attend_one<FMT, DP, 2, false>(p, B, stream) : attend_one<FMT, DP, 1, false>(p, B, stream);
+    if constexpr (kAttendWidest<FMT, DP> >= 2)
+        if (plan.QT == 2) return attend_one<FMT, DP, 2, false>(p, B, stream);
+    return attend_one<FMT, DP, 1, false>(p, B, stream);
 }
 
 template <int FMT>
