@@ -830,19 +830,6 @@ HostBlocks<PinnedMemory> &host_blocks()
     return *blocks;
 }
 
-// A launch that tells how it went, so that of one that failed it is known that no kernel of it is under way: hipGetLastError, behind the <<< >>> form,
-// may tell of an earlier call on this thread, of whomever, and takes that error from its owner.  (Nor does this one pass its grid through the runtime first: a step's call takes 2.85 instead of 3.05
-// us with one launch and 5.27 instead of 5.65 with two, which is the time of a step where short ones of several decodes alternate.)
-template <typename... P, typename... A>
-hipError_t launch(void (*kernel)(P...), dim3 grid, dim3 block, size_t lds, hipStream_t stream, const A &...a)
-{
-    auto with = [&](P... arg) {
-        void *args[] = {&arg...};
-        return hipLaunchKernel(reinterpret_cast<const void *>(kernel), grid, block, args, lds, stream);
-    };
-    return with(a...);
-}
-
 }  // namespace
 
 struct dba_ctx {

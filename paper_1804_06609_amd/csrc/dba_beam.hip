@@ -24,9 +24,8 @@ namespace {
 constexpr size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 constexpr int kMostRows = 1 << 22;          // tokens, or heads of tokens, of one sentence in a call
 
-int launched(const char *who)
+int launched(const char *who, hipError_t e)
 {
-    const hipError_t e = hipGetLastError();
     return e == hipSuccess ? DBA_OK : set_error(DBA_EHIP, "%s: launch failed: %s", who, hipGetErrorString(e));
 }
 
@@ -146,9 +145,12 @@ size_t attend_rows_of(int B, int n, int q_heads, const AttendPlan &a) { return (
 
 // the two launches of a selection
 template <int FMT>
-void select_launch(const SelectParams &p, int B, const void *logits, hipStream_t stream)
+hipError_t select_launch(const SelectParams &p, int B, const void *logits, hipStream_t stream)
 {
-    dba_select_part_kernel<FMT><<<dim3((unsigned)(p.nparts * p.k_in), (unsigned)B), kSelectThreads, 0, stream>>>(logits, p);
+    hipError_t e = launch(dba_select_part_kernel<FMT>, dim3((unsigned)(p.nparts * p.k_in), (unsigned)B), dim3(kSelectThreads), 0, stream, logits, p);
+    if (e != hipSuccess) return e;
+    return p.k_in * p.nparts * p.cap <= 4096 ? launch(dba_select_sentence_kernel<256>, dim3((unsigned)B), dim3(256), 0, stream, p)
+                                             : launch(dba_select_sentence_kernel<1024>, dim3((unsigned)B), dim3(1024), 0, stream, p);
 }
 
 }  // namespace
@@ -201,17 +203,9 @@ DBA_API int dba_beam_select(int B, int k_in, int k_out, int V, int eos_id, int p
     p.eos = eos_id;
     p.pad = pad_id;
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    (void)hipGetLastError();
-    switch (logits_format) {
-        case DBA_LOGP_F32: select_launch<0>(p, B, logits_dev, stream); break;
-        case DBA_LOGP_F16: select_launch<1>(p, B, logits_dev, stream); break;
-        default: select_launch<2>(p, B, logits_dev, stream); break;
-    }
-    const int rc = launched("dba_beam_select");
-    if (rc != DBA_OK) return rc;
-    if (k_in * plan.nparts * plan.cap <= 4096) dba_select_sentence_kernel<256><<<B, 256, 0, stream>>>(p);
-    else dba_select_sentence_kernel<1024><<<B, 1024, 0, stream>>>(p);
-    return launched("dba_beam_select");
+    const hipError_t e = logits_format == DBA_LOGP_F32 ? select_launch<0>(p, B, logits_dev, stream)
+                       : logits_format == DBA_LOGP_F16 ? select_launch<1>(p, B, logits_dev, stream) : select_launch<2>(p, B, logits_dev, stream);
+    return launched("dba_beam_select", e);
 }
 
 DBA_API int dba_beam_reorder(int B, int k, const int32_t *backptr_dev, const dba_state *states_host, int n_states, void *hip_stream)
@@ -255,7 +249,6 @@ DBA_API int dba_beam_reorder(int B, int k, const int32_t *backptr_dev, const dba
             return set_error(DBA_EINVAL, "dba_beam_reorder: a row of state %d has more than 2 GB", i);
     }
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    (void)hipGetLastError();
     ReorderParams p;
     p.back = backptr_dev;
     p.k = k;
@@ -264,14 +257,12 @@ DBA_API int dba_beam_reorder(int B, int k, const int32_t *backptr_dev, const dba
     const auto flush = [&]() -> int {
         if (!p.n_states) return DBA_OK;
         const dim3 grid(blocks, (unsigned)B);
-        if (k <= 4) dba_reorder_kernel<4><<<grid, kReorderThreads, 0, stream>>>(p);
-        else if (k <= 8) dba_reorder_kernel<8><<<grid, kReorderThreads, 0, stream>>>(p);
-        else if (k <= 16) dba_reorder_kernel<16><<<grid, kReorderThreads, 0, stream>>>(p);
-        else if (k <= 32) dba_reorder_kernel<32><<<grid, kReorderThreads, 0, stream>>>(p);
-        else dba_reorder_kernel<64><<<grid, kReorderThreads, 0, stream>>>(p);
+        const auto kernel = k <= 4 ? dba_reorder_kernel<4> : k <= 8 ? dba_reorder_kernel<8> : k <= 16 ? dba_reorder_kernel<16>
+                          : k <= 32 ? dba_reorder_kernel<32> : dba_reorder_kernel<64>;
+        const hipError_t e = launch(kernel, grid, dim3(kReorderThreads), 0, stream, p);
         p.n_states = 0;
         blocks = 0;
-        return launched("dba_beam_reorder");
+        return launched("dba_beam_reorder", e);
     };
     for (int i = 0; i < n_states; ++i) {
         dba_state s = states_host[i];
@@ -350,13 +341,8 @@ DBA_API int dba_cache_append(int B, int n, const dba_cache *cache, const dba_hea
     p.interleaved = interleaved != 0;
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     const dim3 grid((unsigned)n, (unsigned)B);
-    (void)hipGetLastError();
-    switch (cache->format) {
-        case DBA_LOGP_F32: dba_append_kernel<0><<<grid, kAppendThreads, 0, stream>>>(p); break;
-        case DBA_LOGP_F16: dba_append_kernel<1><<<grid, kAppendThreads, 0, stream>>>(p); break;
-        default: dba_append_kernel<2><<<grid, kAppendThreads, 0, stream>>>(p); break;
-    }
-    return launched("dba_cache_append");
+    const auto kernel = cache->format == DBA_LOGP_F32 ? dba_append_kernel<0> : cache->format == DBA_LOGP_F16 ? dba_append_kernel<1> : dba_append_kernel<2>;
+    return launched("dba_cache_append", launch(kernel, grid, dim3(kAppendThreads), 0, stream, p));
 }
 
 DBA_API size_t dba_tree_attend_workspace_bytes(int B, int n, int q_heads, const dba_cache *cache, int max_len)
@@ -409,10 +395,9 @@ DBA_API int dba_tree_attend(int B, int n, int q_heads, const dba_heads *q, const
     p.part_o = static_cast<float *>(workspace_dev);
     p.part_ml = reinterpret_cast<float *>(static_cast<unsigned char *>(workspace_dev) + align256(attend_rows_of(B, n, q_heads, plan) * cache->head_dim * 4));
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    (void)hipGetLastError();
     const hipError_t e = cache->format == DBA_LOGP_F32 ? attend_launch<0>(p, plan, B, stream)
                        : cache->format == DBA_LOGP_F16 ? attend_launch<1>(p, plan, B, stream) : attend_launch<2>(p, plan, B, stream);
-    return e == hipSuccess ? DBA_OK : set_error(DBA_EHIP, "dba_tree_attend: launch failed: %s", hipGetErrorString(e));
+    return launched("dba_tree_attend", e);
 }
 
 }  // extern "C"

@@ -1,5 +1,6 @@
 // Launches of the attention kernels of one format; each format is a source file of its own, which compile side by side.
 #pragma once
+#include "entry.hpp"
 #include "tree_attend.hpp"
 
 namespace dba {
@@ -14,8 +15,7 @@ hipError_t attend_one(const AttendParams &p, int B, hipStream_t stream)
                                                  hipFuncAttributeMaxDynamicSharedMemorySize, lds);
         if (e != hipSuccess) return e;
     }
-    dba_attend_kernel<FMT, DP, QT, ROWS><<<dim3((unsigned)(p.row_tiles * p.splits), (unsigned)p.heads, (unsigned)B), 256, lds, stream>>>(p);
-    return hipGetLastError();
+    return launch(dba_attend_kernel<FMT, DP, QT, ROWS>, dim3((unsigned)(p.row_tiles * p.splits), (unsigned)p.heads, (unsigned)B), dim3(256), lds, stream, p);
 }
 
 template <int FMT, int DP>
@@ -32,13 +32,10 @@ hipError_t attend_rows(const AttendParams &p, const AttendPlan &plan, int B, hip
 template <int FMT>
 hipError_t attend_launch(const AttendParams &p, const AttendPlan &plan, int B, hipStream_t stream)
 {
-    hipError_t e = plan.DP == 64 ? attend_rows<FMT, 64>(p, plan, B, stream)
+    const hipError_t e = plan.DP == 64 ? attend_rows<FMT, 64>(p, plan, B, stream)
                  : plan.DP == 128 ? attend_rows<FMT, 128>(p, plan, B, stream) : attend_rows<FMT, 256>(p, plan, B, stream);
-    if (e == hipSuccess && p.splits > 1) {
-        dba_attend_join_kernel<FMT><<<dim3((unsigned)((p.n * (p.q_heads / p.heads) + 3) / 4), (unsigned)p.heads, (unsigned)B), 256, 0, stream>>>(p, plan.tile);
-        e = hipGetLastError();
-    }
-    return e;
+    if (e != hipSuccess || p.splits == 1) return e;
+    return launch(dba_attend_join_kernel<FMT>, dim3((unsigned)((p.n * (p.q_heads / p.heads) + 3) / 4), (unsigned)p.heads, (unsigned)B), dim3(256), 0, stream, p, plan.tile);
 }
 
 }  // namespace dba
