@@ -9,9 +9,9 @@
 
 namespace dba {
 
-// What a part of a row leaves behind: its greatest logit, the sum of exp(x - top) and how many keys it has handed on.
+// What a part of a row leaves behind: its greatest logit, log sum exp(x - top) and how many keys it has handed on.
 struct SelectPart {
-    double sum;
+    double log_sum;                    // -inf: nothing; not a number: the row offers nothing
     float top;
     int count;
 };
@@ -30,20 +30,25 @@ struct SelectParams {
 
 constexpr int kSelectThreads = 256;    // of the first launch
 constexpr int kSelectChunks = 8;       // 16-byte chunks a thread keeps in registers
-constexpr int kSelectFinal = 512;      // keys the second launch ranks by counting
+constexpr int kSelectFinal = 1024;     // extensions the second launch has room for
+constexpr int kSelectLists = 1024;     // parts with such extensions it has room for
+constexpr double kLn2 = 0.693147180559945309417232121458;
 // log2 e in two parts: a one-part product is off by 1.3e-8 of itself in the same direction for every x, which shows in the sum
 constexpr float kLog2eHi = 1.44269502162933349609375f;
 constexpr float kLog2eLo = (float)(1.442695040888963407359924681 - 1.44269502162933349609375);
 
-// exp(x - top); the difference comes first, so that logits at the type's lowest value do no harm
-__device__ __forceinline__ float exp_below(float x, float top)
+// 2^(x log2 e - m2)
+__device__ __forceinline__ float exp2_above(float x, float m2)
 {
-    const float d = x - top;
-    return __builtin_amdgcn_exp2f(fmaf(d, kLog2eHi, d * kLog2eLo));
+    return __builtin_amdgcn_exp2f(fmaf(x, kLog2eLo, fmaf(x, kLog2eHi, -m2)));
 }
 
 template <int FMT> struct Chunk;       // 16 bytes of logits
 template <> struct Chunk<0> {
+    static __device__ __forceinline__ float most(const uint4 &c)
+    {
+        return fmaxf(fmaxf(__uint_as_float(c.x), __uint_as_float(c.y)), fmaxf(__uint_as_float(c.z), __uint_as_float(c.w)));
+    }
     static constexpr int N = 4;
     typedef float elem_t;
     static __device__ __forceinline__ float get(const uint4 &c, int e) { return __uint_as_float(((const uint32_t *)&c)[e]); }
@@ -51,6 +56,13 @@ template <> struct Chunk<0> {
     static constexpr uint32_t kNone = 0xFF800000u;
 };
 template <> struct Chunk<1> {
+    static __device__ __forceinline__ float most(const uint4 &c)
+    {
+        typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+        const h2 m = __builtin_elementwise_max(__builtin_elementwise_max(__builtin_bit_cast(h2, c.x), __builtin_bit_cast(h2, c.y)),
+                                               __builtin_elementwise_max(__builtin_bit_cast(h2, c.z), __builtin_bit_cast(h2, c.w)));
+        return fmaxf((float)m[0], (float)m[1]);
+    }
     static constexpr int N = 8;
     typedef uint16_t elem_t;
     static __device__ __forceinline__ float get(const uint4 &c, int e)
@@ -63,6 +75,14 @@ template <> struct Chunk<1> {
     static constexpr uint32_t kNone = 0xFC00u;
 };
 template <> struct Chunk<2> {
+    // The greatest pair of halves, read as a float, has the greatest upper half: the lower one only decides between equals.  (An
+    // infinity over a lower half that is not 0 reads as NaN and is passed over: -inf is no extension, +inf shows in the sum.)
+    static __device__ __forceinline__ float most(const uint4 &c)
+    {
+        const float up = fmaxf(fmaxf(__uint_as_float(c.x), __uint_as_float(c.y)), fmaxf(__uint_as_float(c.z), __uint_as_float(c.w)));
+        const float low = fmaxf(fmaxf(__uint_as_float(c.x << 16), __uint_as_float(c.y << 16)), fmaxf(__uint_as_float(c.z << 16), __uint_as_float(c.w << 16)));
+        return fmaxf(__uint_as_float(__float_as_uint(up) & 0xFFFF0000u), low);
+    }
     static constexpr int N = 8;
     typedef uint16_t elem_t;
     static __device__ __forceinline__ float get(const uint4 &c, int e)
@@ -104,7 +124,7 @@ __device__ __forceinline__ int block_sum(int v, int *room)
 // One part of one row.  Bound: HBM (the logits are read once); the exponentials take about a quarter of
 // the VALU's time at that rate.
 template <int FMT>
-__global__ __launch_bounds__(kSelectThreads) void dba_select_part_kernel(const void *logits, SelectParams p)
+__global__ __launch_bounds__(kSelectThreads, 6) void dba_select_part_kernel(const void *logits, SelectParams p)
 {
     typedef Chunk<FMT> C;
     typedef typename C::elem_t elem_t;
@@ -127,7 +147,7 @@ __global__ __launch_bounds__(kSelectThreads) void dba_select_part_kernel(const v
         const bool goes_on = part == 0 && (flags & DBA_FLAG_FINISHED) && !(flags & DBA_FLAG_DEAD) && fabsf(score) < INFINITY;
         if (t == 0) {
             if (goes_on) out_keys[0] = make_key(0.0f, (uint32_t)p.pad);
-            *out = SelectPart{goes_on ? 1.0 : 0.0, 0.0f, goes_on ? 1 : 0};
+            *out = SelectPart{0.0, 0.0f, goes_on ? 1 : 0};
         }
         return;
     }
@@ -135,34 +155,32 @@ __global__ __launch_bounds__(kSelectThreads) void dba_select_part_kernel(const v
     // chunks lie on the 16-byte grid of memory; the first starts `shift` elements before the row
     const int shift = (int)((reinterpret_cast<uintptr_t>(src) & 15) / sizeof(elem_t));
     const int c0 = part * p.part_chunks, c1 = c0 + p.part_chunks;
+    auto chunk_at = [&](int c) {                       // what is not in the row, or in another part, is -inf
+        const int64_t v0 = (int64_t)c * N - shift;
+        if (c < c1 && v0 >= 0 && v0 + N <= p.V) return *reinterpret_cast<const uint4 *>(src + v0);
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = N == 4 ? C::kNone : C::kNone | (C::kNone << 16);
+        if (c < c1) {
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                if (v0 + e >= 0 && v0 + e < p.V) {
+                    const uint32_t x = C::bits(src + v0 + e);
+                    if (N == 4) w[e] = x;
+                    else w[e >> 1] = (e & 1) ? (w[e >> 1] & 0xFFFFu) | (x << 16) : (w[e >> 1] & 0xFFFF0000u) | x;
+                }
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    };
     uint4 raw[R];
 #pragma unroll
+    for (int r = 0; r < R; ++r) raw[r] = chunk_at(c0 + t + r * T);
+    float top = -INFINITY, most_of[R];
+#pragma unroll
     for (int r = 0; r < R; ++r) {
-        const int c = c0 + t + r * T;
-        const int64_t v0 = (int64_t)c * N - shift;
-        if (c < c1 && v0 >= 0 && v0 + N <= p.V) {
-            raw[r] = *reinterpret_cast<const uint4 *>(src + v0);
-        } else {
-            uint32_t w[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = N == 4 ? C::kNone : C::kNone | (C::kNone << 16);
-            if (c < c1) {
-#pragma unroll
-                for (int e = 0; e < N; ++e)
-                    if (v0 + e >= 0 && v0 + e < p.V) {
-                        const uint32_t x = C::bits(src + v0 + e);
-                        if (N == 4) w[e] = x;
-                        else w[e >> 1] = (e & 1) ? (w[e >> 1] & 0xFFFFu) | (x << 16) : (w[e >> 1] & 0xFFFF0000u) | x;
-                    }
-            }
-            raw[r] = make_uint4(w[0], w[1], w[2], w[3]);
-        }
+        most_of[r] = C::most(raw[r]);
+        top = fmaxf(top, most_of[r]);
     }
-    float top = -INFINITY;
-#pragma unroll
-    for (int r = 0; r < R; ++r)
-#pragma unroll
-        for (int e = 0; e < N; ++e) top = fmaxf(top, C::get(raw[r], e));
     s_max[t] = top > -INFINITY ? ord_from_float(top) : 0u;
     if (t == 0) s_count = 0;
     __syncthreads();
@@ -180,20 +198,46 @@ __global__ __launch_bounds__(kSelectThreads) void dba_select_part_kernel(const v
     const uint32_t bar_ord = kth_greatest<T / kWave>(r4, p.k_out, reached);
     const float bar = bar_ord ? float_from_ord(bar_ord) : -INFINITY;
     const float most_x = most ? float_from_ord(most) : 0.0f;
-    // the sum: a few dozen terms a thread in fp32 (each is off by 1e-7 of itself, either way), the threads' in 64 bits
-    float sum = 0.0f;
+    uint32_t hits = 0;
 #pragma unroll
-    for (int r = 0; r < R; ++r)
+    for (int r = 0; r < R; ++r) hits |= (most_of[r] >= bar && most_of[r] > -INFINITY ? 1u : 0u) << r;
+    // The sum: a few dozen terms a thread in fp32 (each is off by 1e-7 of itself, either way), the threads' in 64 bits.  The reference is
+    // the rounded product itself, so that no error of its own comes in; where that would overflow (logits at fp32's lowest value),
+    // two different logits are so far apart that a term is 0 or 1.
+    float sum = 0.0f;
+    const float m2 = most_x * kLog2eHi;
+    const bool huge = !(fabsf(most_x) < 1e37f);
+    if (!huge) {
+        float part_sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int e = 0; e < N; ++e) part_sum[e & 3] += exp2_above(C::get(raw[r], e), m2);
+        sum = (part_sum[0] + part_sum[1]) + (part_sum[2] + part_sum[3]);
+    } else {
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const float x = C::get(raw[r], e);
+                sum += x < most_x ? 0.0f : x == most_x && x < INFINITY ? 1.0f : NAN;
+            }
+    }
+    // the few chunks that reach the bar, from memory once more (registers cannot be indexed)
+    while (hits) {
+        const int r = __ffs(hits) - 1;
+        hits &= hits - 1;
+        const int c = c0 + t + r * T;
+        const uint4 again = chunk_at(c);
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            const float x = C::get(raw[r], e);
-            sum += exp_below(x, most_x);
+            const float x = C::get(again, e);
             if (x >= bar && x > -INFINITY) {
                 const int at = atomicAdd(&s_count, 1);
-                const int c = c0 + t + r * T;
                 if (at < p.cap) s_keys[at] = make_key(x, (uint32_t)(c * N - shift + e));
             }
         }
+    }
     const double total = wave_sum_double((double)sum);
     if (lane_id() == 0) s_sum[t / kWave] = total;
     __syncthreads();
@@ -201,13 +245,16 @@ __global__ __launch_bounds__(kSelectThreads) void dba_select_part_kernel(const v
     if (count > p.cap) {
         // many equal logits, or few threads with any: exactly k_out, by bisection on the keys, which all differ
         auto each = [&](auto f) {
-#pragma unroll
-            for (int r = 0; r < R; ++r)
+#pragma unroll 1
+            for (int r = 0; r < R; ++r) {
+                const int c = c0 + t + r * T;
+                const uint4 again = chunk_at(c);
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
-                    const float x = C::get(raw[r], e);
-                    if (x >= bar && x > -INFINITY) f(make_key(x, (uint32_t)((c0 + t + r * T) * N - shift + e)));
+                    const float x = C::get(again, e);
+                    if (x >= bar && x > -INFINITY) f(make_key(x, (uint32_t)(c * N - shift + e)));
                 }
+            }
         };
         u64 lo = 1, hi = ~0ull;
         while (lo < hi) {
@@ -234,7 +281,8 @@ __global__ __launch_bounds__(kSelectThreads) void dba_select_part_kernel(const v
     if (t == 0) {
         double s = 0.0;
         for (int w = 0; w < NW; ++w) s += s_sum[w];
-        *out = SelectPart{s, most_x, count};
+        // relative to the part's greatest logit, not to its rounded product
+        *out = SelectPart{huge ? log(s) : log(s) + ((double)m2 * kLn2 - (double)most_x), most_x, count};
     }
 }
 
@@ -244,7 +292,12 @@ __device__ __forceinline__ u64 ord_from_double(double s)
     return (u >> 63) ? ~u : (u | 0x8000000000000000ull);
 }
 
-// One sentence: normalisers, then the k_out best of what its rows have handed on.  Bound: latency.
+__device__ __forceinline__ double double_from_ord(u64 o)
+{
+    return __longlong_as_double((long long)((o >> 63) ? (o & 0x7FFFFFFFFFFFFFFFull) : ~o));
+}
+
+// One sentence: normalisers, then the k_out best of what its rows' parts have handed on.  Bound: latency (a chain of loads and barriers).
 template <int T>
 __global__ __launch_bounds__(T) void dba_select_sentence_kernel(SelectParams p)
 {
@@ -253,70 +306,92 @@ __global__ __launch_bounds__(T) void dba_select_sentence_kernel(SelectParams p)
     __shared__ float s_top[DBA_MAX_BEAM];
     __shared__ uint32_t s_max[T];
     __shared__ int s_int[NW];
-    __shared__ int s_count;
-    __shared__ u64 s_ord[kSelectFinal];
-    __shared__ uint32_t s_flat[kSelectFinal];
-    __shared__ double s_score[kSelectFinal];
-    const int t = (int)threadIdx.x, b = (int)blockIdx.x;
-    const SelectPart *parts = p.parts + (size_t)b * p.k_in * p.nparts;
-    const u64 *keys = p.keys + (size_t)b * p.k_in * p.nparts * p.cap;
+    __shared__ int s_count, s_lists;
+    __shared__ uint32_t s_list[kSelectLists];
+    __shared__ u64 s_ord[2 * kSelectFinal];
+    __shared__ uint32_t s_flat[2 * kSelectFinal];
+    const int t = (int)threadIdx.x, b = (int)blockIdx.x, wave = t / kWave;
+    const int lists = p.k_in * p.nparts;
+    const SelectPart *parts = p.parts + (size_t)b * lists;
+    const u64 *keys = p.keys + (size_t)b * lists * p.cap;
     if (t < p.k_in) {
         const int flags = p.flags ? p.flags[b * p.k_in + t] : 0;
         const double score = (double)p.score[b * p.k_in + t];
+        const SelectPart *mine = parts + t * p.nparts;
         double base = score;
         float most = 0.0f;
         if (!(flags & DBA_FLAG_FINISHED)) {
-            most = -INFINITY;
-            for (int i = 0; i < p.nparts; ++i)
-                if (parts[t * p.nparts + i].sum != 0.0) most = fmaxf(most, parts[t * p.nparts + i].top);
-            double sum = 0.0;
-            for (int i = 0; i < p.nparts; ++i) {
-                const SelectPart q = parts[t * p.nparts + i];
-                if (q.sum != 0.0) sum += q.sum * exp((double)q.top - (double)most);
+            double log_sum = mine[0].log_sum;
+            most = mine[0].top;
+            if (p.nparts > 1) {
+                most = -INFINITY;
+                for (int i = 0; i < p.nparts; ++i)
+                    if (mine[i].log_sum != -INFINITY) most = fmaxf(most, mine[i].top);
+                double sum = 0.0;
+                for (int i = 0; i < p.nparts; ++i)
+                    if (mine[i].log_sum != -INFINITY) sum += exp(mine[i].log_sum + ((double)mine[i].top - (double)most));
+                log_sum = log(sum);
             }
-            base = score - log(sum);
+            base = score - log_sum;
         }
         s_top[t] = most;
         s_base[t] = fabs(base) < INFINITY ? base : __longlong_as_double(0x7FF8000000000000ll);
     }
-    if (t == 0) s_count = 0;
+    if (t == 0) s_count = s_lists = 0;
     __syncthreads();
-    const int places = p.k_in * p.nparts * p.cap;
-    auto each = [&](auto f) {
-        for (int i = t; i < places; i += T) {
-            const int list = i / p.cap;
-            if (i - list * p.cap >= parts[list].count) continue;
-            const int h = list / p.nparts;
-            const u64 key = keys[i];
-            const double s = s_base[h] + ((double)float_from_ord((uint32_t)(key >> 32)) - (double)s_top[h]);
-            if (s == s) f(s, (uint32_t)h * (uint32_t)p.V + key_flat(key));
-        }
+    auto score_of = [&](int h, float x) { return s_base[h] + ((double)x - (double)s_top[h]); };
+    auto best_of = [&](int list) -> uint32_t {    // of a list: the image of its greatest score, 0 if it has none
+        if (!parts[list].count) return 0;
+        const double s = score_of(list / p.nparts, parts[list].top);
+        return s == s ? ord_from_float((float)s) : 0u;
+    };
+    // The k_out-th greatest of the lists' best scores is reached by k_out extensions: lists whose best does not reach it are not looked at.
+    auto kth = [&](uint32_t mine) {
+        s_max[t] = mine;
+        __syncthreads();
+        uint32_t r[NW];
+#pragma unroll
+        for (int j = 0; j < NW; ++j) r[j] = s_max[j * kWave + lane_id()];
+        int reached;
+        return kth_greatest<NW>(r, p.k_out, reached);
     };
     uint32_t top = 0;
-    each([&](double s, uint32_t) {
-        const uint32_t o = ord_from_float((float)s);
-        top = top > o ? top : o;
-    });
-    s_max[t] = top;
+    for (int i = t; i < lists; i += T) top = max(top, best_of(i));
+    uint32_t bar = kth(top);
+    for (int i = t; i < lists; i += T) {
+        const uint32_t best = best_of(i);
+        if (best && best >= bar) {
+            const int at = atomicAdd(&s_lists, 1);
+            if (at < kSelectLists) s_list[at] = (uint32_t)i;
+        }
+    }
     __syncthreads();
-    uint32_t r[NW];
-#pragma unroll
-    for (int j = 0; j < NW; ++j) r[j] = s_max[j * kWave + lane_id()];
-    int reached;
-    const uint32_t bar = kth_greatest<NW>(r, p.k_out, reached);
-    auto put = [&](double s, uint32_t flat) {
+    const int active = s_lists;
+    // every extension of the lists that count: f(score, coordinate)
+    auto each = [&](auto f) {
+        const int n = active <= kSelectLists ? active : lists;
+        for (int i = wave; i < n; i += NW) {
+            const int list = active <= kSelectLists ? (int)s_list[i] : i;
+            const int h = list / p.nparts, count = parts[list].count;
+            for (int j = lane_id(); j < count; j += kWave) {
+                const u64 key = keys[(size_t)list * p.cap + j];
+                const double s = score_of(h, float_from_ord((uint32_t)(key >> 32)));
+                if (s == s) f(s, (uint32_t)h * (uint32_t)p.V + key_flat(key));
+            }
+        }
+    };
+    auto put = [&](u64 ord, uint32_t flat, int from) {
         const int at = atomicAdd(&s_count, 1);
         if (at < kSelectFinal) {
-            s_ord[at] = ord_from_double(s);
-            s_flat[at] = flat;
-            s_score[at] = s;
+            s_ord[from + at] = ord;
+            s_flat[from + at] = flat;
         }
     };
     each([&](double s, uint32_t flat) {
-        if (ord_from_float((float)s) >= bar) put(s, flat);
+        if (ord_from_float((float)s) >= bar) put(ord_from_double(s), flat, 0);
     });
     __syncthreads();
-    int count = s_count;
+    int count = s_count, from = 0;
     if (count > kSelectFinal) {
         // the k_out-th greatest score by bisection, then of its equals the first coordinates
         u64 lo = 0, hi = ~0ull;
@@ -344,24 +419,36 @@ __global__ __launch_bounds__(T) void dba_select_sentence_kernel(SelectParams p)
         __syncthreads();
         each([&](double s, uint32_t flat) {
             const u64 o = ord_from_double(s);
-            if (o > lo || (o == lo && flat <= last)) put(s, flat);
+            if (o > lo || (o == lo && flat <= last)) put(o, flat, 0);
         });
         __syncthreads();
         count = min(s_count, kSelectFinal);
+    } else if (count > 2 * kWave) {
+        // fewer to rank: those that reach the k_out-th greatest of the threads' maxima
+        top = 0;
+        for (int i = t; i < count; i += T) top = max(top, (uint32_t)(s_ord[i] >> 32));
+        bar = kth(top);
+        if (t == 0) s_count = 0;
+        __syncthreads();
+        for (int i = t; i < count; i += T)
+            if ((uint32_t)(s_ord[i] >> 32) >= bar) put(s_ord[i], s_flat[i], kSelectFinal);
+        __syncthreads();
+        count = s_count;
+        from = kSelectFinal;
     }
     int32_t *token = p.out_token + (size_t)b * p.k_out, *back = p.out_backptr + (size_t)b * p.k_out;
     float *score = p.out_score + (size_t)b * p.k_out;
     uint8_t *flags = p.out_flags + (size_t)b * p.k_out;
     for (int i = t; i < count; i += T) {
-        const u64 o = s_ord[i];
-        const uint32_t f = s_flat[i];
+        const u64 o = s_ord[from + i];
+        const uint32_t f = s_flat[from + i];
         int rank = 0;
-        for (int j = 0; j < count; ++j) rank += s_ord[j] > o || (s_ord[j] == o && s_flat[j] < f);
+        for (int j = 0; j < count; ++j) rank += s_ord[from + j] > o || (s_ord[from + j] == o && s_flat[from + j] < f);
         if (rank >= p.k_out) continue;
         const int h = (int)(f / (uint32_t)p.V), w = (int)(f - (uint32_t)h * (uint32_t)p.V);
         token[rank] = w;
         back[rank] = h;
-        score[rank] = (float)s_score[i];
+        score[rank] = (float)double_from_ord(o);
         flags[rank] = w == p.eos || (p.flags && (p.flags[b * p.k_in + h] & DBA_FLAG_FINISHED)) ? DBA_FLAG_FINISHED : 0;
     }
     for (int i = count + t; i < p.k_out; i += T) {
