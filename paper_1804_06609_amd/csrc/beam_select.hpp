@@ -30,6 +30,7 @@ struct SelectParams {
 
 constexpr int kSelectThreads = 256;    // of the first launch
 constexpr int kSelectChunks = 8;       // 16-byte chunks a thread keeps in registers
+constexpr int kSelectQueue = 256;      // chunks it looks through for keys
 constexpr int kSelectFinal = 1024;     // extensions the second launch has room for
 constexpr int kSelectLists = 1024;     // parts with such extensions it has room for
 constexpr double kLn2 = 0.693147180559945309417232121458;
@@ -121,10 +122,40 @@ __device__ __forceinline__ int block_sum(int v, int *room)
     return s;
 }
 
+// A bound that at least k of the wave's J * 64 keys reach (0 = no key), and rarely more than k + k/4 + 4: bisection that stops there.  0 if there
+// are fewer than k.  `most`: the greatest key.
+template <int J>
+__device__ __forceinline__ uint32_t bound_of_kth(const uint32_t (&r)[J], int k, uint32_t most)
+{
+    auto reached = [&](uint32_t x) {
+        int c = 0;
+#pragma unroll
+        for (int j = 0; j < J; ++j) c += (int)__popcll(__ballot(r[j] >= x));
+        return c;
+    };
+    int count = reached(1u);
+    if (count < k) return 0;
+    uint32_t least = 0;                                // of the keys there are
+#pragma unroll
+    for (int j = 0; j < J; ++j) least = max(least, r[j] ? ~r[j] : 0u);
+    uint32_t lo = ~wave_max_uniform(least), hi = most;
+    while (count > k + (k >> 2) + 4 && lo < hi) {
+        const uint32_t mid = lo + ((hi - lo + 1) >> 1);
+        const int c = reached(mid);
+        if (c >= k) {
+            lo = mid;
+            count = c;
+        } else {
+            hi = mid - 1;
+        }
+    }
+    return lo;
+}
+
 // One part of one row.  Bound: HBM (the logits are read once); the exponentials take about a quarter of
 // the VALU's time at that rate.
 template <int FMT>
-__global__ __launch_bounds__(kSelectThreads, 6) void dba_select_part_kernel(const void *logits, SelectParams p)
+__global__ __launch_bounds__(kSelectThreads, 8) void dba_select_part_kernel(const void *logits, SelectParams p)
 {
     typedef Chunk<FMT> C;
     typedef typename C::elem_t elem_t;
@@ -132,7 +163,10 @@ __global__ __launch_bounds__(kSelectThreads, 6) void dba_select_part_kernel(cons
     __shared__ uint32_t s_max[T];
     __shared__ double s_sum[NW];
     __shared__ int s_int[NW];
-    __shared__ int s_count;
+    __shared__ int s_count, s_queued;
+    __shared__ uint32_t s_bar;
+    __shared__ uint4 s_queue[kSelectQueue];
+    __shared__ int s_queue_chunk[kSelectQueue];
     __shared__ u64 s_keys[2 * DBA_MAX_BEAM];
     const int t = (int)threadIdx.x;
     const int part = (int)blockIdx.x % p.nparts, h = (int)blockIdx.x / p.nparts, b = (int)blockIdx.y;
@@ -172,35 +206,37 @@ __global__ __launch_bounds__(kSelectThreads, 6) void dba_select_part_kernel(cons
         }
         return make_uint4(w[0], w[1], w[2], w[3]);
     };
+    // rounds of T chunks; one that starts behind the part's end (for this wave) has nothing
+    const int wave = __builtin_amdgcn_readfirstlane(t / kWave);
+    auto has_round = [&](int r) { return c0 + wave * kWave + r * T < c1; };
     uint4 raw[R];
 #pragma unroll
-    for (int r = 0; r < R; ++r) raw[r] = chunk_at(c0 + t + r * T);
+    for (int r = 0; r < R; ++r)
+        if (has_round(r)) raw[r] = chunk_at(c0 + t + r * T);
     float top = -INFINITY, most_of[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        most_of[r] = C::most(raw[r]);
+        most_of[r] = has_round(r) ? C::most(raw[r]) : -INFINITY;
         top = fmaxf(top, most_of[r]);
     }
     s_max[t] = top > -INFINITY ? ord_from_float(top) : 0u;
-    if (t == 0) s_count = 0;
+    if (t == 0) s_count = s_queued = 0;
     __syncthreads();
-    // k_out threads hold something that reaches the k_out-th greatest of the threads' maxima: so does
-    // everything that can be among the part's k_out greatest
-    uint32_t r4[T / kWave];
+    // k_out threads hold something that reaches the k_out-th greatest of the threads' maxima, or a bound a little below it: so does
+    // everything that can be among the part's k_out greatest.  One wave finds the bound while the others go on with the sum.
+    uint32_t r4[NW];
     uint32_t most = 0;
 #pragma unroll
-    for (int j = 0; j < T / kWave; ++j) {
+    for (int j = 0; j < NW; ++j) {
         r4[j] = s_max[j * kWave + lane_id()];
         most = most > r4[j] ? most : r4[j];
     }
-    most = wave_max_u32(most);
-    int reached;
-    const uint32_t bar_ord = kth_greatest<T / kWave>(r4, p.k_out, reached);
-    const float bar = bar_ord ? float_from_ord(bar_ord) : -INFINITY;
+    most = wave_max_uniform(most);
+    if (wave == (int)(blockIdx.x & (NW - 1))) {
+        const uint32_t at_least = bound_of_kth<NW>(r4, p.k_out, most);
+        if (lane_id() == 0) s_bar = at_least;
+    }
     const float most_x = most ? float_from_ord(most) : 0.0f;
-    uint32_t hits = 0;
-#pragma unroll
-    for (int r = 0; r < R; ++r) hits |= (most_of[r] >= bar && most_of[r] > -INFINITY ? 1u : 0u) << r;
     // The sum: a few dozen terms a thread in fp32 (each is off by 1e-7 of itself, either way), the threads' in 64 bits.  The reference is
     // the rounded product itself, so that no error of its own comes in; where that would overflow (logits at fp32's lowest value),
     // two different logits are so far apart that a term is 0 or 1.
@@ -211,38 +247,60 @@ __global__ __launch_bounds__(kSelectThreads, 6) void dba_select_part_kernel(cons
         float part_sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int r = 0; r < R; ++r)
+            if (has_round(r)) {
 #pragma unroll
-            for (int e = 0; e < N; ++e) part_sum[e & 3] += exp2_above(C::get(raw[r], e), m2);
+                for (int e = 0; e < N; ++e) part_sum[e & 3] += exp2_above(C::get(raw[r], e), m2);
+            }
         sum = (part_sum[0] + part_sum[1]) + (part_sum[2] + part_sum[3]);
     } else {
 #pragma unroll
         for (int r = 0; r < R; ++r)
-#pragma unroll
-            for (int e = 0; e < N; ++e) {
+            for (int e = 0; has_round(r) && e < N; ++e) {
                 const float x = C::get(raw[r], e);
                 sum += x < most_x ? 0.0f : x == most_x && x < INFINITY ? 1.0f : NAN;
             }
     }
-    // the few chunks that reach the bar, from memory once more (registers cannot be indexed)
-    while (hits) {
-        const int r = __ffs(hits) - 1;
-        hits &= hits - 1;
-        const int c = c0 + t + r * T;
-        const uint4 again = chunk_at(c);
+    const double total = wave_sum_double((double)sum);
+    if (lane_id() == 0) s_sum[wave] = total;
+    __syncthreads();
+    // the few chunks that reach the bar go through LDS: there a thread looks at one chunk's elements, here it would look at all of its own
+    const float bar = s_bar ? float_from_ord(s_bar) : -INFINITY;
+    int hits = 0;
+#pragma unroll
+    for (int r = 0; r < R; ++r) hits += most_of[r] >= bar && most_of[r] > -INFINITY;
+    if (hits) {
+        int at = atomicAdd(&s_queued, hits);
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            if (most_of[r] >= bar && most_of[r] > -INFINITY) {
+                if (at < kSelectQueue) {
+                    s_queue[at] = raw[r];
+                    s_queue_chunk[at] = c0 + t + r * T;
+                }
+                ++at;
+            }
+    }
+    __syncthreads();
+    const int queued = s_queued;
+    if (queued <= kSelectQueue && t < queued) {
+        const uint4 q = s_queue[t];
+        const int v0 = s_queue_chunk[t] * N - shift;
+        int n = 0;
+#pragma unroll
+        for (int e = 0; e < N; ++e) n += C::get(q, e) >= bar && C::get(q, e) > -INFINITY;
+        int at = atomicAdd(&s_count, n);
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            const float x = C::get(again, e);
+            const float x = C::get(q, e);
             if (x >= bar && x > -INFINITY) {
-                const int at = atomicAdd(&s_count, 1);
-                if (at < p.cap) s_keys[at] = make_key(x, (uint32_t)(c * N - shift + e));
+                if (at < p.cap) s_keys[at] = make_key(x, (uint32_t)(v0 + e));
+                ++at;
             }
         }
     }
-    const double total = wave_sum_double((double)sum);
-    if (lane_id() == 0) s_sum[t / kWave] = total;
     __syncthreads();
     int count = s_count;
-    if (count > p.cap) {
+    if (count > p.cap || queued > kSelectQueue) {
         // many equal logits, or few threads with any: exactly k_out, by bisection on the keys, which all differ
         auto each = [&](auto f) {
 #pragma unroll 1

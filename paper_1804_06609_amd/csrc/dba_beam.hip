@@ -49,7 +49,10 @@ SelectPlan select_plan(int B, int k_in, int k_out, int V, int format)
     const int chunks = (V + per_chunk - 1) / per_chunk + 1;        // a row that starts inside a chunk may touch one more
     const int most = kSelectThreads * kSelectChunks;
     s.nparts = (chunks + most - 1) / most;
+    // whole rounds of the workgroup, where that leaves no part without a chunk
     s.part_chunks = (chunks + s.nparts - 1) / s.nparts;
+    s.part_chunks = (s.part_chunks + kSelectThreads - 1) / kSelectThreads * kSelectThreads;
+    s.nparts = (chunks + s.part_chunks - 1) / s.part_chunks;
     s.cap = std::max(32, 2 * k_out);
     const size_t lists = (size_t)B * k_in * s.nparts;
     s.keys_at = align256(lists * sizeof(SelectPart));
