@@ -362,9 +362,12 @@ __global__ __launch_bounds__(T) void dba_select_sentence_kernel(SelectParams p)
     constexpr int NW = T / kWave;
     __shared__ double s_base[DBA_MAX_BEAM];       // score - log sum exp(x - top); NaN where the row offers nothing
     __shared__ float s_top[DBA_MAX_BEAM];
+    __shared__ int s_done[DBA_MAX_BEAM];
     __shared__ uint32_t s_max[T];
     __shared__ int s_int[NW];
     __shared__ int s_count, s_lists;
+    __shared__ SelectPart s_part[T];
+    __shared__ double s_term[T];
     __shared__ uint32_t s_list[kSelectLists];
     __shared__ u64 s_ord[2 * kSelectFinal];
     __shared__ uint32_t s_flat[2 * kSelectFinal];
@@ -372,35 +375,55 @@ __global__ __launch_bounds__(T) void dba_select_sentence_kernel(SelectParams p)
     const int lists = p.k_in * p.nparts;
     const SelectPart *parts = p.parts + (size_t)b * lists;
     const u64 *keys = p.keys + (size_t)b * lists * p.cap;
+    // what the parts have left behind: in LDS where a thread can take one part, which saves two trips to memory
+    const bool held = lists <= T;
+    if (held && t < lists) s_part[t] = parts[t];
+    const int row_flags = t < p.k_in && p.flags ? p.flags[b * p.k_in + t] : 0;
+    const float row_score = t < p.k_in ? p.score[b * p.k_in + t] : 0.0f;
+    __syncthreads();
+    auto part_of = [&](int i) { return held ? s_part[i] : parts[i]; };
+    // of a row's parts, the exponential of each relative to the row's greatest logit: a part a thread where they are held
+    auto top_of_row = [&](int h) {
+        float most = -INFINITY;
+        for (int i = 0; i < p.nparts; ++i) {
+            const SelectPart q = part_of(h * p.nparts + i);
+            if (q.log_sum != -INFINITY) most = fmaxf(most, q.top);
+        }
+        return most;
+    };
+    auto term_of = [&](int i, float most) {
+        const SelectPart q = part_of(i);
+        return q.log_sum != -INFINITY ? exp(q.log_sum + ((double)q.top - (double)most)) : 0.0;
+    };
+    if (held && p.nparts > 1) {
+        if (t < lists) s_term[t] = term_of(t, top_of_row(t / p.nparts));
+        __syncthreads();
+    }
     if (t < p.k_in) {
-        const int flags = p.flags ? p.flags[b * p.k_in + t] : 0;
-        const double score = (double)p.score[b * p.k_in + t];
-        const SelectPart *mine = parts + t * p.nparts;
-        double base = score;
+        double base = (double)row_score;
         float most = 0.0f;
-        if (!(flags & DBA_FLAG_FINISHED)) {
-            double log_sum = mine[0].log_sum;
-            most = mine[0].top;
+        if (!(row_flags & DBA_FLAG_FINISHED)) {
+            double log_sum = part_of(t * p.nparts).log_sum;
+            most = part_of(t * p.nparts).top;
             if (p.nparts > 1) {
-                most = -INFINITY;
-                for (int i = 0; i < p.nparts; ++i)
-                    if (mine[i].log_sum != -INFINITY) most = fmaxf(most, mine[i].top);
+                most = top_of_row(t);
                 double sum = 0.0;
-                for (int i = 0; i < p.nparts; ++i)
-                    if (mine[i].log_sum != -INFINITY) sum += exp(mine[i].log_sum + ((double)mine[i].top - (double)most));
+                for (int i = t * p.nparts; i < (t + 1) * p.nparts; ++i) sum += held ? s_term[i] : term_of(i, most);
                 log_sum = log(sum);
             }
-            base = score - log_sum;
+            base -= log_sum;
         }
         s_top[t] = most;
+        s_done[t] = row_flags & DBA_FLAG_FINISHED;
         s_base[t] = fabs(base) < INFINITY ? base : __longlong_as_double(0x7FF8000000000000ll);
     }
     if (t == 0) s_count = s_lists = 0;
     __syncthreads();
     auto score_of = [&](int h, float x) { return s_base[h] + ((double)x - (double)s_top[h]); };
     auto best_of = [&](int list) -> uint32_t {    // of a list: the image of its greatest score, 0 if it has none
-        if (!parts[list].count) return 0;
-        const double s = score_of(list / p.nparts, parts[list].top);
+        const SelectPart q = part_of(list);
+        if (!q.count) return 0;
+        const double s = score_of(list / p.nparts, q.top);
         return s == s ? ord_from_float((float)s) : 0u;
     };
     // The k_out-th greatest of the lists' best scores is reached by k_out extensions: lists whose best does not reach it are not looked at.
@@ -410,8 +433,10 @@ __global__ __launch_bounds__(T) void dba_select_sentence_kernel(SelectParams p)
         uint32_t r[NW];
 #pragma unroll
         for (int j = 0; j < NW; ++j) r[j] = s_max[j * kWave + lane_id()];
-        int reached;
-        return kth_greatest<NW>(r, p.k_out, reached);
+        uint32_t most = 0;
+#pragma unroll
+        for (int j = 0; j < NW; ++j) most = max(most, r[j]);
+        return bound_of_kth<NW>(r, p.k_out, wave_max_uniform(most));
     };
     uint32_t top = 0;
     for (int i = t; i < lists; i += T) top = max(top, best_of(i));
@@ -427,14 +452,26 @@ __global__ __launch_bounds__(T) void dba_select_sentence_kernel(SelectParams p)
     const int active = s_lists;
     // every extension of the lists that count: f(score, coordinate)
     auto each = [&](auto f) {
-        const int n = active <= kSelectLists ? active : lists;
-        for (int i = wave; i < n; i += NW) {
-            const int list = active <= kSelectLists ? (int)s_list[i] : i;
-            const int h = list / p.nparts, count = parts[list].count;
-            for (int j = lane_id(); j < count; j += kWave) {
-                const u64 key = keys[(size_t)list * p.cap + j];
-                const double s = score_of(h, float_from_ord((uint32_t)(key >> 32)));
-                if (s == s) f(s, (uint32_t)h * (uint32_t)p.V + key_flat(key));
+        // 64 keys a wave at a time, eight such loads under way
+        const int pieces = (p.cap + kWave - 1) / kWave, n = (active <= kSelectLists ? active : lists) * pieces;
+        for (int i0 = wave; i0 < n; i0 += 8 * NW) {
+            u64 key[8];
+            int row[8];
+#pragma unroll
+            for (int x = 0; x < 8; ++x) {
+                const int i = i0 + x * NW, piece = pieces == 2 ? i & 1 : 0;
+                key[x] = 0;
+                row[x] = 0;
+                if (i >= n) continue;                  // (the same for the whole wave)
+                const int at = pieces == 2 ? i >> 1 : i, list = active <= kSelectLists ? (int)s_list[at] : at;
+                const int j = piece * kWave + lane_id();
+                row[x] = list / p.nparts;
+                if (j < part_of(list).count) key[x] = keys[(size_t)list * p.cap + j];
+            }
+#pragma unroll
+            for (int x = 0; x < 8; ++x) {
+                const double s = score_of(row[x], float_from_ord((uint32_t)(key[x] >> 32)));
+                if (key[x] && s == s) f(s, (uint32_t)row[x] * (uint32_t)p.V + key_flat(key[x]));
             }
         }
     };
@@ -481,7 +518,7 @@ __global__ __launch_bounds__(T) void dba_select_sentence_kernel(SelectParams p)
         });
         __syncthreads();
         count = min(s_count, kSelectFinal);
-    } else if (count > 2 * kWave) {
+    } else if (count > p.k_out + 16) {
         // fewer to rank: those that reach the k_out-th greatest of the threads' maxima
         top = 0;
         for (int i = t; i < count; i += T) top = max(top, (uint32_t)(s_ord[i] >> 32));
@@ -497,17 +534,21 @@ __global__ __launch_bounds__(T) void dba_select_sentence_kernel(SelectParams p)
     int32_t *token = p.out_token + (size_t)b * p.k_out, *back = p.out_backptr + (size_t)b * p.k_out;
     float *score = p.out_score + (size_t)b * p.k_out;
     uint8_t *flags = p.out_flags + (size_t)b * p.k_out;
-    for (int i = t; i < count; i += T) {
-        const u64 o = s_ord[from + i];
-        const uint32_t f = s_flat[from + i];
+    // sixteen threads count what goes before an extension
+    for (int i = t / 16; i < (count + 3) / 4 * 4; i += T / 16) {       // (whole waves: the lanes of one exchange below)
+        const bool is = i < count;
+        const u64 o = is ? s_ord[from + i] : 0;
+        const uint32_t f = is ? s_flat[from + i] : 0;
         int rank = 0;
-        for (int j = 0; j < count; ++j) rank += s_ord[from + j] > o || (s_ord[from + j] == o && s_flat[from + j] < f);
-        if (rank >= p.k_out) continue;
+        for (int j = t & 15; j < count; j += 16) rank += s_ord[from + j] > o || (s_ord[from + j] == o && s_flat[from + j] < f);
+#pragma unroll
+        for (int d = 8; d; d >>= 1) rank += __shfl_xor(rank, d);
+        if (!is || (t & 15) || rank >= p.k_out) continue;
         const int h = (int)(f / (uint32_t)p.V), w = (int)(f - (uint32_t)h * (uint32_t)p.V);
         token[rank] = w;
         back[rank] = h;
         score[rank] = (float)double_from_ord(o);
-        flags[rank] = w == p.eos || (p.flags && (p.flags[b * p.k_in + h] & DBA_FLAG_FINISHED)) ? DBA_FLAG_FINISHED : 0;
+        flags[rank] = w == p.eos || s_done[h] ? DBA_FLAG_FINISHED : 0;
     }
     for (int i = count + t; i < p.k_out; i += T) {
         token[i] = p.pad;

@@ -152,7 +152,7 @@ hipError_t select_launch(const SelectParams &p, int B, const void *logits, hipSt
 {
     hipError_t e = launch(dba_select_part_kernel<FMT>, dim3((unsigned)(p.nparts * p.k_in), (unsigned)B), dim3(kSelectThreads), 0, stream, logits, p);
     if (e != hipSuccess) return e;
-    return p.k_in * p.nparts * p.cap <= 4096 ? launch(dba_select_sentence_kernel<256>, dim3((unsigned)B), dim3(256), 0, stream, p)
+    return p.k_in * p.nparts <= 32 ? launch(dba_select_sentence_kernel<256>, dim3((unsigned)B), dim3(256), 0, stream, p)
                                              : launch(dba_select_sentence_kernel<1024>, dim3((unsigned)B), dim3(1024), 0, stream, p);
 }
 
