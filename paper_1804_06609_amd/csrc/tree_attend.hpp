@@ -12,6 +12,7 @@
 #pragma once
 #include "cache_append.hpp"
 #include "paged.hpp"
+#include "wave_topk.hpp"
 
 namespace dba {
 
@@ -110,15 +111,16 @@ __device__ __forceinline__ bool make_finite(u32x4 &c)
     return found;
 }
 
-__device__ __forceinline__ float max_over_groups(float v)      // over the four lanes of a row
+// Over the four lanes of a row, without a trip through LDS.
+__device__ __forceinline__ float max_over_groups(float v)
 {
-    v = fmaxf(v, __shfl_xor(v, 16));
-    return fmaxf(v, __shfl_xor(v, 32));
+    v = fmaxf(v, __uint_as_float(xor16_valu_u32(__float_as_uint(v))));
+    return fmaxf(v, __uint_as_float(xor32_u32(__float_as_uint(v))));
 }
 __device__ __forceinline__ float sum_over_groups(float v)
 {
-    v += __shfl_xor(v, 16);
-    return v + __shfl_xor(v, 32);
+    v += __uint_as_float(xor16_valu_u32(__float_as_uint(v)));
+    return v + __uint_as_float(xor32_u32(__float_as_uint(v)));
 }
 
 // How a kernel's LDS is laid out.  ROWS: the four waves have rows of their own and share tiles of 64 tokens, keys and values both in LDS;
@@ -236,6 +238,16 @@ __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) vo
             }
     };
 
+    // which rows see which tokens of tile u (bit t: token t)
+    auto seen_of = [&](int u, int t) -> unsigned long long {
+        if (u < prefix_tiles || u >= u1) return ~0ull;
+        const int j0 = (u - prefix_tiles) * TT;
+        if (p.mask) return (j0 >> 6) < p.mask_words ? mask_row[t][j0 >> 6] >> (j0 & 63) : 0;
+        const int last = chain[t] - j0;
+        return last < 0 ? 0 : last >= 63 ? ~0ull : (2ull << last) - 1;
+    };
+    unsigned long long seen[QT], seen_next[QT];
+
     f32x4 o[QT][DT];
     float m[QT], l[QT];
 #pragma unroll
@@ -253,6 +265,8 @@ __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) vo
         page[t] = page_of(first, t);
         page_next[t] = page_of(first + step, t);
     }
+#pragma unroll
+    for (int t = 0; t < QT; ++t) seen_next[t] = seen_of(first, t);
     if (first < u1) {
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
@@ -265,22 +279,7 @@ __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) vo
     int buf = 0;
     for (int u = first; u < u1; u += step) {
         const bool in_tree = u >= prefix_tiles;
-        const int j0 = (u - prefix_tiles) * TT;        // of a tile of the tree
         unsigned char *const kb = s_mem + buf * A::TILE, *const vb = s_v + (ROWS ? buf * A::TILE : 0);
-        // which rows see which tokens of the tile (bit t: token t)
-        unsigned long long seen[QT];
-#pragma unroll
-        for (int t = 0; t < QT; ++t) {
-            seen[t] = ~0ull;
-            if (in_tree) {
-                if (p.mask) {
-                    seen[t] = (j0 >> 6) < p.mask_words ? mask_row[t][j0 >> 6] >> (j0 & 63) : 0;
-                } else {
-                    const int last = chain[t] - j0;
-                    seen[t] = last < 0 ? 0 : last >= 63 ? ~0ull : (2ull << last) - 1;
-                }
-            }
-        }
         // this wave's tokens of the tile: values into LDS, where those that are not there, and in the tree what is not finite,
         // become 0 (a weight of 0 would not keep them out of the product)
         unsigned long long live = 0;
@@ -315,8 +314,14 @@ __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) vo
             __syncthreads();
             live = s_live[buf][0] | s_live[buf][1] | s_live[buf][2] | s_live[buf][3];
         }
-        // the next tile's values, and in this form its keys, are asked for now
+        // The next tile's mask and values, and in this form its keys, are asked for now, and before them the pages of the one
+        // behind: loads come back in order, so waiting for a tile is waiting for all that the next steps need.
         int64_t at[NT];
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+            seen[t] = seen_next[t];
+            seen_next[t] = seen_of(u + step, t);
+        }
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             page[t] = page_next[t];
@@ -376,15 +381,15 @@ __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) vo
                 for (int d = 0; d < DT; ++d) o[j][d] *= keep;
             }
             const float base = m[j] == -INFINITY ? 0.0f : m[j];
-            float sum = 0.0f;
+            float sum[2] = {0.0f, 0.0f};
 #pragma unroll
             for (int t = 0; t < CT; ++t)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     s[t][j][i] = __builtin_amdgcn_exp2f(fmaf(s[t][j][i], sl2, -base));
-                    sum += s[t][j][i];
+                    sum[i & 1] += s[t][j][i];
                 }
-            l[j] += sum;
+            l[j] += sum[0] + sum[1];
         }
         // O^T += V^T P^T
         if constexpr (FMT == 0) {
