@@ -95,12 +95,6 @@ template <> struct Chunk<2> {
     static constexpr uint32_t kNone = 0xFF80u;
 };
 
-__device__ __forceinline__ float wave_max_float(float v)
-{
-#pragma unroll
-    for (int d = 32; d; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
-    return v;
-}
 __device__ __forceinline__ double wave_sum_double(double v)
 {
 #pragma unroll

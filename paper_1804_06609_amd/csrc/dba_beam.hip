@@ -395,6 +395,8 @@ DBA_API int dba_tree_attend(int B, int n, int q_heads, const dba_heads *q, const
     p.tile_rows = plan.tile_rows;
     p.splits = plan.splits;
     p.chunk = plan.chunk;
+    p.pairs = B * cache->heads;
+    p.groups = p.pairs * plan.splits;
     p.part_o = static_cast<float *>(workspace_dev);
     p.part_ml = reinterpret_cast<float *>(static_cast<unsigned char *>(workspace_dev) + align256(attend_rows_of(B, n, q_heads, plan) * cache->head_dim * 4));
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);

@@ -27,6 +27,7 @@ struct AttendParams {
     int n, q_heads, heads, D, mask_words, max_len;
     int row_tiles, tile_rows;          // workgroups along the rows, rows of each
     int splits, chunk;                 // workgroups along the token axis, tiles of each
+    int pairs, groups;                 // sentences times heads; times splits
     float scale;
 };
 
@@ -111,6 +112,13 @@ __device__ __forceinline__ bool make_finite(u32x4 &c)
     return found;
 }
 
+__device__ __forceinline__ float wave_max_float(float v)
+{
+#pragma unroll
+    for (int d = 32; d; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
+    return v;
+}
+
 // Over the four lanes of a row, without a trip through LDS.
 __device__ __forceinline__ float max_over_groups(float v)
 {
@@ -157,7 +165,10 @@ struct AttendShape {
     }
 };
 
-// Grid: x = row tile + row_tiles * split, y = head of the cache, z = sentence.
+// Workgroups come to the eight XCDs in turn.  The row tiles of one part of one head, which read the same tokens, are put behind each
+// other on one XCD, whose L2 then serves all but the first (63 nodes, 8 query heads to one, 32 sentences of 500 to 4000 tokens:
+// 225 -> 140 us).  There the parts of the token axis vary slowest, so that what is left of short sentences comes last; where
+// tokens are read once they vary fastest (4 sentences of 50000 and more: 186 instead of 199 us).
 template <int FMT, int DP, int QT, bool ROWS>
 __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) void dba_attend_kernel(AttendParams p)
 {
@@ -170,8 +181,19 @@ __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) vo
     __shared__ int s_bad;
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int c = lane & 15, g = lane >> 4;
-    const int row_tile = (int)blockIdx.x % p.row_tiles, split = (int)blockIdx.x / p.row_tiles;
-    const int head = (int)blockIdx.y, b = (int)blockIdx.z;
+    const uint32_t id = blockIdx.y * gridDim.x + blockIdx.x, turn = id / 8;
+    const uint32_t group = turn / (uint32_t)p.row_tiles * 8 + id % 8;
+    if (group >= (uint32_t)p.groups) return;
+    const int row_tile = (int)(turn % (uint32_t)p.row_tiles);
+    int split, pair;
+    if (ROWS) {
+        split = (int)(group / (uint32_t)p.pairs);
+        pair = (int)(group % (uint32_t)p.pairs);
+    } else {
+        pair = (int)(group / (uint32_t)p.splits);
+        split = (int)((group + (uint32_t)pair * (uint32_t)p.splits / 8) % (uint32_t)p.splits);    // (an XCD gets all kinds of parts)
+    }
+    const int b = pair / p.heads, head = pair % p.heads;
     const int G = p.q_heads / p.heads, rows = p.n * G;
     const int row0 = (ROWS ? row_tile * 4 + wave : row_tile) * 16 * QT;
 
@@ -434,9 +456,10 @@ __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) vo
     }
 
     // results: [rows, D] of the output, or this split's part
+    const bool whole = tiles <= p.chunk;               // no other part has anything
     const size_t part = (((size_t)b * p.heads + head) * p.splits + split) * rows;
     auto put_row = [&](int r, float mm, float ll) {    // statistics of a row
-        if (p.splits > 1) {
+        if (!whole) {
             p.part_ml[(part + r) * 2] = mm;
             p.part_ml[(part + r) * 2 + 1] = ll;
         } else if (p.lse) {
@@ -444,7 +467,7 @@ __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) vo
         }
     };
     auto put = [&](int r, int d, float ll, f32x4 v) {  // four elements of a row
-        if (p.splits > 1) {
+        if (!whole) {
             *reinterpret_cast<f32x4 *>(p.part_o + (part + r) * p.D + d) = v;
             return;
         }
@@ -535,12 +558,13 @@ __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) vo
             if (!(fabsf(y) < INFINITY)) v += y;
         }
         if (v == 0.0f) continue;
-        if (p.splits > 1) p.part_o[(part + r) * p.D + e] = v;
+        if (!whole) p.part_o[(part + r) * p.D + e] = v;
         else reinterpret_cast<E *>(p.out.data)[(int64_t)b * p.out.sent + (int64_t)node * p.out.token + (int64_t)(head * G + r % G) * p.out.head + e] = (E)v;
     }
 }
 
-// Joins the splits of a row: one wave a row, four elements a lane.
+// Joins the parts of a row, a wave a row: its lanes take a part's four elements each, and as many parts at a time as there are lanes for.
+// Rows with one part have been written already.
 template <int FMT>
 __global__ __launch_bounds__(256) void dba_attend_join_kernel(AttendParams p, int tile)
 {
@@ -550,26 +574,51 @@ __global__ __launch_bounds__(256) void dba_attend_join_kernel(AttendParams p, in
     if (r >= rows) return;
     int tree_all;
     const Span span = span_of_rows(p, b, r / p.tile_rows, G, tree_all);
-    const int tree = span.end - span.prefix;
-    const int tiles = (span.prefix + tile - 1) / tile + (tree + tile - 1) / tile;
-    const int live = max(1, min(p.splits, (tiles + p.chunk - 1) / p.chunk));
+    const int tiles = (span.prefix + tile - 1) / tile + (span.end - span.prefix + tile - 1) / tile;
+    if (tiles <= p.chunk) return;
+    const int parts = (tiles + p.chunk - 1) / p.chunk;
     const size_t part = ((size_t)b * p.heads + head) * p.splits * rows + r;
-    float top = -INFINITY;
-    for (int s = 0; s < live; ++s) top = fmaxf(top, p.part_ml[(part + (size_t)s * rows) * 2]);
-    float sum = 0.0f;
+    const int across = p.D <= 32 ? 8 : p.D <= 64 ? 16 : p.D <= 128 ? 32 : 64, d = lane % across * 4;     // lanes of a part
+    float top = -INFINITY, sum = 0.0f;
     f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
-    const int d = lane * 4;
-    for (int s = 0; s < live; ++s) {
-        const size_t at = part + (size_t)s * rows;
-        const float ms = p.part_ml[at * 2], ls = p.part_ml[at * 2 + 1];
-        if (ls == 0.0f) continue;
-        const float f = ms == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ms - top);
-        sum += ls * f;
-        if (d < p.D) v += *reinterpret_cast<const f32x4 *>(p.part_o + at * p.D + d) * f;
+    for (int s0 = 0; s0 < parts; s0 += 64) {
+        const int n = min(64, parts - s0);
+        float ms = -INFINITY, ls = 0.0f;
+        if (lane < n) {
+            const size_t at = part + (size_t)(s0 + lane) * rows;
+            ms = p.part_ml[at * 2];
+            ls = p.part_ml[at * 2 + 1];
+        }
+        const float top1 = fmaxf(top, wave_max_float(ms));
+        const float keep = top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(top - top1);
+        const float w = ls == 0.0f ? 0.0f : ms == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ms - top1);
+        float more = ls * w;
+#pragma unroll
+        for (int x = 32; x; x >>= 1) more += __shfl_xor(more, x);
+        top = top1;
+        sum = sum * keep + more;
+        v *= keep;
+        for (int s1 = 0; s1 < n; s1 += 4 * (64 / across)) {
+            f32x4 y[4];
+            float f[4];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const int s = s1 + x * (64 / across) + lane / across;
+                f[x] = __shfl(w, s & 63);
+                y[x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                if (s < n && d < p.D) y[x] = *reinterpret_cast<const f32x4 *>(p.part_o + (part + (size_t)(s0 + s) * rows) * p.D + d);
+                else f[x] = 0.0f;
+            }
+#pragma unroll
+            for (int x = 0; x < 4; ++x) v += y[x] * f[x];
+        }
     }
+    for (int x = across; x < 64; x *= 2)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] += __shfl_xor(v[i], x);
     const int64_t row = ((int64_t)b * p.n + r / G) * p.q_heads + head * G + r % G;
     if (lane == 0 && p.lse) p.lse[row] = sum != 0.0f ? (top + __builtin_amdgcn_logf(sum)) * kLn2f : -INFINITY;
-    if (d < p.D) {
+    if (lane < across && d < p.D) {
         v *= sum != 0.0f ? 1.0f / sum : 0.0f;
         E *to = reinterpret_cast<E *>(p.out.data) + ((int64_t)b * p.out.sent + (int64_t)(r / G) * p.out.token + (int64_t)(head * G + r % G) * p.out.head + d);
         if constexpr (FMT == 0) *reinterpret_cast<f32x4 *>(to) = v;

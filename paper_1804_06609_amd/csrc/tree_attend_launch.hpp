@@ -15,7 +15,8 @@ hipError_t attend_one(const AttendParams &p, int B, hipStream_t stream)
                                                  hipFuncAttributeMaxDynamicSharedMemorySize, lds);
         if (e != hipSuccess) return e;
     }
-    return launch(dba_attend_kernel<FMT, DP, QT, ROWS>, dim3((unsigned)(p.row_tiles * p.splits), (unsigned)p.heads, (unsigned)B), dim3(256), lds, stream, p);
+    const unsigned blocks = ((unsigned)p.groups + 7) / 8 * 8 * (unsigned)p.row_tiles, wide = blocks < 65536 ? blocks : 65536;
+    return launch(dba_attend_kernel<FMT, DP, QT, ROWS>, dim3(wide, (blocks + wide - 1) / wide), dim3(256), lds, stream, p);
 }
 
 template <int FMT, int DP>
