@@ -121,11 +121,12 @@ AttendPlan attend_plan(int B, int n, int q_heads, const dba_cache &c, int max_le
     a.QT = a.shared ? (a.DP <= 128 ? 2 : 1) : rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
     a.tile_rows = (a.shared ? 64 : 16) * a.QT;
     a.row_tiles = (rows + a.tile_rows - 1) / a.tile_rows;
-    a.tile = a.shared ? 64 : f32 ? 16 : 32;
+    a.tile = a.shared ? 64
+           : a.DP == 64 && a.QT <= 2 ? (f32 ? attend_tile<0, 64, 2> : attend_tile<1, 64, 2>) : f32 ? attend_tile<0, 128, 2> : attend_tile<1, 128, 2>;
     const int tiles = (max_len + a.tile - 1) / a.tile + 1;         // (the prefix and the tree each end in a tile of their own)
     const int64_t groups = (int64_t)B * c.heads * a.row_tiles;
     const int64_t want = std::max<int64_t>(1, (1024 + groups - 1) / groups);
-    const int least = a.shared ? 4 : 8;
+    const int least = 4;
     int64_t chunk = std::max<int64_t>(least, (tiles + want - 1) / want);
     chunk = (chunk + 3) / 4 * 4;
     a.chunk = (int)chunk;
@@ -344,8 +345,10 @@ DBA_API int dba_cache_append(int B, int n, const dba_cache *cache, const dba_hea
     p.interleaved = interleaved != 0;
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     const dim3 grid((unsigned)n, (unsigned)B);
+    const int pairs = (p.q_heads + 2 * p.heads) * (((p.D * (int)elem_bytes(cache->format) + 15) / 16 + 1) / 2);
+    const unsigned threads = (unsigned)std::min(kAppendThreads, (pairs + 63) / 64 * 64);       // a thread for every two chunks of a token
     const auto kernel = cache->format == DBA_LOGP_F32 ? dba_append_kernel<0> : cache->format == DBA_LOGP_F16 ? dba_append_kernel<1> : dba_append_kernel<2>;
-    return launched("dba_cache_append", launch(kernel, grid, dim3(kAppendThreads), 0, stream, p));
+    return launched("dba_cache_append", launch(kernel, grid, dim3(threads), 0, stream, p));
 }
 
 DBA_API size_t dba_tree_attend_workspace_bytes(int B, int n, int q_heads, const dba_cache *cache, int max_len)

@@ -131,14 +131,17 @@ __device__ __forceinline__ float sum_over_groups(float v)
     return v + __uint_as_float(xor32_u32(__float_as_uint(v)));
 }
 
+// Tokens a wave takes at a time where it has tiles of its own: 16 KB of keys and values where there are registers for that.
+template <int FMT, int DP, int QT> constexpr int attend_tile = (FMT == 0 ? 16 : 32) * (DP == 64 && QT <= 2 ? 2 : 1);
+
 // How a kernel's LDS is laid out.  ROWS: the four waves have rows of their own and share tiles of 64 tokens, keys and values both in LDS;
-// else they have all rows and tiles of their own (32 tokens, 16 in fp32), keys straight in registers, values in LDS.
+// else they have all rows and tiles of their own, keys straight in registers, values in LDS.
 template <int FMT, int DP, int QT, bool ROWS>
 struct AttendShape {
     static constexpr int ES = FMT == 0 ? 4 : 2;
     static constexpr int KS = DP / 32;                  // steps of 32 elements
     static constexpr int DT = DP / 16;                  // tiles of 16 elements
-    static constexpr int NT = ROWS || FMT == 0 ? 1 : 2; // 16-token tiles a wave loads at a time
+    static constexpr int NT = ROWS ? 1 : attend_tile<FMT, DP, QT> / 16;     // 16-token tiles a wave loads at a time
     static constexpr int CT = ROWS ? 4 : NT;            // and works on at a time
     static constexpr int TT = 16 * CT;
     static constexpr int ROW = DP * ES;                 // bytes
