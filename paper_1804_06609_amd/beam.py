@@ -75,11 +75,11 @@ def _stream(x: torch.Tensor) -> int:
     return torch._C._cuda_getCurrentRawStream(index)       # (torch.cuda.current_stream() takes 2.8 us to say the same)
 
 
-def _ints(name: str, x: Optional[torch.Tensor], shape, like: torch.Tensor) -> Optional[int]:
+def _ints(name: str, x: Optional[torch.Tensor], shape, device: int) -> Optional[int]:
     """Address of a dense int32 tensor of this shape (None where it may be left out)."""
     if x is None:
         return None
-    if x.dtype is not torch.int32 or x.shape != shape or x.device != like.device or not x.is_contiguous():
+    if x.dtype is not torch.int32 or x.shape != shape or x.get_device() != device or not x.is_contiguous():
         _fail(f"{name} must be a contiguous int32 tensor {tuple(shape)} on the device of the others")
     return x.data_ptr()
 
@@ -88,7 +88,7 @@ def _workspace(nbytes: int, like: torch.Tensor):
     """(tensor, address): torch's allocations start on 512 bytes."""
     if not nbytes:
         return None, None
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=like.device)
+    ws = like.new_empty(nbytes, dtype=torch.uint8)
     return ws, ws.data_ptr()
 
 
@@ -100,9 +100,9 @@ def select(logits: torch.Tensor, score: torch.Tensor, flags: Optional[torch.Tens
     if logits.dim() != 3 or logits.dtype not in _FORMATS or (logits.shape[2] > 1 and logits.stride(2) != 1):
         _fail("logits must be [B, k, V] of fp32, fp16 or bf16 with a dense last axis")
     B, k, V = logits.shape
-    stream = _stream(logits)
+    stream, device = _stream(logits), logits.get_device()
     for name, x, dtype in (("score", score, torch.float32), ("flags", flags, torch.uint8)):
-        if x is not None and (x.dtype is not dtype or x.shape != (B, k) or not x.is_contiguous() or x.device != logits.device):
+        if x is not None and (x.dtype is not dtype or x.shape != (B, k) or not x.is_contiguous() or x.get_device() != device):
             _fail(f"{name} must be a contiguous {dtype} tensor [B, k] on the device of the logits")
     if out is None:
         like = score if k_out == k else score.new_empty((B, k_out))
@@ -110,7 +110,7 @@ def select(logits: torch.Tensor, score: torch.Tensor, flags: Optional[torch.Tens
                torch.empty_like(like, dtype=torch.uint8))
     else:
         for x, dtype in zip(out, (torch.int32, torch.int32, torch.float32, torch.uint8), strict=True):
-            if x.dtype is not dtype or x.shape != (B, k_out) or not x.is_contiguous() or x.device != logits.device:
+            if x.dtype is not dtype or x.shape != (B, k_out) or not x.is_contiguous() or x.get_device() != device:
                 _fail("out must be four contiguous tensors [B, k_out]: int32, int32, fp32, uint8")
     fmt = _FORMATS[logits.dtype]
     nbytes = lib.dba_beam_select_workspace_bytes(B, k, k_out, V, fmt)
@@ -151,14 +151,15 @@ def reorder(backptr: torch.Tensor, states: Sequence[torch.Tensor], out: Optional
         _fail("backptr must be [B, k]")
     B, k = backptr.shape
     stream = _stream(backptr)
-    back = _ints("backptr", backptr, backptr.shape, backptr)
+    device = backptr.get_device()
+    back = _ints("backptr", backptr, backptr.shape, device)
     out = states if out is None else out
     if len(out) != len(states):
         _fail("as many tensors out as states")
     table = []                                         # the fields of dba_state, one state after another
     rows = B * k
     for s, d in zip(states, out):
-        if s.shape[:2] != (B, k) or s.shape != d.shape or s.dtype is not d.dtype or s.device != backptr.device or d.device != backptr.device:
+        if s.shape[:2] != (B, k) or s.shape != d.shape or s.dtype is not d.dtype or s.get_device() != device or d.get_device() != device:
             _fail("states and out must be [B, k, ...] tensors alike in shape and type, on the device of backptr")
         if s.is_contiguous() and d.is_contiguous():
             row = s.numel() // rows * s.element_size()
@@ -178,30 +179,34 @@ def reorder(backptr: torch.Tensor, states: Sequence[torch.Tensor], out: Optional
     return out
 
 
-def _cache(k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor, like: torch.Tensor) -> bytes:
-    strides = [[st if size > 1 else 0 for st, size in zip(x.stride(), x.shape)] for x in (k_pages, v_pages)]
-    if k_pages.dim() != 4 or v_pages.shape != k_pages.shape or strides[0] != strides[1] or strides[0][3] != 1:
-        _fail("k_pages and v_pages must be [pages, page_size, heads, head_dim], laid out alike, with a dense last axis")
-    if k_pages.dtype not in _FORMATS or v_pages.dtype is not k_pages.dtype or k_pages.dtype is not like.dtype:
+def _cache(k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor, like: torch.Tensor, device: int) -> bytes:
+    shape = k_pages.shape
+    if len(shape) != 4 or v_pages.shape != shape:
+        _fail("k_pages and v_pages must be [pages, page_size, heads, head_dim]")
+    n_pages, page, heads, D = shape
+    s, r = k_pages.stride(), v_pages.stride()
+    if s != r or page == 1 or heads == 1 or n_pages == 1:  # the stride of an axis of one is never used; torch gives it any value
+        s, r = ([st if size > 1 else 0 for st, size in zip(x, shape)] for x in (s, r))
+    if s != r or (D > 1 and s[3] != 1):
+        _fail("k_pages and v_pages must be laid out alike, with a dense last axis")
+    dtype = k_pages.dtype
+    if dtype not in _FORMATS or v_pages.dtype is not dtype or like.dtype is not dtype:
         _fail("keys, values, queries and pages must be of one type: fp32, fp16 or bf16")
     if table.dtype is not torch.int32 or table.dim() != 2 or table.stride(1) != 1 or table.shape[0] != like.shape[0]:
         _fail("table must be an int32 tensor [B, max_pages] with a dense last axis")
-    if k_pages.device != like.device or v_pages.device != like.device or table.device != like.device:
+    if k_pages.get_device() != device or v_pages.get_device() != device or table.get_device() != device:
         _fail("tensors must be on one device")
-    n_pages, page, heads, D = k_pages.shape
-    s = strides[0]
     return _pack_cache(k_pages.data_ptr(), v_pages.data_ptr(), table.data_ptr(), table.stride(0), s[0], s[1], s[2],
-                  _FORMATS[k_pages.dtype], n_pages, page, table.shape[1], heads, D)
+                       _FORMATS[dtype], n_pages, page, table.shape[1], heads, D)
 
 
-def _heads(name: str, x: torch.Tensor, B: int, n: int, heads: Optional[int], D: int, like: torch.Tensor) -> bytes:
-    if x.dim() != 4 or x.shape[0] != B or x.shape[1] != n or (heads is not None and x.shape[2] != heads) or x.shape[3] != D:
-        _fail(f"{name} must be [B, n, heads, head_dim]")
-    if x.dtype is not like.dtype or x.device != like.device or x.stride(3) != 1:
+def _heads(name: str, x: torch.Tensor, shape, dtype, device: int) -> bytes:
+    if x.shape != shape:
+        _fail(f"{name} must be [B, n, heads, head_dim], here {tuple(shape)}")
+    s = x.stride()
+    if x.dtype is not dtype or x.get_device() != device or (s[3] != 1 and shape[3] > 1):
         _fail(f"{name} must be of the type and on the device of the others, with a dense last axis")
-    # the stride of an axis of one is never used; torch gives it any value
-    s = [st if size > 1 else 0 for st, size in zip(x.stride(), x.shape)]
-    return _pack_heads(x.data_ptr(), s[0], s[1], s[2])
+    return _pack_heads(x.data_ptr(), s[0] if shape[0] > 1 else 0, s[1] if shape[1] > 1 else 0, s[2] if shape[2] > 1 else 0)
 
 
 def append(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor, first: torch.Tensor,
@@ -212,24 +217,30 @@ def append(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: tor
     tensor if None; q itself is allowed), which is returned."""
     lib = load()
     stream = _stream(k)
-    if k.dim() != 4:
+    shape, dtype, device = k.shape, k.dtype, k.get_device()
+    if len(shape) != 4:
         _fail("k must be [B, n, heads, head_dim]")
-    B, n, heads, D = k.shape
-    cache = _cache(k_pages, v_pages, table, k)
+    B, n, heads, D = shape
+    cache = _cache(k_pages, v_pages, table, k, device)
     if k_pages.shape[2:] != (heads, D):
         _fail("k has other heads than the cache")
-    kh, vh = _heads("k", k, B, n, heads, D, k), _heads("v", v, B, n, heads, D, k)
     qh = oh = None
+    q_heads = 0
     if q is not None:
+        if q.dim() != 4:
+            _fail("q must be [B, n, q_heads, head_dim]")
+        q_heads = q.shape[2]
         if q_out is None:
-            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        qh, oh = _heads("q", q, B, n, None, D, k), _heads("q_out", q_out, B, n, q.shape[2], D, k)
-    if inv_freq is not None and (inv_freq.dtype is not torch.float32 or inv_freq.dim() != 1 or not inv_freq.is_contiguous() or inv_freq.device != k.device):
-        _fail("inv_freq must be a contiguous fp32 tensor [rot_dim / 2]")
-    rot = 0 if inv_freq is None else 2 * inv_freq.shape[0]
-    _b._check(lib.dba_cache_append(B, n, cache, kh, vh, 0 if q is None else q.shape[2], qh, oh,
-                                   _ints("first", first, (B,), k), _ints("count", count, (B,), k), _ints("position", position, (B, n), k),
-                                   inv_freq.data_ptr() if rot else None, rot, int(interleaved), stream))
+            q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        qh, oh = _heads("q", q, (B, n, q_heads, D), dtype, device), _heads("q_out", q_out, (B, n, q_heads, D), dtype, device)
+    rot, freq = 0, None
+    if inv_freq is not None:
+        if inv_freq.dtype is not torch.float32 or inv_freq.dim() != 1 or not inv_freq.is_contiguous() or inv_freq.get_device() != device:
+            _fail("inv_freq must be a contiguous fp32 tensor [rot_dim / 2]")
+        rot, freq = 2 * inv_freq.shape[0], inv_freq.data_ptr()
+    _b._check(lib.dba_cache_append(B, n, cache, _heads("k", k, shape, dtype, device), _heads("v", v, shape, dtype, device), q_heads, qh, oh,
+                                   _ints("first", first, (B,), device), _ints("count", count, (B,), device),
+                                   _ints("position", position, (B, n), device), freq, rot, interleaved, stream))
     return q_out
 
 
@@ -242,29 +253,30 @@ def attend(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, table:
     if None; a close bound makes a better launch).  Returns out, or (out, lse [B, n, q_heads] fp32)."""
     lib = load()
     stream = _stream(q)
-    if q.dim() != 4:
+    shape, dtype, device = q.shape, q.dtype, q.get_device()
+    if len(shape) != 4:
         _fail("q must be [B, n, q_heads, head_dim]")
-    B, n, heads, D = q.shape
-    cache = _cache(k_pages, v_pages, table, q)
+    B, n, heads, D = shape
+    cache = _cache(k_pages, v_pages, table, q, device)
     if k_pages.shape[3] != D:
         _fail("q has another head_dim than the cache")
     if out is None:
-        out = q.new_empty((B, n, heads, D))
-    words = 0
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    words, bits = 0, None
     if mask is not None:
-        if mask.dtype is not torch.int64 or mask.dim() != 3 or mask.shape[:2] != (B, n) or not mask.is_contiguous() or mask.device != q.device:
+        if mask.dtype is not torch.int64 or mask.dim() != 3 or mask.shape[:2] != (B, n) or not mask.is_contiguous() or mask.get_device() != device:
             _fail("mask must be a contiguous int64 tensor [B, n, words] on the device of the others")
         words = mask.shape[2]
-        if not words:                                  # a mask without a bit: nothing of the tree is seen
+        if words:
+            bits = mask.data_ptr()
+        else:                                              # a mask without a bit: nothing of the tree is seen
             tree = None
-    qh, oh = _heads("q", q, B, n, heads, D, q), _heads("out", out, B, n, heads, D, q)
-    lse = torch.empty((B, n, heads), dtype=torch.float32, device=q.device) if return_lse else None
+    lse = q.new_empty((B, n, heads), dtype=torch.float32) if return_lse else None
     if max_len is None:
         max_len = min(table.shape[1] * k_pages.shape[1], 2**31 - 1)
     nbytes = lib.dba_tree_attend_workspace_bytes(B, n, heads, cache, max_len)
     ws, at = _workspace(nbytes, q)
-    _b._check(lib.dba_tree_attend(B, n, heads, qh, cache, _ints("prefix", prefix, (B,), q),
-                                  _ints("tree", tree, (B,), q), mask.data_ptr() if words else None, words, max_len,
-                                  D ** -0.5 if scale is None else float(scale), oh, lse.data_ptr() if return_lse else None,
-                                  at, nbytes, stream))
+    _b._check(lib.dba_tree_attend(B, n, heads, _heads("q", q, shape, dtype, device), cache, _ints("prefix", prefix, (B,), device),
+                                  _ints("tree", tree, (B,), device), bits, words, max_len, D ** -0.5 if scale is None else scale,
+                                  _heads("out", out, shape, dtype, device), lse.data_ptr() if return_lse else None, at, nbytes, stream))
     return (out, lse) if return_lse else out
