@@ -123,23 +123,21 @@ def select(logits: torch.Tensor, score: torch.Tensor, flags: Optional[torch.Tens
 
 def _pieces(x: torch.Tensor):
     """[B, k, ...] as (sent, row, seg strides in bytes, pieces, bytes of a piece); the axes behind the second fold into two."""
-    e = x.element_size()
-    shape, strides = list(x.shape[2:]), list(x.stride()[2:])
-    seg, dense = 1, 1                                  # dense: elements of a piece so far
-    while shape and (shape[-1] == 1 or strides[-1] == dense):
-        dense *= shape.pop()
-        strides.pop()
-    seg_stride = 0
-    while shape:
-        n, s = shape.pop(), strides.pop()
-        if n == 1:
-            continue
-        if seg == 1:
-            seg_stride = s
-        elif s != seg_stride * seg:
-            return None
-        seg *= n
-    return x.stride(0) * e, x.stride(1) * e, seg_stride * e, seg, dense * e
+    e, shape, strides = x.element_size(), x.shape, x.stride()
+    i, dense = len(shape) - 1, 1                       # dense: elements of a piece so far
+    while i > 1 and (strides[i] == dense or shape[i] == 1):
+        dense *= shape[i]
+        i -= 1
+    seg, seg_stride = 1, 0
+    while i > 1:
+        if shape[i] != 1:
+            if seg == 1:
+                seg_stride = strides[i]
+            elif strides[i] != seg_stride * seg:
+                return None
+            seg *= shape[i]
+        i -= 1
+    return strides[0] * e, strides[1] * e, seg_stride * e, seg, dense * e
 
 
 def reorder(backptr: torch.Tensor, states: Sequence[torch.Tensor], out: Optional[Sequence[torch.Tensor]] = None):
@@ -157,15 +155,17 @@ def reorder(backptr: torch.Tensor, states: Sequence[torch.Tensor], out: Optional
     if len(out) != len(states):
         _fail("as many tensors out as states")
     table = []                                         # the fields of dba_state, one state after another
-    rows = B * k
+    rows, head = B * k, backptr.shape
     for s, d in zip(states, out):
-        if s.shape[:2] != (B, k) or s.shape != d.shape or s.dtype is not d.dtype or s.get_device() != device or d.get_device() != device:
+        shape = s.shape
+        if shape[:2] != head or d.shape != shape or s.dtype is not d.dtype or s.get_device() != device or d.get_device() != device:
             _fail("states and out must be [B, k, ...] tensors alike in shape and type, on the device of backptr")
         if s.is_contiguous() and d.is_contiguous():
             row = s.numel() // rows * s.element_size()
             table += (d.data_ptr(), s.data_ptr(), row * k, row, 0, row * k, row, 0, 1, row)
             continue
-        a, c = _pieces(s), _pieces(d)
+        a = _pieces(s)
+        c = a if d is s or d.stride() == s.stride() else _pieces(d)
         if a is None or c is None:
             _fail("a state's axes behind the second must fold into pieces of one stride")
         if a[3:] != c[3:]:                             # one side is more finely cut: the smaller piece serves both

@@ -31,6 +31,7 @@ struct SelectParams {
 constexpr int kSelectThreads = 256;    // of the first launch
 constexpr int kSelectChunks = 8;       // 16-byte chunks a thread keeps in registers
 constexpr int kSelectQueue = 256;      // chunks it looks through for keys
+constexpr int kSelectKeys = 1024;      // keys it chooses from
 constexpr int kSelectFinal = 1024;     // extensions the second launch has room for
 constexpr int kSelectLists = 1024;     // parts with such extensions it has room for
 constexpr double kLn2 = 0.693147180559945309417232121458;
@@ -161,7 +162,7 @@ __global__ __launch_bounds__(kSelectThreads, 8) void dba_select_part_kernel(cons
     __shared__ uint32_t s_bar;
     __shared__ uint4 s_queue[kSelectQueue];
     __shared__ int s_queue_chunk[kSelectQueue];
-    __shared__ u64 s_keys[2 * DBA_MAX_BEAM];
+    __shared__ u64 s_keys[kSelectKeys];
     const int t = (int)threadIdx.x;
     const int part = (int)blockIdx.x % p.nparts, h = (int)blockIdx.x / p.nparts, b = (int)blockIdx.y;
     const int row = b * p.k_in + h;
@@ -287,15 +288,48 @@ __global__ __launch_bounds__(kSelectThreads, 8) void dba_select_part_kernel(cons
         for (int e = 0; e < N; ++e) {
             const float x = C::get(q, e);
             if (x >= bar && x > -INFINITY) {
-                if (at < p.cap) s_keys[at] = make_key(x, (uint32_t)(v0 + e));
+                if (at < kSelectKeys) s_keys[at] = make_key(x, (uint32_t)(v0 + e));
                 ++at;
             }
         }
     }
     __syncthreads();
     int count = s_count;
-    if (count > p.cap || queued > kSelectQueue) {
-        // many equal logits, or few threads with any: exactly k_out, by bisection on the keys, which all differ
+    if (queued <= kSelectQueue && count > p.cap && count <= kSelectKeys) {
+        // short rows, or the best next to each other: the first wave hands on those from a bound that at least k_out and at most
+        // cap of the keys reach (they all differ)
+        if (wave == 0) {
+            constexpr int J = kSelectKeys / kWave;
+            u64 key[J];
+#pragma unroll
+            for (int j = 0; j < J; ++j) key[j] = j * kWave + lane_id() < count ? s_keys[j * kWave + lane_id()] : 0;
+            u64 lo = 1, hi = ~0ull;
+            int n = count;
+            while (n > p.cap && lo < hi) {
+                const u64 mid = lo + ((hi - lo) >> 1) + 1;
+                int c = 0;
+#pragma unroll
+                for (int j = 0; j < J; ++j) c += (int)__popcll(__ballot(key[j] >= mid));
+                if (c >= p.k_out) {
+                    lo = mid;
+                    n = c;
+                } else {
+                    hi = mid - 1;
+                }
+            }
+            int at = 0;
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                const u64 in = __ballot(key[j] >= lo && key[j]);
+                if ((in >> lane_id()) & 1) out_keys[at + (int)__popcll(in & ((1ull << lane_id()) - 1))] = key[j];
+                at += (int)__popcll(in);
+            }
+            if (lane_id() == 0) s_int[0] = at;         // (not s_count: other waves may not have read it yet)
+        }
+        __syncthreads();
+        count = s_int[0];
+    } else if (count > p.cap || queued > kSelectQueue) {
+        // a great many equal logits: exactly k_out, by bisection on the keys
         auto each = [&](auto f) {
 #pragma unroll 1
             for (int r = 0; r < R; ++r) {
@@ -328,8 +362,10 @@ __global__ __launch_bounds__(kSelectThreads, 8) void dba_select_part_kernel(cons
         });
         __syncthreads();
         count = min(s_count, p.cap);
+        for (int i = t; i < count; i += T) out_keys[i] = s_keys[i];
+    } else {
+        for (int i = t; i < count; i += T) out_keys[i] = s_keys[i];
     }
-    for (int i = t; i < count; i += T) out_keys[i] = s_keys[i];
     if (t == 0) {
         double s = 0.0;
         for (int w = 0; w < NW; ++w) s += s_sum[w];

@@ -141,6 +141,21 @@ def test_select_equal_logits_go_to_the_first(beam, dtype, V):
         assert got[0][1].tolist() == token[0].tolist() and got[1][1].tolist() == back[0].tolist()
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("V", [200, 1164, 20000, 70001])
+def test_select_where_the_best_lie_together(beam, dtype, V):
+    """Tokens in the order of their frequency, up and down; coarse logits, of which many are equal; a block of tokens allowed."""
+    g = gen(V)
+    x = torch.randn(4, 9, V, generator=g) * 2
+    x[0] = x[0].sort(dim=1, descending=True).values
+    x[1] = x[1].sort(dim=1).values
+    x[2] = (x[2] * 2).round() / 2
+    x[3, :, V // 2:] = -math.inf
+    score = -torch.rand(4, 9, generator=g) * 4 - 5
+    for k_out in (1, 9, 31, 64):
+        check_select(beam, x.to(dtype), score, None, k_out)
+
+
 def test_select_twice_is_the_same(beam):
     logits, score, flags = a_beam(9, 4, 20, 32000, torch.float32)
     args = [logits.cuda(), score.cuda(), flags.cuda(), 20, EOS, PAD]
