@@ -9,6 +9,7 @@ Nothing of the methods runs here, and there is no fallback: without the built li
 from __future__ import annotations
 
 import ctypes
+import functools
 import struct
 from typing import Optional, Sequence
 
@@ -121,9 +122,9 @@ def select(logits: torch.Tensor, score: torch.Tensor, flags: Optional[torch.Tens
     return tuple(out)
 
 
-def _pieces(x: torch.Tensor):
+@functools.lru_cache(maxsize=1024)
+def _pieces(shape, strides, e: int):
     """[B, k, ...] as (sent, row, seg strides in bytes, pieces, bytes of a piece); the axes behind the second fold into two."""
-    e, shape, strides = x.element_size(), x.shape, x.stride()
     i, dense = len(shape) - 1, 1                       # dense: elements of a piece so far
     while i > 1 and (strides[i] == dense or shape[i] == 1):
         dense *= shape[i]
@@ -164,8 +165,7 @@ def reorder(backptr: torch.Tensor, states: Sequence[torch.Tensor], out: Optional
             row = s.numel() // rows * s.element_size()
             table += (d.data_ptr(), s.data_ptr(), row * k, row, 0, row * k, row, 0, 1, row)
             continue
-        a = _pieces(s)
-        c = a if d is s or d.stride() == s.stride() else _pieces(d)
+        a, c = _pieces(shape, s.stride(), s.element_size()), _pieces(shape, d.stride(), d.element_size())
         if a is None or c is None:
             _fail("a state's axes behind the second must fold into pieces of one stride")
         if a[3:] != c[3:]:                             # one side is more finely cut: the smaller piece serves both

@@ -518,6 +518,20 @@ __global__ __launch_bounds__(T) void dba_select_sentence_kernel(SelectParams p)
     __syncthreads();
     int count = s_count, from = 0;
     if (count > kSelectFinal) {
+        // hardly more lists than slots: a better bound, from the threads' greatest
+        top = 0;
+        each([&](double s, uint32_t) { top = max(top, ord_from_float((float)s)); });
+        bar = max(bar, kth(top));
+        if (t == 0) s_count = 0;
+        __syncthreads();
+        each([&](double s, uint32_t flat) {
+            if (ord_from_float((float)s) >= bar) put(ord_from_double(s), flat, 0);
+        });
+        __syncthreads();
+        count = s_count;
+        __syncthreads();                           // (read by all before it is set again)
+    }
+    if (count > kSelectFinal) {
         // the k_out-th greatest score by bisection, then of its equals the first coordinates
         u64 lo = 0, hi = ~0ull;
         while (lo < hi) {

@@ -110,25 +110,30 @@ HeadsAt heads_of(const dba_heads *h)
     return HeadsAt{static_cast<unsigned char *>(h->data), h->sent_stride, h->token_stride, h->head_stride};
 }
 
+// Rows (nodes times the query heads of a cache head) decide the form.  Up to 64, a wave holds them all and the waves share out the tokens,
+// which are then read once; with more, or without registers for so many, the waves have rows of their own and share the tokens' tiles
+// (504 rows of 128: 145 us against 246 with row tiles of 64 that each read the tokens; 40 to 48 rows of 128: 175 and 197 us against
+// 182 and 184 with shared tiles).  The token axis is cut into as many parts as fill the GPU once: each part costs a start-up of several
+// trips to memory, and twice as many were slower (one sentence of 29000 tokens 59 against 43 us, five of 21600 56 against 39),
+// but for shared tiles, whose sentences' lengths matter more than that.
 AttendPlan attend_plan(int B, int n, int q_heads, const dba_cache &c, int max_len)
 {
     AttendPlan a;
     const int rows = n * (q_heads / c.heads);
-    a.DP = c.head_dim <= 64 ? 64 : c.head_dim <= 128 ? 128 : 256;
     const bool f32 = c.format == DBA_LOGP_F32;
+    a.DP = c.head_dim <= 64 ? 64 : c.head_dim <= 128 ? 128 : 256;
     const int widest = a.DP == 64 ? kAttendWidest<1, 64> : a.DP == 256 ? kAttendWidest<1, 256> : f32 ? kAttendWidest<0, 128> : kAttendWidest<1, 128>;
     a.shared = rows > 16 * widest;
     a.QT = a.shared ? (a.DP <= 128 ? 2 : 1) : rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
     a.tile_rows = (a.shared ? 64 : 16) * a.QT;
     a.row_tiles = (rows + a.tile_rows - 1) / a.tile_rows;
     a.tile = a.shared ? 64
-           : a.DP == 64 && a.QT <= 2 ? (f32 ? attend_tile<0, 64, 2> : attend_tile<1, 64, 2>) : f32 ? attend_tile<0, 128, 2> : attend_tile<1, 128, 2>;
+           : a.DP == 64 && a.QT <= 2 ? (f32 ? attend_tile<0, 64, 2> : attend_tile<1, 64, 2>) : f32 ? attend_tile<0, 256, 1> : attend_tile<1, 256, 1>;
     const int tiles = (max_len + a.tile - 1) / a.tile + 1;         // (the prefix and the tree each end in a tile of their own)
     const int64_t groups = (int64_t)B * c.heads * a.row_tiles;
-    const int64_t want = std::max<int64_t>(1, (1024 + groups - 1) / groups);
-    const int least = 4;
-    int64_t chunk = std::max<int64_t>(least, (tiles + want - 1) / want);
-    chunk = (chunk + 3) / 4 * 4;
+    const int resident = a.DP == 256 || (a.DP == 128 && (a.QT == 4 || (f32 && a.QT == 2))) ? 256 : 512;
+    const int64_t parts = std::max<int64_t>(1, resident * (a.shared ? 2 : 1) / groups);
+    const int64_t chunk = std::max<int64_t>(4, ((tiles + parts - 1) / parts + 3) / 4 * 4);         // a tile a wave at least
     a.chunk = (int)chunk;
     a.splits = (int)((tiles + chunk - 1) / chunk);
     return a;

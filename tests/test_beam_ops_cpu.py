@@ -180,7 +180,8 @@ def test_tensors_have_to_be_on_the_gpu():
     (lambda: torch.zeros(2, 3, 4, 5, 10, 8)[:, :, :, :2, :6], None),
 ])
 def test_pieces_of_a_state(make, want):
-    assert beam._pieces(make()) == want
+    x = make()
+    assert beam._pieces(x.shape, x.stride(), x.element_size()) == want
 
 
 # ---- the cache's addresses ---------------------------------------------------------------------------------------------
