@@ -117,10 +117,11 @@ DBA_API int dba_cache_append(int B, int n, const dba_cache *cache, const dba_hea
  * sees: the prefix[b] first ones of the sentence's cache and, of the tree[b] ones behind them, token j where bit j % 64 of
  * mask[b, i, j / 64] is set (bits from 64 * mask_words on count as not set); without a mask those with j <= tree[b] - n + i (the n queries are
  * the last n tokens of a chain).  A node that sees nothing gets 0 and a normaliser of -inf.
- *   q, out         [B, n, q_heads, head_dim]; q_heads a multiple of the cache's heads
+ *   q, out         [B, n, q_heads, head_dim]; q_heads a multiple of the cache's heads; n * q_heads <= 2^22, and B * heads times the
+ *                  sixteens of n * q_heads / heads at most 2^28
  *   prefix_dev, tree_dev   device [B] int32; negative ones count as 0; tree_dev may be NULL (0 everywhere)
  *   mask_dev       device [B, n, mask_words] uint64, or NULL
- *   max_len        no sentence sees tokens from max_len on (at most max_pages * page_size); the launch is laid out for it
+ *   max_len        no sentence sees tokens from max_len on (at most max_pages * page_size and 2^31 - 1024); the launch is laid out for it
  *   out_lse_dev    device [B, n, q_heads] fp32: log of the sum of the exponentials; may be NULL
  *   workspace_dev  device, 256-byte aligned, at least dba_tree_attend_workspace_bytes bytes (which may be 0)
  * What masked places, and places behind the end, hold never matters, NaN and infinities included.

@@ -162,7 +162,7 @@ def reorder(backptr: torch.Tensor, states: Sequence[torch.Tensor], out: Optional
         if shape[:2] != head or d.shape != shape or s.dtype is not d.dtype or s.get_device() != device or d.get_device() != device:
             _fail("states and out must be [B, k, ...] tensors alike in shape and type, on the device of backptr")
         if s.is_contiguous() and d.is_contiguous():
-            row = s.numel() // rows * s.element_size()
+            row = s.numel() // max(1, rows) * s.element_size()
             table += (d.data_ptr(), s.data_ptr(), row * k, row, 0, row * k, row, 0, 1, row)
             continue
         a, c = _pieces(shape, s.stride(), s.element_size()), _pieces(shape, d.stride(), d.element_size())
@@ -273,7 +273,7 @@ def attend(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, table:
             tree = None
     lse = q.new_empty((B, n, heads), dtype=torch.float32) if return_lse else None
     if max_len is None:
-        max_len = min(table.shape[1] * k_pages.shape[1], 2**31 - 1)
+        max_len = min(table.shape[1] * k_pages.shape[1], 2**31 - 1024)
     nbytes = lib.dba_tree_attend_workspace_bytes(B, n, heads, cache, max_len)
     ws, at = _workspace(nbytes, q)
     _b._check(lib.dba_tree_attend(B, n, heads, _heads("q", q, shape, dtype, device), cache, _ints("prefix", prefix, (B,), device),

@@ -23,6 +23,7 @@ namespace {
 
 constexpr size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 constexpr int kMostRows = 1 << 22;          // tokens, or heads of tokens, of one sentence in a call
+constexpr int kMostLength = INT32_MAX - 1023;   // tokens that attention looks at: positions of the tiles behind them are ints, too
 
 int launched(const char *who, hipError_t e)
 {
@@ -146,7 +147,10 @@ const char *attend_fault(int B, int n, int q_heads, const dba_cache *cache, int 
     if (B < 1 || B > 65535 || n < 1 || q_heads < 1 || q_heads > 8192 || (int64_t)n * q_heads > kMostRows)
         return "need 1 <= B <= 65535, 1 <= q_heads <= 8192, n >= 1, n * q_heads <= 2^22";
     if (q_heads % cache->heads) return "q_heads must be a multiple of the cache's heads";
-    if (max_len < 1 || max_len > cache->max_pages * cache->page_size) return "need 1 <= max_len <= max_pages * page_size";
+    if (max_len < 1 || max_len > cache->max_pages * cache->page_size || max_len > kMostLength)
+        return "need 1 <= max_len <= max_pages * page_size, max_len <= 2^31 - 1024";
+    if ((int64_t)B * cache->heads * (((int64_t)n * (q_heads / cache->heads) + 15) / 16) > (1 << 28))
+        return "need B * heads * (n * q_heads / heads, in sixteens) <= 2^28";
     return nullptr;
 }
 

@@ -2,7 +2,7 @@
 //
 // For one sentence and one head of the cache, the queries that read it are rows: row r is node r / G, query head r % G of the
 // G that share the head.  With x = scale log2 e (q . k), a row's output is sum 2^(x_t - m) v_t / sum 2^(x_t - m) over the tokens it
-// sees, m being the running maximum; parts of the token axis are joined by their maxima and sums.
+// sees, m being the running maximum (less a constant in fp16); parts of the token axis are joined by their maxima and sums.
 //
 // Both products run on the matrix units, transposed: S^T = K Q^T leaves lane (g, c) of a wave (c = lane % 16, g = lane / 16) with
 // four consecutive tokens 4g .. 4g+3 of row c, which is what the second product O^T = V^T P^T takes as its right operand: the
@@ -51,6 +51,10 @@ typedef short i16x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2f = 0.69314718055994530942f;
+
+// A row's greatest weight is 2^kWeightBits, and m its score less that: where weights are rounded to fp16, whose exponents end at 2^-14 (and
+// steps at 2^-24), a long tail of small ones would be lost from the product and not from the sum.
+template <int FMT> constexpr float kWeightBits = FMT == 1 ? 14.0f : 0.0f;
 
 // Eight elements of a row along the contraction: 16 bytes, or 32 in fp32.
 template <int FMT> struct Frag {
@@ -202,7 +206,7 @@ __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) vo
 
     int tree_all;
     const Span span = span_of_rows(p, b, row_tile, G, tree_all);
-    const int tree = span.end - span.prefix;
+    const int tree = span.end - span.prefix;           // (max_len leaves room for a few tiles more before 2^31)
     const int prefix_tiles = (span.prefix + TT - 1) / TT, tiles = prefix_tiles + (tree + TT - 1) / TT;
     const int u0 = split * p.chunk, u1 = min(tiles, u0 + p.chunk);
     if (u0 >= tiles && split > 0) return;              // (the join does not ask for it; the first split is always there)
@@ -396,7 +400,7 @@ __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) vo
             for (int t = 0; t < CT; ++t)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) top = fmaxf(top, s[t][j][i]);
-            top = max_over_groups(top) * sl2;
+            top = fmaf(max_over_groups(top), sl2, -kWeightBits<FMT>);
             if (__any(top > m[j])) {                   // (a maximum stays as it is in most tiles)
                 const float m1 = fmaxf(m[j], top);
                 const float keep = m1 == m[j] ? 1.0f : __builtin_amdgcn_exp2f(m[j] - m1);

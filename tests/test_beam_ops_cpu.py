@@ -164,6 +164,14 @@ def test_attend_refuses(kw, frag):
     _refused(_attend(**kw), frag)
 
 
+def test_attend_refuses_what_positions_or_the_grid_have_no_room_for():
+    long = _cache(page=1, max_pages=2**31 - 1, table_stride=2**31 - 1, n_pages=2**31 - 1)
+    _refused(_attend(long, max_len=2**31 - 1023), "2^31 - 1024")
+    assert beam.load().dba_tree_attend_workspace_bytes(1, 1, 4, ctypes.byref(long), 2**31 - 1023) == 0
+    assert beam.load().dba_tree_attend_workspace_bytes(1, 1, 4, ctypes.byref(long), 2**31 - 1024) > 0
+    _refused(_attend(q_heads=8, B=65535, n=1 << 15), "2^28")
+
+
 def test_tensors_have_to_be_on_the_gpu():
     with pytest.raises(dba.DbaError, match="GPU"):
         beam.select(torch.zeros(1, 2, 8), torch.zeros(1, 2), None, 2, 2, 0)

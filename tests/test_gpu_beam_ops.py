@@ -221,6 +221,13 @@ def test_reorder_of_more_states_than_one_launch_takes(beam):
         assert torch.equal(d.cpu(), plain_reorder(back, x))
 
 
+def test_reorder_of_no_rows_is_refused(beam):
+    from paper_1804_06609_amd import DbaError
+    for shape in ((0, 4), (3, 0)):
+        with pytest.raises(DbaError, match="B"):
+            beam.reorder(torch.zeros(shape, dtype=torch.int32, device="cuda"), [torch.zeros(shape + (5,), device="cuda")])
+
+
 # ---- caches ------------------------------------------------------------------------------------------------------------
 def a_cache(seed, B, tokens, heads, D, page, dtype, layout="nhd", fill=None):
     """Pages of B sentences in random order; "hnd" has the heads before the tokens of a page."""
@@ -486,6 +493,24 @@ def test_attend_what_is_not_seen_does_not_matter(beam, dtype, bad):
     near(got[:, :n // 2], lse[:, :n // 2], half)
     if bad != -math.inf:                                                # who does see it is told
         assert not torch.isfinite(got[:, n // 2:].float()).all(dim=3).any()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n", [1, 70])
+def test_attend_over_a_long_tail_of_small_weights(beam, dtype, n):
+    """One token of weight 1 whose value is 0, thousands of 2^-26 with values of 1: the output is theirs alone."""
+    D, L = 8, 6000
+    k_pages, v_pages, table = a_cache(4, 1, L, 1, D, 16, dtype, fill=0.0)
+    v_pages[...] = 1
+    at = int(table[0, 1]), 3
+    k_pages[at] = 0
+    k_pages[at[0], at[1], 0, 0] = 18.0
+    v_pages[at] = 0
+    q = torch.zeros(1, n, 1, D, dtype=dtype, device="cuda")
+    q[..., 0] = 1
+    prefix, none = torch.tensor([L], dtype=torch.int32), torch.tensor([0], dtype=torch.int32)
+    got, lse = beam.attend(q, k_pages, v_pages, table.cuda(), prefix.cuda(), scale=1.0, return_lse=True)
+    near(got, lse, plain_attend(q, k_pages, v_pages, table, prefix, none, None, 1.0))
 
 
 @pytest.mark.parametrize("dtype", TYPES)
