@@ -5,6 +5,8 @@
 // into registers, sums the exponentials, and hands on the part's k_out greatest logits (and a few more).
 // A second launch, one workgroup per sentence, puts the normalisers together and ranks what has been handed on.
 #pragma once
+#include <type_traits>
+
 #include "wave_topk.hpp"
 
 namespace dba {
@@ -54,7 +56,7 @@ template <> struct Chunk<0> {
     static constexpr int N = 4;
     typedef float elem_t;
     static __device__ __forceinline__ float get(const uint4 &c, int e) { return __uint_as_float(((const uint32_t *)&c)[e]); }
-    static __device__ __forceinline__ uint32_t bits(const float *p) { return __float_as_uint(*p); }
+    static __device__ __forceinline__ float value(float x) { return x; }
     static constexpr uint32_t kNone = 0xFF800000u;
 };
 template <> struct Chunk<1> {
@@ -73,7 +75,7 @@ template <> struct Chunk<1> {
         const uint16_t h = (uint16_t)((e & 1) ? w >> 16 : w);
         return (float)__builtin_bit_cast(_Float16, h);
     }
-    static __device__ __forceinline__ uint32_t bits(const uint16_t *p) { return *p; }
+    static __device__ __forceinline__ float value(uint16_t x) { return (float)__builtin_bit_cast(_Float16, x); }
     static constexpr uint32_t kNone = 0xFC00u;
 };
 template <> struct Chunk<2> {
@@ -92,15 +94,31 @@ template <> struct Chunk<2> {
         const uint32_t w = ((const uint32_t *)&c)[e >> 1];
         return __uint_as_float((e & 1) ? w & 0xFFFF0000u : w << 16);
     }
-    static __device__ __forceinline__ uint32_t bits(const uint16_t *p) { return *p; }
+    static __device__ __forceinline__ float value(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
     static constexpr uint32_t kNone = 0xFF80u;
 };
 
+// Sums and maxima over a wave without a trip through LDS.
+template <int J>
+__device__ __forceinline__ double add_lane_xor(double v)
+{
+    return v + __longlong_as_double((long long)xor_lane_t<u64, J, true>((u64)__double_as_longlong(v)));
+}
 __device__ __forceinline__ double wave_sum_double(double v)
 {
-#pragma unroll
-    for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
-    return v;
+    return add_lane_xor<32>(add_lane_xor<16>(add_lane_xor<8>(add_lane_xor<4>(add_lane_xor<2>(add_lane_xor<1>(v))))));
+}
+
+// A place in a list for every lane of the wave that asks for one: one atomic a wave (lanes' own would be taken one after the other).
+__device__ __forceinline__ int place_of_lane(u64 asking, int first)
+{
+    return first + __builtin_amdgcn_mbcnt_hi((uint32_t)(asking >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)asking, 0));
+}
+__device__ __forceinline__ int places_for_wave(int n, int *count)
+{
+    int first = 0;
+    if (lane_id() == 0) first = atomicAdd(count, n);
+    return __builtin_amdgcn_readfirstlane(first);
 }
 
 // Sum of `v` over the workgroup, in every thread.  `room`: one int per wave; ends with a barrier.
@@ -147,8 +165,10 @@ __device__ __forceinline__ uint32_t bound_of_kth(const uint32_t (&r)[J], int k, 
     return lo;
 }
 
-// One part of one row.  Bound: HBM (the logits are read once); the exponentials take about a quarter of
-// the VALU's time at that rate.
+// One part of one row.  Bound: HBM (the logits are read once); with 16 bits the VALU is about as busy: an element takes five
+// instructions, one of them the exponential.  So nothing else is done element by element: addresses are the same for a whole wave
+// but for its lanes' 16 bytes, edges of a row that do not fill a chunk are single elements of the first wave, and of the chunks only those that
+// reach the bar are looked through (128 x 64 rows of 50000 in bf16: SELECT_TIME).
 template <int FMT>
 __global__ __launch_bounds__(kSelectThreads, 8) void dba_select_part_kernel(const void *logits, SelectParams p)
 {
@@ -163,8 +183,8 @@ __global__ __launch_bounds__(kSelectThreads, 8) void dba_select_part_kernel(cons
     __shared__ uint4 s_queue[kSelectQueue];
     __shared__ int s_queue_chunk[kSelectQueue];
     __shared__ u64 s_keys[kSelectKeys];
-    const int t = (int)threadIdx.x;
-    const int part = (int)blockIdx.x % p.nparts, h = (int)blockIdx.x / p.nparts, b = (int)blockIdx.y;
+    const int t = (int)threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(t / kWave);
+    const int part = (int)blockIdx.x, h = (int)blockIdx.y, b = (int)blockIdx.z;
     const int row = b * p.k_in + h;
     const size_t list = (size_t)row * p.nparts + part;
     SelectPart *out = p.parts + list;
@@ -181,34 +201,36 @@ __global__ __launch_bounds__(kSelectThreads, 8) void dba_select_part_kernel(cons
         return;
     }
     const elem_t *src = static_cast<const elem_t *>(logits) + ((int64_t)b * p.sent_stride + (int64_t)h * p.row_stride);
-    // chunks lie on the 16-byte grid of memory; the first starts `shift` elements before the row
+    // Chunks lie on the 16-byte grid of memory; the first starts `shift` elements before the row.  [full0, full1) lie in the row whole;
+    // the elements before and behind them are taken one by one, by the first 2N threads of the parts they lie in.
     const int shift = (int)((reinterpret_cast<uintptr_t>(src) & 15) / sizeof(elem_t));
-    const int c0 = part * p.part_chunks, c1 = c0 + p.part_chunks;
-    auto chunk_at = [&](int c) {                       // what is not in the row, or in another part, is -inf
-        const int64_t v0 = (int64_t)c * N - shift;
-        if (c < c1 && v0 >= 0 && v0 + N <= p.V) return *reinterpret_cast<const uint4 *>(src + v0);
-        uint32_t w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = N == 4 ? C::kNone : C::kNone | (C::kNone << 16);
-        if (c < c1) {
-#pragma unroll
-            for (int e = 0; e < N; ++e)
-                if (v0 + e >= 0 && v0 + e < p.V) {
-                    const uint32_t x = C::bits(src + v0 + e);
-                    if (N == 4) w[e] = x;
-                    else w[e >> 1] = (e & 1) ? (w[e >> 1] & 0xFFFFu) | (x << 16) : (w[e >> 1] & 0xFFFF0000u) | x;
-                }
-        }
-        return make_uint4(w[0], w[1], w[2], w[3]);
+    const uint4 *grid = reinterpret_cast<const uint4 *>(src - shift);
+    const int full0 = shift ? 1 : 0, full1 = (p.V + shift) / N;
+    const int c0 = part * p.part_chunks, c1 = min(c0 + p.part_chunks, full1);
+    auto wave_chunk = [&](int r) { return c0 + wave * kWave + r * T; };
+    auto has_round = [&](int r) { return wave_chunk(r) < c1; };       // the same for the whole wave
+    auto none = [] { const uint32_t w = N == 4 ? C::kNone : C::kNone | (C::kNone << 16); return make_uint4(w, w, w, w); };
+    auto load_round = [&](int r) {                     // what is not a whole chunk of this part is -inf
+        const int cw = wave_chunk(r);
+        const uint4 *from = grid + cw;
+        if (cw >= full0 && cw + kWave <= c1) return from[(uint32_t)lane];
+        uint4 v = none();
+        if (cw + lane >= full0 && cw + lane < c1) v = from[(uint32_t)lane];
+        return v;
     };
-    // rounds of T chunks; one that starts behind the part's end (for this wave) has nothing
-    const int wave = __builtin_amdgcn_readfirstlane(t / kWave);
-    auto has_round = [&](int r) { return c0 + wave * kWave + r * T < c1; };
     uint4 raw[R];
 #pragma unroll
     for (int r = 0; r < R; ++r)
-        if (has_round(r)) raw[r] = chunk_at(c0 + t + r * T);
-    float top = -INFINITY, most_of[R];
+        if (has_round(r)) raw[r] = load_round(r);
+    float edge = -INFINITY;                            // a single element
+    int edge_at = 0;
+    if (t < 2 * N) {
+        const int head = full1 == 0 ? p.V : shift ? N - shift : 0, tail = full1 == 0 ? 0 : (p.V + shift) % N;
+        const bool first = t < N;
+        edge_at = first ? t : p.V - tail + (t - N);
+        if (first ? part == 0 && t < head : c0 <= full1 && full1 - c0 < p.part_chunks && t - N < tail) edge = C::value(src[edge_at]);
+    }
+    float top = edge, most_of[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         most_of[r] = has_round(r) ? C::most(raw[r]) : -INFINITY;
@@ -223,23 +245,23 @@ __global__ __launch_bounds__(kSelectThreads, 8) void dba_select_part_kernel(cons
     uint32_t most = 0;
 #pragma unroll
     for (int j = 0; j < NW; ++j) {
-        r4[j] = s_max[j * kWave + lane_id()];
+        r4[j] = s_max[j * kWave + lane];
         most = most > r4[j] ? most : r4[j];
     }
     most = wave_max_uniform(most);
-    if (wave == (int)(blockIdx.x & (NW - 1))) {
+    if (wave == ((part + h) & (NW - 1))) {
         const uint32_t at_least = bound_of_kth<NW>(r4, p.k_out, most);
-        if (lane_id() == 0) s_bar = at_least;
+        if (lane == 0) s_bar = at_least;
     }
     const float most_x = most ? float_from_ord(most) : 0.0f;
     // The sum: a few dozen terms a thread in fp32 (each is off by 1e-7 of itself, either way), the threads' in 64 bits.  The reference is
     // the rounded product itself, so that no error of its own comes in; where that would overflow (logits at fp32's lowest value),
     // two different logits are so far apart that a term is 0 or 1.
-    float sum = 0.0f;
+    float sum;
     const float m2 = most_x * kLog2eHi;
     const bool huge = !(fabsf(most_x) < 1e37f);
     if (!huge) {
-        float part_sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        float part_sum[4] = {exp2_above(edge, m2), 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int r = 0; r < R; ++r)
             if (has_round(r)) {
@@ -248,49 +270,53 @@ __global__ __launch_bounds__(kSelectThreads, 8) void dba_select_part_kernel(cons
             }
         sum = (part_sum[0] + part_sum[1]) + (part_sum[2] + part_sum[3]);
     } else {
+        auto term = [&](float x) { return x < most_x ? 0.0f : x == most_x && x < INFINITY ? 1.0f : NAN; };
+        sum = term(edge);
+#pragma unroll 1
+        for (int r = 0; r < R && has_round(r); ++r) {
+            const uint4 again = load_round(r);
 #pragma unroll
-        for (int r = 0; r < R; ++r)
-            for (int e = 0; has_round(r) && e < N; ++e) {
-                const float x = C::get(raw[r], e);
-                sum += x < most_x ? 0.0f : x == most_x && x < INFINITY ? 1.0f : NAN;
-            }
+            for (int e = 0; e < N; ++e) sum += term(C::get(again, e));
+        }
     }
     const double total = wave_sum_double((double)sum);
-    if (lane_id() == 0) s_sum[wave] = total;
+    if (lane == 0) s_sum[wave] = total;
     __syncthreads();
-    // the few chunks that reach the bar go through LDS: there a thread looks at one chunk's elements, here it would look at all of its own
-    const float bar = s_bar ? float_from_ord(s_bar) : -INFINITY;
+    // the few chunks that reach the bar go through LDS, where all threads share their elements out
+    const float bar = s_bar ? float_from_ord(s_bar) : -3.402823466e38f;     // (-inf and NaN reach no bar)
     int hits = 0;
 #pragma unroll
-    for (int r = 0; r < R; ++r) hits += most_of[r] >= bar && most_of[r] > -INFINITY;
+    for (int r = 0; r < R; ++r) hits += (int)__popcll(__ballot(most_of[r] >= bar));
     if (hits) {
-        int at = atomicAdd(&s_queued, hits);
+        int at = places_for_wave(hits, &s_queued);
 #pragma unroll
-        for (int r = 0; r < R; ++r)
-            if (most_of[r] >= bar && most_of[r] > -INFINITY) {
-                if (at < kSelectQueue) {
-                    s_queue[at] = raw[r];
-                    s_queue_chunk[at] = c0 + t + r * T;
-                }
-                ++at;
+        for (int r = 0; r < R; ++r) {
+            const u64 in = __ballot(most_of[r] >= bar);
+            const int mine = place_of_lane(in, at);
+            if (most_of[r] >= bar && mine < kSelectQueue) {
+                s_queue[mine] = raw[r];
+                s_queue_chunk[mine] = wave_chunk(r) + lane;
             }
+            at += (int)__popcll(in);
+        }
     }
+    auto put = [&](bool wanted, float x, int at) {
+        const u64 in = __ballot(wanted);
+        if (!in) return;
+        const int mine = place_of_lane(in, places_for_wave((int)__popcll(in), &s_count));
+        if (wanted && mine < kSelectKeys) s_keys[mine] = make_key(x, (uint32_t)at);
+    };
+    if (wave == 0) put(edge >= bar, edge, edge_at);
     __syncthreads();
     const int queued = s_queued;
-    if (queued <= kSelectQueue && t < queued) {
-        const uint4 q = s_queue[t];
-        const int v0 = s_queue_chunk[t] * N - shift;
-        int n = 0;
-#pragma unroll
-        for (int e = 0; e < N; ++e) n += C::get(q, e) >= bar && C::get(q, e) > -INFINITY;
-        int at = atomicAdd(&s_count, n);
-#pragma unroll
-        for (int e = 0; e < N; ++e) {
-            const float x = C::get(q, e);
-            if (x >= bar && x > -INFINITY) {
-                if (at < kSelectKeys) s_keys[at] = make_key(x, (uint32_t)(v0 + e));
-                ++at;
-            }
+    if (queued <= kSelectQueue) {
+        typedef elem_t __attribute__((may_alias)) elem_of_chunk;
+        const elem_of_chunk *elems = reinterpret_cast<const elem_of_chunk *>(s_queue);
+        for (int i0 = wave * kWave; i0 < queued * N; i0 += T) {
+            const int i = i0 + lane;
+            const bool is = i < queued * N;
+            const float x = is ? C::value(elems[i]) : -INFINITY;
+            put(x >= bar, x, is ? s_queue_chunk[i / N] * N - shift + i % N : 0);
         }
     }
     __syncthreads();
@@ -302,7 +328,7 @@ __global__ __launch_bounds__(kSelectThreads, 8) void dba_select_part_kernel(cons
             constexpr int J = kSelectKeys / kWave;
             u64 key[J];
 #pragma unroll
-            for (int j = 0; j < J; ++j) key[j] = j * kWave + lane_id() < count ? s_keys[j * kWave + lane_id()] : 0;
+            for (int j = 0; j < J; ++j) key[j] = j * kWave + lane < count ? s_keys[j * kWave + lane] : 0;
             u64 lo = 1, hi = ~0ull;
             int n = count;
             while (n > p.cap && lo < hi) {
@@ -321,24 +347,24 @@ __global__ __launch_bounds__(kSelectThreads, 8) void dba_select_part_kernel(cons
 #pragma unroll
             for (int j = 0; j < J; ++j) {
                 const u64 in = __ballot(key[j] >= lo && key[j]);
-                if ((in >> lane_id()) & 1) out_keys[at + (int)__popcll(in & ((1ull << lane_id()) - 1))] = key[j];
+                if ((in >> lane) & 1) out_keys[place_of_lane(in, at)] = key[j];
                 at += (int)__popcll(in);
             }
-            if (lane_id() == 0) s_int[0] = at;         // (not s_count: other waves may not have read it yet)
+            if (lane == 0) s_int[0] = at;              // (not s_count: other waves may not have read it yet)
         }
         __syncthreads();
         count = s_int[0];
     } else if (count > p.cap || queued > kSelectQueue) {
         // a great many equal logits: exactly k_out, by bisection on the keys
         auto each = [&](auto f) {
+            if (edge >= bar) f(make_key(edge, (uint32_t)edge_at));
 #pragma unroll 1
-            for (int r = 0; r < R; ++r) {
-                const int c = c0 + t + r * T;
-                const uint4 again = chunk_at(c);
+            for (int r = 0; r < R && has_round(r); ++r) {
+                const uint4 again = load_round(r);
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
                     const float x = C::get(again, e);
-                    if (x >= bar && x > -INFINITY) f(make_key(x, (uint32_t)(c * N - shift + e)));
+                    if (x >= bar) f(make_key(x, (uint32_t)((wave_chunk(r) + lane) * N - shift + e)));
                 }
             }
         };
@@ -457,20 +483,25 @@ __global__ __launch_bounds__(T) void dba_select_sentence_kernel(SelectParams p)
         return s == s ? ord_from_float((float)s) : 0u;
     };
     // The k_out-th greatest of the lists' best scores is reached by k_out extensions: lists whose best does not reach it are not looked at.
-    auto kth = [&](uint32_t mine) {
+    auto kth = [&](uint32_t mine, int n) {         // n: threads from there on have nothing
         s_max[t] = mine;
         __syncthreads();
-        uint32_t r[NW];
+        auto of = [&](auto &r) {
+            uint32_t most = 0;
+            constexpr int J = sizeof(r) / sizeof(r[0]);
 #pragma unroll
-        for (int j = 0; j < NW; ++j) r[j] = s_max[j * kWave + lane_id()];
-        uint32_t most = 0;
-#pragma unroll
-        for (int j = 0; j < NW; ++j) most = max(most, r[j]);
-        return bound_of_kth<NW>(r, p.k_out, wave_max_uniform(most));
+            for (int j = 0; j < J; ++j) {
+                r[j] = s_max[j * kWave + lane_id()];
+                most = max(most, r[j]);
+            }
+            return bound_of_kth<J>(r, p.k_out, wave_max_uniform(most));
+        };
+        uint32_t r4[4], r[NW];
+        return NW == 4 || n <= 4 * kWave ? of(r4) : of(r);
     };
     uint32_t top = 0;
     for (int i = t; i < lists; i += T) top = max(top, best_of(i));
-    uint32_t bar = kth(top);
+    uint32_t bar = kth(top, lists);
     for (int i = t; i < lists; i += T) {
         const uint32_t best = best_of(i);
         if (best && best >= bar) {
@@ -480,15 +511,16 @@ __global__ __launch_bounds__(T) void dba_select_sentence_kernel(SelectParams p)
     }
     __syncthreads();
     const int active = s_lists;
-    // every extension of the lists that count: f(score, coordinate)
-    auto each = [&](auto f) {
-        // 64 keys a wave at a time, eight such loads under way
+    // every extension of the lists that count: f(score, coordinate); 64 keys a wave at a time, U such loads under way (the first time
+    // eight; where a sentence needs more looks, one, as the code of this kernel comes through the instruction cache in every launch)
+    auto each_by = [&](auto under_way, auto f) {
+        constexpr int U = decltype(under_way)::value;
         const int pieces = (p.cap + kWave - 1) / kWave, n = (active <= kSelectLists ? active : lists) * pieces;
-        for (int i0 = wave; i0 < n; i0 += 8 * NW) {
-            u64 key[8];
-            int row[8];
+        for (int i0 = wave; i0 < n; i0 += U * NW) {
+            u64 key[U];
+            int row[U];
 #pragma unroll
-            for (int x = 0; x < 8; ++x) {
+            for (int x = 0; x < U; ++x) {
                 const int i = i0 + x * NW, piece = pieces == 2 ? i & 1 : 0;
                 key[x] = 0;
                 row[x] = 0;
@@ -499,12 +531,13 @@ __global__ __launch_bounds__(T) void dba_select_sentence_kernel(SelectParams p)
                 if (j < part_of(list).count) key[x] = keys[(size_t)list * p.cap + j];
             }
 #pragma unroll
-            for (int x = 0; x < 8; ++x) {
+            for (int x = 0; x < U; ++x) {
                 const double s = score_of(row[x], float_from_ord((uint32_t)(key[x] >> 32)));
                 if (key[x] && s == s) f(s, (uint32_t)row[x] * (uint32_t)p.V + key_flat(key[x]));
             }
         }
     };
+    auto each = [&](auto f) { each_by(std::integral_constant<int, 1>{}, f); };
     auto put = [&](u64 ord, uint32_t flat, int from) {
         const int at = atomicAdd(&s_count, 1);
         if (at < kSelectFinal) {
@@ -512,7 +545,7 @@ __global__ __launch_bounds__(T) void dba_select_sentence_kernel(SelectParams p)
             s_flat[from + at] = flat;
         }
     };
-    each([&](double s, uint32_t flat) {
+    each_by(std::integral_constant<int, 8>{}, [&](double s, uint32_t flat) {
         if (ord_from_float((float)s) >= bar) put(ord_from_double(s), flat, 0);
     });
     __syncthreads();
@@ -521,7 +554,7 @@ __global__ __launch_bounds__(T) void dba_select_sentence_kernel(SelectParams p)
         // hardly more lists than slots: a better bound, from the threads' greatest
         top = 0;
         each([&](double s, uint32_t) { top = max(top, ord_from_float((float)s)); });
-        bar = max(bar, kth(top));
+        bar = max(bar, kth(top, T));
         if (t == 0) s_count = 0;
         __syncthreads();
         each([&](double s, uint32_t flat) {
@@ -566,7 +599,7 @@ __global__ __launch_bounds__(T) void dba_select_sentence_kernel(SelectParams p)
         // fewer to rank: those that reach the k_out-th greatest of the threads' maxima
         top = 0;
         for (int i = t; i < count; i += T) top = max(top, (uint32_t)(s_ord[i] >> 32));
-        bar = kth(top);
+        bar = kth(top, count);
         if (t == 0) s_count = 0;
         __syncthreads();
         for (int i = t; i < count; i += T)

@@ -160,7 +160,7 @@ size_t attend_rows_of(int B, int n, int q_heads, const AttendPlan &a) { return (
 template <int FMT>
 hipError_t select_launch(const SelectParams &p, int B, const void *logits, hipStream_t stream)
 {
-    hipError_t e = launch(dba_select_part_kernel<FMT>, dim3((unsigned)(p.nparts * p.k_in), (unsigned)B), dim3(kSelectThreads), 0, stream, logits, p);
+    hipError_t e = launch(dba_select_part_kernel<FMT>, dim3((unsigned)p.nparts, (unsigned)p.k_in, (unsigned)B), dim3(kSelectThreads), 0, stream, logits, p);
     if (e != hipSuccess) return e;
     return p.k_in * p.nparts <= 32 ? launch(dba_select_sentence_kernel<256>, dim3((unsigned)B), dim3(256), 0, stream, p)
                                              : launch(dba_select_sentence_kernel<1024>, dim3((unsigned)B), dim3(1024), 0, stream, p);
