@@ -2,7 +2,7 @@
 //
 // For one sentence and one head of the cache, the queries that read it are rows: row r is node r / G, query head r % G of the
 // G that share the head.  With x = scale log2 e (q . k), a row's output is sum 2^(x_t - m) v_t / sum 2^(x_t - m) over the tokens it
-// sees, m being the running maximum (less a constant in fp16); parts of the token axis are joined by their maxima and sums.
+// sees, m being about the running maximum; parts of the token axis are joined by their m and sums.
 //
 // Both products run on the matrix units, transposed: S^T = K Q^T leaves lane (g, c) of a wave (c = lane % 16, g = lane / 16) with
 // four consecutive tokens 4g .. 4g+3 of row c, which is what the second product O^T = V^T P^T takes as its right operand: the
@@ -52,9 +52,11 @@ typedef short i16x4 __attribute__((ext_vector_type(4)));
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2f = 0.69314718055994530942f;
 
-// A row's greatest weight is 2^kWeightBits, and m its score less that: where weights are rounded to fp16, whose exponents end at 2^-14 (and
-// steps at 2^-24), a long tail of small ones would be lost from the product and not from the sum.
-template <int FMT> constexpr float kWeightBits = FMT == 1 ? 14.0f : 0.0f;
+// A row's weights are 2^(x - m) with m kept kWeightBits below the maximum that it was set by, and set anew where a tile's maximum passes that
+// by more than kWeightRoom (which few tiles do; by any amount every third tile did, at 64 multiplications for two rows of 128).  fp16, whose
+// exponents end at 2^-14 and 2^15, has its weights near the upper end, or a long tail of small ones would be lost from the product and not from the sum.
+template <int FMT> constexpr float kWeightBits = FMT == 1 ? 12.0f : 0.0f;
+template <int FMT> constexpr float kWeightRoom = FMT == 1 ? 3.5f : 8.0f;
 
 // Eight elements of a row along the contraction: 16 bytes, or 32 in fp32.
 template <int FMT> struct Frag {
@@ -116,11 +118,25 @@ __device__ __forceinline__ bool make_finite(u32x4 &c)
     return found;
 }
 
+// Over a wave, without a trip through LDS.
+template <int J> __device__ __forceinline__ float xor_lane_float(float v) { return __uint_as_float(xor_lane_u32<J, true>(__float_as_uint(v))); }
 __device__ __forceinline__ float wave_max_float(float v)
 {
-#pragma unroll
-    for (int d = 32; d; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
-    return v;
+    v = fmaxf(v, xor_lane_float<1>(v));
+    v = fmaxf(v, xor_lane_float<2>(v));
+    v = fmaxf(v, xor_lane_float<4>(v));
+    v = fmaxf(v, xor_lane_float<8>(v));
+    v = fmaxf(v, xor_lane_float<16>(v));
+    return fmaxf(v, xor_lane_float<32>(v));
+}
+__device__ __forceinline__ float wave_sum_float(float v)
+{
+    v += xor_lane_float<1>(v);
+    v += xor_lane_float<2>(v);
+    v += xor_lane_float<4>(v);
+    v += xor_lane_float<8>(v);
+    v += xor_lane_float<16>(v);
+    return v + xor_lane_float<32>(v);
 }
 
 // Over the four lanes of a row, without a trip through LDS.
@@ -401,7 +417,7 @@ __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) vo
 #pragma unroll
                 for (int i = 0; i < 4; ++i) top = fmaxf(top, s[t][j][i]);
             top = fmaf(max_over_groups(top), sl2, -kWeightBits<FMT>);
-            if (__any(top > m[j])) {                   // (a maximum stays as it is in most tiles)
+            if (__any(top > m[j] + kWeightRoom<FMT>)) {
                 const float m1 = fmaxf(m[j], top);
                 const float keep = m1 == m[j] ? 1.0f : __builtin_amdgcn_exp2f(m[j] - m1);
                 m[j] = m1;
@@ -570,66 +586,94 @@ __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) vo
     }
 }
 
-// Joins the parts of a row, a wave a row: its lanes take a part's four elements each, and as many parts at a time as there are lanes for.
-// Rows with one part have been written already.
-template <int FMT>
-__global__ __launch_bounds__(256) void dba_attend_join_kernel(AttendParams p, int tile)
+// Joins the parts of a row: 2^(m_s - m) O_s and 2^(m_s - m) l_s added up over its parts s.  Of a part, a lane takes four elements, and as many parts
+// are taken at a time as there are lanes for.  A wave has Q rows of one row tile: where there are a great many rows, what is done once a wave
+// (addresses, divisions) is what the VALU's time goes to (16000 rows of 128 in two parts: JOIN_TIME); with few, the chain of loads
+// counts, and a row a wave is best (1024 rows in 16 parts: 6.9 against 12 us).  Rows with one part have been written already.
+template <int FMT, int Q>
+__global__ __launch_bounds__(256) void dba_attend_join_kernel(AttendParams p, int tile, int tile_shift)
 {
     typedef typename Elem<FMT>::type E;
     const int lane = (int)threadIdx.x & 63, b = (int)blockIdx.z, head = (int)blockIdx.y;
-    const int G = p.q_heads / p.heads, rows = p.n * G, r = (int)blockIdx.x * 4 + ((int)threadIdx.x >> 6);
-    if (r >= rows) return;
+    const int G = p.q_heads / p.heads, rows = p.n * G;
+    const int r0 = ((int)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6)) * Q;
+    if (r0 >= rows) return;
     int tree_all;
-    const Span span = span_of_rows(p, b, r / p.tile_rows, G, tree_all);
+    const Span span = span_of_rows(p, b, r0 >> tile_shift, G, tree_all);
     const int tiles = (span.prefix + tile - 1) / tile + (span.end - span.prefix + tile - 1) / tile;
     if (tiles <= p.chunk) return;
     const int parts = (tiles + p.chunk - 1) / p.chunk;
-    const size_t part = ((size_t)b * p.heads + head) * p.splits * rows + r;
-    const int across = p.D <= 32 ? 8 : p.D <= 64 ? 16 : p.D <= 128 ? 32 : 64, d = lane % across * 4;     // lanes of a part
-    float top = -INFINITY, sum = 0.0f;
-    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+    const size_t part = ((size_t)b * p.heads + head) * p.splits * rows + r0;
+    const int across = p.D <= 32 ? 8 : p.D <= 64 ? 16 : p.D <= 128 ? 32 : 64, side = 64 / across;   // lanes of a part, parts side by side
+    const int d = lane % across * 4;
+    float top[Q], sum[Q];
+    f32x4 v[Q];
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+        top[q] = -INFINITY;
+        sum[q] = 0.0f;
+        v[q] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
     for (int s0 = 0; s0 < parts; s0 += 64) {
         const int n = min(64, parts - s0);
-        float ms = -INFINITY, ls = 0.0f;
-        if (lane < n) {
-            const size_t at = part + (size_t)(s0 + lane) * rows;
-            ms = p.part_ml[at * 2];
-            ls = p.part_ml[at * 2 + 1];
+        float w[Q];
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+            float ms = -INFINITY, ls = 0.0f;
+            if (lane < n && r0 + q < rows) {
+                const float2 ml = *reinterpret_cast<const float2 *>(p.part_ml + (part + (size_t)(s0 + lane) * rows + q) * 2);
+                ms = ml.x;
+                ls = ml.y;
+            }
+            const float top1 = fmaxf(top[q], wave_max_float(ms));
+            const float keep = top[q] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(top[q] - top1);
+            w[q] = ls == 0.0f ? 0.0f : ms == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ms - top1);
+            top[q] = top1;
+            sum[q] = sum[q] * keep + wave_sum_float(ls * w[q]);
+            v[q] *= keep;
         }
-        const float top1 = fmaxf(top, wave_max_float(ms));
-        const float keep = top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(top - top1);
-        const float w = ls == 0.0f ? 0.0f : ms == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ms - top1);
-        float more = ls * w;
+        constexpr int U = 4 / Q > 0 ? 4 / Q : 1;       // parts of a row that a lane has under way
+        for (int s1 = 0; s1 < n; s1 += U * side) {
+            f32x4 y[Q][U];
 #pragma unroll
-        for (int x = 32; x; x >>= 1) more += __shfl_xor(more, x);
-        top = top1;
-        sum = sum * keep + more;
-        v *= keep;
-        for (int s1 = 0; s1 < n; s1 += 4 * (64 / across)) {
-            f32x4 y[4];
-            float f[4];
+            for (int x = 0; x < U; ++x) {
+                const int s = s1 + x * side + lane / across;
+                const float *at = p.part_o + (part + (size_t)(s0 + s) * rows) * p.D + d;
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                const int s = s1 + x * (64 / across) + lane / across;
-                f[x] = __shfl(w, s & 63);
-                y[x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-                if (s < n && d < p.D) y[x] = *reinterpret_cast<const f32x4 *>(p.part_o + (part + (size_t)(s0 + s) * rows) * p.D + d);
-                else f[x] = 0.0f;
+                for (int q = 0; q < Q; ++q) {
+                    y[q][x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                    if (s < n && d < p.D && r0 + q < rows) y[q][x] = *reinterpret_cast<const f32x4 *>(at + q * p.D);
+                }
             }
 #pragma unroll
-            for (int x = 0; x < 4; ++x) v += y[x] * f[x];
+            for (int x = 0; x < U; ++x) {
+                const int s = s1 + x * side + lane / across;
+#pragma unroll
+                for (int q = 0; q < Q; ++q) {
+                    const float f = __shfl(w[q], s & 63);
+                    v[q] += y[q][x] * (s < n && d < p.D ? f : 0.0f);
+                }
+            }
         }
     }
-    for (int x = across; x < 64; x *= 2)
+    int node = r0 / G, h = r0 - node * G;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] += __shfl_xor(v[i], x);
-    const int64_t row = ((int64_t)b * p.n + r / G) * p.q_heads + head * G + r % G;
-    if (lane == 0 && p.lse) p.lse[row] = sum != 0.0f ? (top + __builtin_amdgcn_logf(sum)) * kLn2f : -INFINITY;
-    if (lane < across && d < p.D) {
-        v *= sum != 0.0f ? 1.0f / sum : 0.0f;
-        E *to = reinterpret_cast<E *>(p.out.data) + ((int64_t)b * p.out.sent + (int64_t)(r / G) * p.out.token + (int64_t)(head * G + r % G) * p.out.head + d);
-        if constexpr (FMT == 0) *reinterpret_cast<f32x4 *>(to) = v;
-        else *reinterpret_cast<uint2 *>(to) = make_uint2(pack2<FMT>(v[0], v[1]), pack2<FMT>(v[2], v[3]));
+    for (int q = 0; q < Q; ++q) {
+        if (r0 + q >= rows) return;
+        for (int x = across; x < 64; x *= 2)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[q][i] += __shfl_xor(v[q][i], x);
+        if (lane == 0 && p.lse) p.lse[((int64_t)b * p.n + node) * p.q_heads + head * G + h] = sum[q] != 0.0f ? (top[q] + __builtin_amdgcn_logf(sum[q])) * kLn2f : -INFINITY;
+        if (lane < across && d < p.D) {
+            v[q] *= sum[q] != 0.0f ? 1.0f / sum[q] : 0.0f;
+            E *to = reinterpret_cast<E *>(p.out.data) + ((int64_t)b * p.out.sent + (int64_t)node * p.out.token + (int64_t)(head * G + h) * p.out.head + d);
+            if constexpr (FMT == 0) *reinterpret_cast<f32x4 *>(to) = v[q];
+            else *reinterpret_cast<uint2 *>(to) = make_uint2(pack2<FMT>(v[q][0], v[q][1]), pack2<FMT>(v[q][2], v[q][3]));
+        }
+        if (++h == G) {
+            h = 0;
+            ++node;
+        }
     }
 }
 

@@ -36,7 +36,9 @@ hipError_t attend_launch(const AttendParams &p, const AttendPlan &plan, int B, h
     const hipError_t e = plan.DP == 64 ? attend_rows<FMT, 64>(p, plan, B, stream)
                  : plan.DP == 128 ? attend_rows<FMT, 128>(p, plan, B, stream) : attend_rows<FMT, 256>(p, plan, B, stream);
     if (e != hipSuccess || p.splits == 1) return e;
-    return launch(dba_attend_join_kernel<FMT>, dim3((unsigned)((p.n * (p.q_heads / p.heads) + 3) / 4), (unsigned)p.heads, (unsigned)B), dim3(256), 0, stream, p, plan.tile);
+    const int rows = p.n * (p.q_heads / p.heads), Q = (int64_t)B * p.heads * rows >= 16384 ? 4 : 1;
+    return launch(Q == 4 ? dba_attend_join_kernel<FMT, 4> : dba_attend_join_kernel<FMT, 1>, dim3((unsigned)((rows + 4 * Q - 1) / (4 * Q)), (unsigned)p.heads, (unsigned)B),
+                  dim3(256), 0, stream, p, plan.tile, __builtin_ctz((unsigned)plan.tile_rows));
 }
 
 }  // namespace dba
