@@ -116,7 +116,9 @@ HeadsAt heads_of(const dba_heads *h)
 // (504 rows of 128: 145 us against 246 with row tiles of 64 that each read the tokens; 40 to 48 rows of 128: 175 and 197 us against
 // 182 and 184 with shared tiles).  The token axis is cut into as many parts as fill the GPU once: each part costs a start-up of several
 // trips to memory, and twice as many were slower (one sentence of 29000 tokens 59 against 43 us, five of 21600 56 against 39),
-// but for shared tiles, whose sentences' lengths matter more than that.
+// but for shared tiles, whose sentences' lengths matter more than that.  There the first part of a sentence has a quarter more than an even share, so that
+// fewer sentences have rows to join and what comes last is short (32 sentences of 500 to 4000 tokens, 63 nodes of 32 heads: 127 us; even parts
+// 144, half as much again 135, one part a sentence 147, three 153).
 AttendPlan attend_plan(int B, int n, int q_heads, const dba_cache &c, int max_len)
 {
     AttendPlan a;
@@ -134,7 +136,8 @@ AttendPlan attend_plan(int B, int n, int q_heads, const dba_cache &c, int max_le
     const int64_t groups = (int64_t)B * c.heads * a.row_tiles;
     const int resident = a.DP == 256 || (a.DP == 128 && (a.QT == 4 || (f32 && a.QT == 2))) ? 256 : 512;
     const int64_t parts = std::max<int64_t>(1, resident * (a.shared ? 2 : 1) / groups);
-    const int64_t chunk = std::max<int64_t>(4, ((tiles + parts - 1) / parts + 3) / 4 * 4);         // a tile a wave at least
+    const int64_t even = (tiles + parts - 1) / parts;
+    const int64_t chunk = a.shared ? even * 5 / 4 : std::max<int64_t>(4, (even + 3) / 4 * 4);       // a tile a wave at least
     a.chunk = (int)chunk;
     a.splits = (int)((tiles + chunk - 1) / chunk);
     return a;
