@@ -25,6 +25,12 @@ constexpr size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 constexpr int kMostRows = 1 << 22;          // tokens, or heads of tokens, of one sentence in a call
 constexpr int kMostLength = INT32_MAX - 1023;   // tokens that attention looks at: positions of the tiles behind them are ints, too
 
+bool overlaps(const void *a, size_t a_bytes, const void *b, size_t b_bytes)
+{
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return x < y + b_bytes && y < x + a_bytes;
+}
+
 int launched(const char *who, hipError_t e)
 {
     return e == hipSuccess ? DBA_OK : set_error(DBA_EHIP, "%s: launch failed: %s", who, hipGetErrorString(e));
@@ -199,6 +205,11 @@ DBA_API int dba_beam_select(int B, int k_in, int k_out, int V, int eos_id, int p
         return set_error(DBA_EINVAL, "dba_beam_select: workspace_dev must be 256-byte aligned");
     if (workspace_bytes < plan.total)
         return set_error(DBA_ENOMEM, "dba_beam_select: workspace has %zu bytes, %zu needed", workspace_bytes, plan.total);
+    const size_t rows_in = (size_t)B * k_in, rows_out = (size_t)B * k_out;
+    const struct { const void *at; size_t bytes; } outs[] = {{out_token_dev, rows_out * 4}, {out_backptr_dev, rows_out * 4}, {out_score_dev, rows_out * 4}, {out_flags_dev, rows_out}};
+    for (const auto &o : outs)
+        if (overlaps(o.at, o.bytes, score_dev, rows_in * 4) || (flags_dev && overlaps(o.at, o.bytes, flags_dev, rows_in)))
+            return set_error(DBA_EINVAL, "dba_beam_select: the new beam lies in the old one's scores or flags");
     SelectParams p;
     p.score = score_dev;
     p.flags = flags_dev;

@@ -62,6 +62,13 @@ def test_select_refuses(kw, frag):
     _refused(_select(**kw), frag)
 
 
+@pytest.mark.parametrize("kw", [dict(osc=AT), dict(tok=AT + 28), dict(back=AT - 28), dict(ofl=AT + 4099), dict(ofl=AT + 31)])
+def test_select_refuses_a_new_beam_in_the_old_one(kw):
+    """2 x 4 scores from AT, flags 4096 behind; everything else lies apart."""
+    apart = dict(tok=AT + (1 << 13), back=AT + (2 << 13), osc=AT + (3 << 13), ofl=AT + (4 << 13), score=AT, flags=AT + 4096, logits=AT + (5 << 13), ws=AT + (6 << 13))
+    _refused(_select(**{**apart, **kw}), "old one")
+
+
 def test_select_workspace():
     size = beam.load().dba_beam_select_workspace_bytes
     assert 0 < size(1, 5, 5, 1000, 0) < 1 << 20
