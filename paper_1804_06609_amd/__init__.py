@@ -2,7 +2,8 @@
 
 The product is libdba.so (HIP, gfx950) declared in include/dba.h; this package
 is its ctypes binding.  PyTorch is used by callers only to own device memory
-and streams.
+and streams.  The operators next to the step (include/dba_beam.h) are in the
+module `beam`, on torch tensors.
 """
 from .binding import (DBA_EHIP, DBA_EINVAL, DBA_ENOMEM, DBA_ESTATE, DBA_FLAG_DEAD,  # noqa: F401
                       DBA_FLAG_FINISHED, DBA_LOGP_BF16, DBA_LOGP_F16, DBA_LOGP_F32, DBA_MAX_BEAM,

@@ -4,7 +4,7 @@
 cache, rotated on the way) and `attend` (a tree's nodes over that cache).  All enqueue their work on the current stream of
 the current device, where their tensors have to be, and return without waiting; workspaces come from torch's allocator on that
 stream.  A tensor that was made on another stream is the caller's to wait for, as with any torch operator.
-Nothing of the methods runs here, and there is no fallback: without the built library the calls raise.
+Nothing of the methods runs here, and there is no fallback: without the built library the calls raise.  None has a gradient.
 """
 from __future__ import annotations
 

@@ -168,7 +168,7 @@ __device__ __forceinline__ uint32_t bound_of_kth(const uint32_t (&r)[J], int k, 
 // One part of one row.  Bound: HBM (the logits are read once); with 16 bits the VALU is about as busy: an element takes five
 // instructions, one of them the exponential.  So nothing else is done element by element: addresses are the same for a whole wave
 // but for its lanes' 16 bytes, edges of a row that do not fill a chunk are single elements of the first wave, and of the chunks only those that
-// reach the bar are looked through (128 x 64 rows of 50000 in bf16: SELECT_TIME).
+// reach the bar are looked through (128 x 64 rows of 50000 in bf16: 158 us, 5.2 TB/s; 64 x 20 of 32000 in fp32: 24.6 us, 6.7 TB/s).
 template <int FMT>
 __global__ __launch_bounds__(kSelectThreads, 8) void dba_select_part_kernel(const void *logits, SelectParams p)
 {
@@ -411,7 +411,8 @@ __device__ __forceinline__ double double_from_ord(u64 o)
     return __longlong_as_double((long long)((o >> 63) ? (o & 0x7FFFFFFFFFFFFFFFull) : ~o));
 }
 
-// One sentence: normalisers, then the k_out best of what its rows' parts have handed on.  Bound: latency (a chain of loads and barriers).
+// One sentence: normalisers, then the k_out best of what its rows' parts have handed on.  Bound: latency, a chain of loads and barriers through
+// code that no other launch has left in the instruction cache (5 us for 5 lists, 9.4 for 80, 18 for 256 with k_out = 64).
 template <int T>
 __global__ __launch_bounds__(T) void dba_select_sentence_kernel(SelectParams p)
 {

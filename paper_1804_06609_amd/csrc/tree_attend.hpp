@@ -188,6 +188,11 @@ struct AttendShape {
     }
 };
 
+// Bound: without ROWS memory; each token is read once.  A pool with the heads of a token side by side gives 128 or 256 bytes at a time (64 sentences of
+// 20 branches, heads of 64: 78 us, 4.1 TB/s; 4 of 57000 tokens, heads of 128: 188 us, 5.0 TB/s), one with a head's tokens side by side
+// more (68 and 172 us).  With ROWS the issue slots: a tile of 64 tokens and 32 rows of 128 takes a wave 64 matrix instructions
+// and 350 others (32 sentences of 500 to 4000 tokens, 63 nodes of 32 heads: 122 us, 0.6 PFLOP/s of fp16).
+//
 // Workgroups come to the eight XCDs in turn.  The row tiles of one part of one head, which read the same tokens, are put behind each
 // other on one XCD, whose L2 then serves all but the first (63 nodes, 8 query heads to one, 32 sentences of 500 to 4000 tokens:
 // 225 -> 140 us).  There the parts of the token axis vary slowest, so that what is left of short sentences comes last; where
@@ -588,7 +593,7 @@ __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) vo
 
 // Joins the parts of a row: 2^(m_s - m) O_s and 2^(m_s - m) l_s added up over its parts s.  Of a part, a lane takes four elements, and as many parts
 // are taken at a time as there are lanes for.  A wave has Q rows of one row tile: where there are a great many rows, what is done once a wave
-// (addresses, divisions) is what the VALU's time goes to (16000 rows of 128 in two parts: JOIN_TIME); with few, the chain of loads
+// (addresses, divisions) is what the VALU's time goes to (64500 rows of 128, half of them in two parts: 25 us with a row a wave, 15 with four); with few, the chain of loads
 // counts, and a row a wave is best (1024 rows in 16 parts: 6.9 against 12 us).  Rows with one part have been written already.
 template <int FMT, int Q>
 __global__ __launch_bounds__(256) void dba_attend_join_kernel(AttendParams p, int tile, int tile_shift)
