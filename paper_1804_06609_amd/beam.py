@@ -45,6 +45,14 @@ _SIGNATURES = {
 # the same structures as bytes, which are made in half the time
 _pack_cache = struct.Struct("@3P4q6i").pack
 _pack_heads = struct.Struct("@P3q").pack
+
+
+@functools.lru_cache(maxsize=256)
+def _pack_states(fields: int):
+    return struct.Struct(f"@{fields}q").pack
+
+
+_F32, _I32, _U8, _empty_like, _CONTIGUOUS = torch.float32, torch.int32, torch.uint8, torch.empty_like, torch.contiguous_format
 _FORMATS = {torch.float32: _b.DBA_LOGP_F32, torch.float16: _b.DBA_LOGP_F16, torch.bfloat16: _b.DBA_LOGP_BF16}
 
 _lib = None
@@ -80,7 +88,7 @@ def _ints(name: str, x: Optional[torch.Tensor], shape, device: int) -> Optional[
     """Address of a dense int32 tensor of this shape (None where it may be left out)."""
     if x is None:
         return None
-    if x.dtype is not torch.int32 or x.shape != shape or x.get_device() != device or not x.is_contiguous():
+    if x.dtype is not _I32 or x.shape != shape or x.get_device() != device or not x.is_contiguous():
         _fail(f"{name} must be a contiguous int32 tensor {tuple(shape)} on the device of the others")
     return x.data_ptr()
 
@@ -89,7 +97,7 @@ def _workspace(nbytes: int, like: torch.Tensor):
     """(tensor, address): torch's allocations start on 512 bytes."""
     if not nbytes:
         return None, None
-    ws = like.new_empty(nbytes, dtype=torch.uint8)
+    ws = like.new_empty(nbytes, dtype=_U8)
     return ws, ws.data_ptr()
 
 
@@ -98,25 +106,28 @@ def select(logits: torch.Tensor, score: torch.Tensor, flags: Optional[torch.Tens
     """The new beam from logits [B, k_in, V] (fp32, fp16 or bf16; last axis dense), score [B, k_in] fp32 and flags [B, k_in] uint8 or
     None: (token, backptr, score, flags), each [B, k_out] as dba_step writes them.  `out`: four tensors to write to."""
     lib = load()
-    if logits.dim() != 3 or logits.dtype not in _FORMATS or (logits.shape[2] > 1 and logits.stride(2) != 1):
+    shape, fmt = logits.shape, _FORMATS.get(logits.dtype)
+    if len(shape) != 3 or fmt is None:
         _fail("logits must be [B, k, V] of fp32, fp16 or bf16 with a dense last axis")
-    B, k, V = logits.shape
-    stream, device = _stream(logits), logits.get_device()
-    for name, x, dtype in (("score", score, torch.float32), ("flags", flags, torch.uint8)):
-        if x is not None and (x.dtype is not dtype or x.shape != (B, k) or not x.is_contiguous() or x.get_device() != device):
-            _fail(f"{name} must be a contiguous {dtype} tensor [B, k] on the device of the logits")
+    B, k, V = shape
+    sent, row, one = logits.stride()
+    if one != 1 and V > 1:
+        _fail("logits must be [B, k, V] of fp32, fp16 or bf16 with a dense last axis")
+    stream, device, of_rows = _stream(logits), logits.get_device(), (B, k)
+    if score.dtype is not _F32 or score.shape != of_rows or not score.is_contiguous() or score.get_device() != device:
+        _fail("score must be a contiguous fp32 tensor [B, k] on the device of the logits")
+    if flags is not None and (flags.dtype is not _U8 or flags.shape != of_rows or not flags.is_contiguous() or flags.get_device() != device):
+        _fail("flags must be a contiguous uint8 tensor [B, k] on the device of the logits")
     if out is None:
         like = score if k_out == k else score.new_empty((B, k_out))
-        out = (torch.empty_like(like, dtype=torch.int32), torch.empty_like(like, dtype=torch.int32), torch.empty_like(like),
-               torch.empty_like(like, dtype=torch.uint8))
+        out = (_empty_like(like, dtype=_I32), _empty_like(like, dtype=_I32), _empty_like(like), _empty_like(like, dtype=_U8))
     else:
-        for x, dtype in zip(out, (torch.int32, torch.int32, torch.float32, torch.uint8), strict=True):
+        for x, dtype in zip(out, (_I32, _I32, _F32, _U8), strict=True):
             if x.dtype is not dtype or x.shape != (B, k_out) or not x.is_contiguous() or x.get_device() != device:
                 _fail("out must be four contiguous tensors [B, k_out]: int32, int32, fp32, uint8")
-    fmt = _FORMATS[logits.dtype]
     nbytes = lib.dba_beam_select_workspace_bytes(B, k, k_out, V, fmt)
     ws, at = _workspace(nbytes, logits)
-    _b._check(lib.dba_beam_select(B, k, k_out, V, eos_id, pad_id, logits.data_ptr(), fmt, logits.stride(0), logits.stride(1),
+    _b._check(lib.dba_beam_select(B, k, k_out, V, eos_id, pad_id, logits.data_ptr(), fmt, sent, row,
                                   score.data_ptr(), None if flags is None else flags.data_ptr(), out[0].data_ptr(), out[1].data_ptr(),
                                   out[2].data_ptr(), out[3].data_ptr(), at, nbytes, stream))
     return tuple(out)
@@ -156,14 +167,15 @@ def reorder(backptr: torch.Tensor, states: Sequence[torch.Tensor], out: Optional
     if len(out) != len(states):
         _fail("as many tensors out as states")
     table = []                                         # the fields of dba_state, one state after another
-    rows, head = B * k, backptr.shape
+    rows = B * k or 1
     for s, d in zip(states, out):
         shape = s.shape
-        if shape[:2] != head or d.shape != shape or s.dtype is not d.dtype or s.get_device() != device or d.get_device() != device:
+        if d.shape != shape or len(shape) < 2 or shape[0] != B or shape[1] != k or s.dtype is not d.dtype or s.get_device() != device or d.get_device() != device:
             _fail("states and out must be [B, k, ...] tensors alike in shape and type, on the device of backptr")
         if s.is_contiguous() and d.is_contiguous():
-            row = s.numel() // max(1, rows) * s.element_size()
-            table += (d.data_ptr(), s.data_ptr(), row * k, row, 0, row * k, row, 0, 1, row)
+            row = s.nbytes // rows
+            sent = row * k
+            table += (d.data_ptr(), s.data_ptr(), sent, row, 0, sent, row, 0, 1, row)
             continue
         a, c = _pieces(shape, s.stride(), s.element_size()), _pieces(shape, d.stride(), d.element_size())
         if a is None or c is None:
@@ -174,12 +186,11 @@ def reorder(backptr: torch.Tensor, states: Sequence[torch.Tensor], out: Optional
                 _fail("the axes of a state and its out must fold alike")
             a, c = ((x[0], x[1], piece if x[4] > piece else x[2], x[3] * x[4] // piece, piece) for x in (a, c))
         table += (d.data_ptr(), s.data_ptr(), *c[:3], *a)
-    table = (_L * len(table))(*table)
-    _b._check(lib.dba_beam_reorder(B, k, back, table, len(states), stream))
+    _b._check(lib.dba_beam_reorder(B, k, back, _pack_states(len(table))(*table), len(states), stream))
     return out
 
 
-def _cache(k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor, like: torch.Tensor, device: int) -> bytes:
+def _cache(k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor, B: int, dtype, device: int) -> bytes:
     shape = k_pages.shape
     if len(shape) != 4 or v_pages.shape != shape:
         _fail("k_pages and v_pages must be [pages, page_size, heads, head_dim]")
@@ -189,24 +200,28 @@ def _cache(k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor, li
         s, r = ([st if size > 1 else 0 for st, size in zip(x, shape)] for x in (s, r))
     if s != r or (D > 1 and s[3] != 1):
         _fail("k_pages and v_pages must be laid out alike, with a dense last axis")
-    dtype = k_pages.dtype
-    if dtype not in _FORMATS or v_pages.dtype is not dtype or like.dtype is not dtype:
+    if k_pages.dtype is not dtype or v_pages.dtype is not dtype or dtype not in _FORMATS:
         _fail("keys, values, queries and pages must be of one type: fp32, fp16 or bf16")
-    if table.dtype is not torch.int32 or table.dim() != 2 or table.stride(1) != 1 or table.shape[0] != like.shape[0]:
+    pages_of = table.shape
+    if len(pages_of) != 2 or table.dtype is not torch.int32 or pages_of[0] != B:
+        _fail("table must be an int32 tensor [B, max_pages] with a dense last axis")
+    row, one = table.stride()
+    if one != 1:
         _fail("table must be an int32 tensor [B, max_pages] with a dense last axis")
     if k_pages.get_device() != device or v_pages.get_device() != device or table.get_device() != device:
         _fail("tensors must be on one device")
-    return _pack_cache(k_pages.data_ptr(), v_pages.data_ptr(), table.data_ptr(), table.stride(0), s[0], s[1], s[2],
-                       _FORMATS[dtype], n_pages, page, table.shape[1], heads, D)
+    return _pack_cache(k_pages.data_ptr(), v_pages.data_ptr(), table.data_ptr(), row, s[0], s[1], s[2],
+                       _FORMATS[dtype], n_pages, page, pages_of[1], heads, D)
 
 
 def _heads(name: str, x: torch.Tensor, shape, dtype, device: int) -> bytes:
     if x.shape != shape:
         _fail(f"{name} must be [B, n, heads, head_dim], here {tuple(shape)}")
-    s = x.stride()
-    if x.dtype is not dtype or x.get_device() != device or (s[3] != 1 and shape[3] > 1):
+    sent, token, head, one = x.stride()
+    B, n, heads, D = shape
+    if x.dtype is not dtype or x.get_device() != device or (one != 1 and D > 1):
         _fail(f"{name} must be of the type and on the device of the others, with a dense last axis")
-    return _pack_heads(x.data_ptr(), s[0] if shape[0] > 1 else 0, s[1] if shape[1] > 1 else 0, s[2] if shape[2] > 1 else 0)
+    return _pack_heads(x.data_ptr(), sent if B > 1 else 0, token if n > 1 else 0, head if heads > 1 else 0)
 
 
 def append(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor, first: torch.Tensor,
@@ -221,7 +236,7 @@ def append(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: tor
     if len(shape) != 4:
         _fail("k must be [B, n, heads, head_dim]")
     B, n, heads, D = shape
-    cache = _cache(k_pages, v_pages, table, k, device)
+    cache = _cache(k_pages, v_pages, table, B, dtype, device)
     if k_pages.shape[2:] != (heads, D):
         _fail("k has other heads than the cache")
     qh = oh = None
@@ -231,7 +246,7 @@ def append(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: tor
             _fail("q must be [B, n, q_heads, head_dim]")
         q_heads = q.shape[2]
         if q_out is None:
-            q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+            q_out = _empty_like(q, memory_format=_CONTIGUOUS)
         qh, oh = _heads("q", q, (B, n, q_heads, D), dtype, device), _heads("q_out", q_out, (B, n, q_heads, D), dtype, device)
     rot, freq = 0, None
     if inv_freq is not None:
@@ -257,11 +272,11 @@ def attend(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, table:
     if len(shape) != 4:
         _fail("q must be [B, n, q_heads, head_dim]")
     B, n, heads, D = shape
-    cache = _cache(k_pages, v_pages, table, q, device)
+    cache = _cache(k_pages, v_pages, table, B, dtype, device)
     if k_pages.shape[3] != D:
         _fail("q has another head_dim than the cache")
     if out is None:
-        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        out = _empty_like(q, memory_format=_CONTIGUOUS)
     words, bits = 0, None
     if mask is not None:
         if mask.dtype is not torch.int64 or mask.dim() != 3 or mask.shape[:2] != (B, n) or not mask.is_contiguous() or mask.get_device() != device:
