@@ -125,6 +125,9 @@ HeadsAt heads_of(const dba_heads *h)
 // but for shared tiles, whose sentences' lengths matter more than that.  There the first part of a sentence has a quarter more than an even share, so that
 // fewer sentences have rows to join and what comes last is short (32 sentences of 500 to 4000 tokens, 63 nodes of 32 heads: 127 us; even parts
 // 144, half as much again 135, one part a sentence 147, three 153).
+// Two heads a workgroup (SIDE) halve the workgroups: 1024 heads of 64 in two rounds of 512 or in one 83 and 75 us, of 128 81 and 74, 1024 of 256 in four rounds or
+// two 122 and 116, 2048 of 32 66 and 62; but 1200 of 80, in three rounds or in two of which the second is nearly empty, 75 and 82, and 512 of 128, which then need
+// parts to fill the GPU, 110 and 117.
 AttendPlan attend_plan(int B, int n, int q_heads, const dba_cache &c, int max_len)
 {
     AttendPlan a;
@@ -139,11 +142,15 @@ AttendPlan attend_plan(int B, int n, int q_heads, const dba_cache &c, int max_le
     a.tile = a.shared ? 64
            : a.DP == 64 && a.QT <= 2 ? (f32 ? attend_tile<0, 64, 2> : attend_tile<1, 64, 2>) : f32 ? attend_tile<0, 256, 1> : attend_tile<1, 256, 1>;
     const int tiles = (max_len + a.tile - 1) / a.tile + 1;         // (the prefix and the tree each end in a tile of their own)
-    const int64_t groups = (int64_t)B * c.heads * a.row_tiles;
     const int resident = a.DP == 256 || (a.DP == 128 && (a.QT == 4 || (f32 && a.QT == 2))) ? 256 : 512;
+    // two heads a workgroup where that leaves no more of the last round of workgroups empty
+    const int64_t pairs = (int64_t)B * c.heads;
+    const auto rounds = [&](int64_t n) { return (n + resident - 1) / resident; };
+    a.side = !a.shared && c.heads % 2 == 0 && pairs >= 2 * resident && 2 * rounds(pairs / 2) * 19 <= rounds(pairs) * 20 ? 2 : 1;
+    const int64_t groups = pairs / a.side * a.row_tiles;
     const int64_t parts = std::max<int64_t>(1, resident * (a.shared ? 2 : 1) / groups);
     const int64_t even = (tiles + parts - 1) / parts;
-    const int64_t chunk = a.shared ? even * 5 / 4 : std::max<int64_t>(4, (even + 3) / 4 * 4);       // a tile a wave at least
+    const int64_t chunk = a.shared ? even * 5 / 4 : std::max<int64_t>(4 / a.side, (even + 3) / 4 * 4);
     a.chunk = (int)chunk;
     a.splits = (int)((tiles + chunk - 1) / chunk);
     return a;
@@ -421,7 +428,7 @@ DBA_API int dba_tree_attend(int B, int n, int q_heads, const dba_heads *q, const
     p.tile_rows = plan.tile_rows;
     p.splits = plan.splits;
     p.chunk = plan.chunk;
-    p.pairs = B * cache->heads;
+    p.pairs = B * (cache->heads / plan.side);
     p.groups = p.pairs * plan.splits;
     p.part_o = static_cast<float *>(workspace_dev);
     p.part_ml = reinterpret_cast<float *>(static_cast<unsigned char *>(workspace_dev) + align256(attend_rows_of(B, n, q_heads, plan) * cache->head_dim * 4));

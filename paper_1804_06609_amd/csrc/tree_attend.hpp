@@ -27,7 +27,7 @@ struct AttendParams {
     int n, q_heads, heads, D, mask_words, max_len;
     int row_tiles, tile_rows;          // workgroups along the rows, rows of each
     int splits, chunk;                 // workgroups along the token axis, tiles of each
-    int pairs, groups;                 // sentences times heads; times splits
+    int pairs, groups;                 // sentences times heads, or pairs of them; times splits
     float scale;
 };
 
@@ -189,15 +189,18 @@ struct AttendShape {
 };
 
 // Bound: without ROWS memory; each token is read once.  A pool with the heads of a token side by side gives 128 or 256 bytes at a time (64 sentences of
-// 20 branches, heads of 64: 78 us, 4.1 TB/s; 4 of 57000 tokens, heads of 128: 188 us, 5.0 TB/s), one with a head's tokens side by side
-// more (68 and 172 us).  With ROWS the issue slots: a tile of 64 tokens and 32 rows of 128 takes a wave 64 matrix instructions
+// 20 branches, heads of 64: 72 us, 4.4 TB/s; 4 of 57000 tokens, heads of 128: 188 us, 5.0 TB/s), one with a head's tokens side by side
+// more (68 and 172 us with a head a workgroup).  With ROWS the issue slots: a tile of 64 tokens and 32 rows of 128 takes a wave 64 matrix instructions
 // and 350 others (32 sentences of 500 to 4000 tokens, 63 nodes of 32 heads: 122 us, 0.6 PFLOP/s of fp16).
+//
+// SIDE: heads of a workgroup.  With two, waves 0 and 2 have the first, 1 and 3 the second: a longer stretch of memory where the heads of a token lie
+// side by side, and twice the tiles a wave for the same start and end (83 -> 75 us in the first case above; four heads 106).
 //
 // Workgroups come to the eight XCDs in turn.  The row tiles of one part of one head, which read the same tokens, are put behind each
 // other on one XCD, whose L2 then serves all but the first (63 nodes, 8 query heads to one, 32 sentences of 500 to 4000 tokens:
 // 225 -> 140 us).  There the parts of the token axis vary slowest, so that what is left of short sentences comes last; where
 // tokens are read once they vary fastest (4 sentences of 50000 and more: 186 instead of 199 us).
-template <int FMT, int DP, int QT, bool ROWS>
+template <int FMT, int DP, int QT, bool ROWS, int SIDE>
 __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) void dba_attend_kernel(AttendParams p)
 {
     typedef AttendShape<FMT, DP, QT, ROWS> A;
@@ -221,7 +224,8 @@ __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) vo
         pair = (int)(group / (uint32_t)p.splits);
         split = (int)((group + (uint32_t)pair * (uint32_t)p.splits / 8) % (uint32_t)p.splits);    // (an XCD gets all kinds of parts)
     }
-    const int b = pair / p.heads, head = pair % p.heads;
+    const int heads_at = p.heads / SIDE;
+    const int b = pair / heads_at, head0 = pair % heads_at * SIDE, head = head0 + wave % SIDE;
     const int G = p.q_heads / p.heads, rows = p.n * G;
     const int row0 = (ROWS ? row_tile * 4 + wave : row_tile) * 16 * QT;
 
@@ -258,7 +262,7 @@ __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) vo
 
     // tokens of tile u that this wave loads: 16 * (ROWS ? wave : 0) + 16 t + c
     const int load0 = ROWS ? wave * 16 : 0;
-    const int step = ROWS ? 1 : 4, first = ROWS ? u0 : u0 + wave;
+    const int step = ROWS ? 1 : 4 / SIDE, first = ROWS ? u0 : u0 + wave / SIDE;
     auto page_of = [&](int u, int t) -> int {          // -1: no such token
         const bool in_tree = u >= prefix_tiles;
         const int pos = (in_tree ? span.prefix + (u - prefix_tiles) * TT : u * TT) + load0 + t * 16 + c;
@@ -485,22 +489,22 @@ __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) vo
 
     // results: [rows, D] of the output, or this split's part
     const bool whole = tiles <= p.chunk;               // no other part has anything
-    const size_t part = (((size_t)b * p.heads + head) * p.splits + split) * rows;
-    auto put_row = [&](int r, float mm, float ll) {    // statistics of a row
+    auto part_of = [&](int hd) { return (((size_t)b * p.heads + hd) * p.splits + split) * rows; };
+    auto put_row = [&](int hd, int r, float mm, float ll) {        // statistics of a row
         if (!whole) {
-            p.part_ml[(part + r) * 2] = mm;
-            p.part_ml[(part + r) * 2 + 1] = ll;
+            p.part_ml[(part_of(hd) + r) * 2] = mm;
+            p.part_ml[(part_of(hd) + r) * 2 + 1] = ll;
         } else if (p.lse) {
-            p.lse[((int64_t)b * p.n + r / G) * p.q_heads + head * G + r % G] = ll != 0.0f ? (mm + __builtin_amdgcn_logf(ll)) * kLn2f : -INFINITY;
+            p.lse[((int64_t)b * p.n + r / G) * p.q_heads + hd * G + r % G] = ll != 0.0f ? (mm + __builtin_amdgcn_logf(ll)) * kLn2f : -INFINITY;
         }
     };
-    auto put = [&](int r, int d, float ll, f32x4 v) {  // four elements of a row
+    auto put = [&](int hd, int r, int d, float ll, f32x4 v) {      // four elements of a row
         if (!whole) {
-            *reinterpret_cast<f32x4 *>(p.part_o + (part + r) * p.D + d) = v;
+            *reinterpret_cast<f32x4 *>(p.part_o + (part_of(hd) + r) * p.D + d) = v;
             return;
         }
         const float f = ll != 0.0f ? 1.0f / ll : 0.0f; // (a sum that is not a number is not nothing)
-        E *to = reinterpret_cast<E *>(p.out.data) + ((int64_t)b * p.out.sent + (int64_t)(r / G) * p.out.token + (int64_t)(head * G + r % G) * p.out.head + d);
+        E *to = reinterpret_cast<E *>(p.out.data) + ((int64_t)b * p.out.sent + (int64_t)(r / G) * p.out.token + (int64_t)(hd * G + r % G) * p.out.head + d);
         v *= f;
         if constexpr (FMT == 0) *reinterpret_cast<f32x4 *>(to) = v;
         else *reinterpret_cast<uint2 *>(to) = make_uint2(pack2<FMT>(v[0], v[1]), pack2<FMT>(v[2], v[3]));
@@ -512,10 +516,10 @@ __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) vo
         for (int j = 0; j < QT; ++j) {
             const int r = row0 + j * 16 + c;
             if (r >= rows) continue;
-            if (g == 0) put_row(r, m[j], l[j]);
+            if (g == 0) put_row(head, r, m[j], l[j]);
 #pragma unroll
             for (int d = 0; d < DT; ++d)
-                if (d * 16 + g * 4 < p.D) put(r, d * 16 + g * 4, l[j], o[j][d]);
+                if (d * 16 + g * 4 < p.D) put(head, r, d * 16 + g * 4, l[j], o[j][d]);
         }
     } else {
         // the four waves' parts: each on the common maximum, then added up from LDS
@@ -526,21 +530,26 @@ __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) vo
                 s_ml[wave][j * 16 + c][1] = l[j];
             }
         __syncthreads();                               // (and nobody reads values any more)
-        float top[QT], sum[QT], f[QT];
+        float sum[SIDE][QT], f[QT];                       // of each head of this workgroup
 #pragma unroll
-        for (int j = 0; j < QT; ++j) {
-            top[j] = -INFINITY;
-            sum[j] = 0.0f;
+        for (int hh = 0; hh < SIDE; ++hh) {
 #pragma unroll
-            for (int w = 0; w < 4; ++w) top[j] = fmaxf(top[j], s_ml[w][j * 16 + c][0]);
+            for (int j = 0; j < QT; ++j) {
+                float top = -INFINITY;
+                sum[hh][j] = 0.0f;
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                const float mw = s_ml[w][j * 16 + c][0], lw = s_ml[w][j * 16 + c][1];
-                sum[j] += mw == -INFINITY ? lw : lw * __builtin_amdgcn_exp2f(mw - top[j]);
+                for (int w = 0; w < 4; ++w)
+                    if (w % SIDE == hh) top = fmaxf(top, s_ml[w][j * 16 + c][0]);
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    if (w % SIDE != hh) continue;
+                    const float mw = s_ml[w][j * 16 + c][0], lw = s_ml[w][j * 16 + c][1];
+                    sum[hh][j] += mw == -INFINITY ? lw : lw * __builtin_amdgcn_exp2f(mw - top);
+                }
+                if (wave % SIDE == hh) f[j] = m[j] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[j] - top);
+                const int r = row0 + j * 16 + c;
+                if (wave == hh && g == 0 && r < rows) put_row(head, r, top, sum[hh][j]);
             }
-            f[j] = m[j] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[j] - top[j]);
-            const int r = row0 + j * 16 + c;
-            if (wave == 0 && g == 0 && r < rows) put_row(r, top[j], sum[j]);
         }
         f32x4 *const s_o = reinterpret_cast<f32x4 *>(s_mem);       // [wave][j][d of this round][lane]
         constexpr int DR = DT / 4;
@@ -553,16 +562,20 @@ __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) vo
                 for (int d = 0; d < DR; ++d) s_o[((wave * QT + j) * DR + d) * 64 + lane] = o[j][round * DR + d] * f[j];
             __syncthreads();
 #pragma unroll
-            for (int j = 0; j < QT; ++j)
+            for (int hh = 0; hh < SIDE; ++hh) {
 #pragma unroll
-                for (int d = 0; d < DR; ++d) {
-                    if ((j * DR + d) % 4 != wave) continue;
-                    f32x4 v = s_o[(j * DR + d) * 64 + lane];
+                for (int j = 0; j < QT; ++j)
 #pragma unroll
-                    for (int w = 1; w < 4; ++w) v += s_o[((w * QT + j) * DR + d) * 64 + lane];
-                    const int r = row0 + j * 16 + c, e = (round * DR + d) * 16 + g * 4;
-                    if (r < rows && e < p.D) put(r, e, sum[j], v);
-                }
+                    for (int d = 0; d < DR; ++d) {
+                        if (((hh * QT + j) * DR + d) % 4 != wave) continue;
+                        f32x4 v = s_o[((hh * QT + j) * DR + d) * 64 + lane];
+#pragma unroll
+                        for (int w = 1; w < 4; ++w)
+                            if (w > hh && w % SIDE == hh) v += s_o[((w * QT + j) * DR + d) * 64 + lane];
+                        const int r = row0 + j * 16 + c, e = (round * DR + d) * 16 + g * 4;
+                        if (r < rows && e < p.D) put(head0 + hh, r, e, sum[hh][j], v);
+                    }
+            }
         }
     }
 
@@ -573,22 +586,23 @@ __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) vo
     if (!s_bad) return;
     const int t0 = max(0, u0 - prefix_tiles) * TT, t1 = min(tree, (u1 - prefix_tiles) * TT);
     const int r0 = row_tile * p.tile_rows, r1 = min(rows, r0 + p.tile_rows);
-    for (int x = (int)threadIdx.x; x < (r1 - r0) * p.D; x += 256) {
-        const int r = r0 + x / p.D, e = x % p.D, node = r / G;
-        float v = 0.0f;
-        for (int t = t0; t < t1; ++t) {
-            if (p.mask ? (t >> 6) >= p.mask_words || !((p.mask[((int64_t)b * p.n + node) * p.mask_words + (t >> 6)] >> (t & 63)) & 1)
-                       : t > tree_all - p.n + node)
-                continue;
-            const int64_t at = token_offset(p.cache, b, (int64_t)span.prefix + t);
-            if (at < 0) continue;
-            const float y = (float)reinterpret_cast<const E *>(p.v_pages)[at + head_at + e];
-            if (!(fabsf(y) < INFINITY)) v += y;
+    for (int hd = head0; hd < head0 + SIDE; ++hd)
+        for (int x = (int)threadIdx.x; x < (r1 - r0) * p.D; x += 256) {
+            const int r = r0 + x / p.D, e = x % p.D, node = r / G;
+            float v = 0.0f;
+            for (int t = t0; t < t1; ++t) {
+                if (p.mask ? (t >> 6) >= p.mask_words || !((p.mask[((int64_t)b * p.n + node) * p.mask_words + (t >> 6)] >> (t & 63)) & 1)
+                           : t > tree_all - p.n + node)
+                    continue;
+                const int64_t at = token_offset(p.cache, b, (int64_t)span.prefix + t);
+                if (at < 0) continue;
+                const float y = (float)reinterpret_cast<const E *>(p.v_pages)[at + (int64_t)hd * p.cache.head_stride + e];
+                if (!(fabsf(y) < INFINITY)) v += y;
+            }
+            if (v == 0.0f) continue;
+            if (!whole) p.part_o[(part_of(hd) + r) * p.D + e] = v;
+            else reinterpret_cast<E *>(p.out.data)[(int64_t)b * p.out.sent + (int64_t)node * p.out.token + (int64_t)(hd * G + r % G) * p.out.head + e] = (E)v;
         }
-        if (v == 0.0f) continue;
-        if (!whole) p.part_o[(part + r) * p.D + e] = v;
-        else reinterpret_cast<E *>(p.out.data)[(int64_t)b * p.out.sent + (int64_t)node * p.out.token + (int64_t)(head * G + r % G) * p.out.head + e] = (E)v;
-    }
 }
 
 // Joins the parts of a row: 2^(m_s - m) O_s and 2^(m_s - m) l_s added up over its parts s.  Of a part, a lane takes four elements, and as many parts
@@ -688,6 +702,7 @@ template <int FMT, int DP> constexpr int kAttendWidest = DP == 64 ? 4 : DP == 12
 // How a call is laid out: which kernel, how many workgroups along the rows and the token axis.
 struct AttendPlan {
     int DP, QT;
+    int side;                          // heads of a workgroup whose waves have tiles of their own: 1 or 2
     bool shared;                       // the waves have rows of their own (ROWS)
     int tile, tile_rows, row_tiles, splits, chunk;
 };

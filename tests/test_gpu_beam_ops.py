@@ -514,6 +514,39 @@ def test_attend_over_a_long_tail_of_small_weights(beam, dtype, n):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("B,n,Hq,Hkv,D,masked", [(128, 2, 16, 8, 64, True), (128, 1, 8, 8, 128, False), (64, 20, 16, 16, 24, True), (52, 3, 20, 20, 80, True), (32, 2, 16, 16, 256, False),
+                                                 (128, 9, 32, 8, 64, True)])
+def test_attend_of_many_sentences(beam, dtype, B, n, Hq, Hkv, D, masked):
+    r = np.random.RandomState(B + D)
+    prefix, tree = r.randint(0, 40, B), r.randint(0, 70, B)
+    prefix[0], tree[0] = 150, 64
+    prefix[1], tree[1] = 0, 0
+    check_attend(beam, dtype, B, n, Hq, Hkv, D, 8, prefix.tolist(), tree.tolist(), masked=masked, seed=5, density=0.2)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_attend_of_many_sentences_what_is_not_seen_does_not_matter(beam, dtype):
+    B, n, H, D, page = 128, 2, 8, 64, 8
+    prefix, tree = torch.full((B,), 5, dtype=torch.int32), torch.full((B,), 33, dtype=torch.int32)
+    k_pages, v_pages, table = a_cache(2, B, 40, H, D, page, dtype)
+    q = torch.randn(B, n, H, D, generator=gen(3)).to(dtype).cuda()
+    mask, bits = random_mask(1, B, n, 1)
+    bits[:, 0, 30], bits[:, 1, 30] = False, True
+    mask = torch.from_numpy(np.packbits(bits, axis=2, bitorder="little").view(np.int64).reshape(B, n, 1).copy())
+    want = plain_attend(q, k_pages, v_pages, table, prefix, tree, lambda b, i, j: bits[b, i, j], D ** -0.5)
+    at = 5 + 30
+    for b in range(B):                                                  # one element of one head is not a number, differently for each sentence
+        v_pages[int(table[b, at // page]), at % page, b % H, b % D] = math.nan
+    got, lse = beam.attend(q, k_pages, v_pages, table.cuda(), prefix.cuda(), tree.cuda(), mask.cuda(), return_lse=True)
+    near(got[:, :1], lse[:, :1], [x[:, :1] for x in want])
+    spoiled = torch.zeros(B, H, D, dtype=torch.bool)
+    spoiled[torch.arange(B), torch.arange(B) % H, torch.arange(B) % D] = True
+    seen = got[:, 1].cpu().double()
+    assert torch.equal(torch.isnan(seen), spoiled)
+    assert ((seen - want[0][:, 1]).abs()[~spoiled] <= want[2][:, 1][~spoiled]).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 def test_attend_no_further_than_max_len(beam, dtype):
     B, n, H, D = 2, 3, 2, 64
     k_pages, v_pages, table = a_cache(2, B, 320, H, D, 16, dtype)
