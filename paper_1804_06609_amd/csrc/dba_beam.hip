@@ -119,7 +119,7 @@ HeadsAt heads_of(const dba_heads *h)
 
 // Rows (nodes times the query heads of a cache head) decide the form.  Up to 64, a wave holds them all and the waves share out the tokens,
 // which are then read once; with more, or without registers for so many, the waves have rows of their own and share the tokens' tiles
-// (504 rows of 128: 145 us against 246 with row tiles of 64 that each read the tokens; 40 to 48 rows of 128: 175 and 197 us against
+// (when this was chosen, 504 rows of 128 took 145 us against 246 with row tiles of 64 that each read the tokens; 40 to 48 rows of 128: 175 and 197 us against
 // 182 and 184 with shared tiles).  The token axis is cut into as many parts as fill the GPU once: each part costs a start-up of several
 // trips to memory, and twice as many were slower (one sentence of 29000 tokens 59 against 43 us, five of 21600 56 against 39),
 // but for shared tiles, whose sentences' lengths matter more than that.  There the first part of a sentence has a quarter more than an even share, so that

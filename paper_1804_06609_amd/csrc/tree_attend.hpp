@@ -189,8 +189,8 @@ struct AttendShape {
 };
 
 // Bound: without ROWS memory; each token is read once.  A pool with the heads of a token side by side gives 128 or 256 bytes at a time (64 sentences of
-// 20 branches, heads of 64: 72 us, 4.4 TB/s; 4 of 57000 tokens, heads of 128: 188 us, 5.0 TB/s), one with a head's tokens side by side
-// more (68 and 172 us with a head a workgroup).  With ROWS the issue slots: a tile of 64 tokens and 32 rows of 128 takes a wave 64 matrix instructions
+// 20 branches, heads of 64: 68 us, 4.7 TB/s; 4 of 57000 tokens, heads of 128: 187 us, 5.0 TB/s), one with a head's tokens side by side
+// more (the second 172 us).  With ROWS the issue slots: a tile of 64 tokens and 32 rows of 128 takes a wave 64 matrix instructions
 // and 350 others (32 sentences of 500 to 4000 tokens, 63 nodes of 32 heads: 122 us, 0.6 PFLOP/s of fp16).
 //
 // SIDE: heads of a workgroup.  With two, waves 0 and 2 have the first, 1 and 3 the second: a longer stretch of memory where the heads of a token lie
