@@ -31,7 +31,9 @@ struct SelectParams {
 };
 
 constexpr int kSelectThreads = 256;    // of the first launch
-constexpr int kSelectChunks = 8;       // 16-byte chunks a thread keeps in registers
+// 16-byte chunks a thread keeps in registers: as many as 64 registers have room for, since a workgroup's chain of barriers takes 9 us however much it has read
+// (rows of 50000 in 16 bits in three parts instead of four: 158 -> 135 us; with ten registers spill)
+constexpr int kSelectChunks = 9;
 constexpr int kSelectQueue = 256;      // chunks it looks through for keys
 constexpr int kSelectKeys = 1024;      // keys it chooses from
 constexpr int kSelectFinal = 1024;     // extensions the second launch has room for
@@ -165,10 +167,10 @@ __device__ __forceinline__ uint32_t bound_of_kth(const uint32_t (&r)[J], int k, 
     return lo;
 }
 
-// One part of one row.  Bound: HBM (the logits are read once); with 16 bits the VALU is about as busy: an element takes five
+// One part of one row.  Bound: HBM (the logits are read once), and with 16 bits the VALU nearly: an element takes five
 // instructions, one of them the exponential.  So nothing else is done element by element: addresses are the same for a whole wave
 // but for its lanes' 16 bytes, edges of a row that do not fill a chunk are single elements of the first wave, and of the chunks only those that
-// reach the bar are looked through (128 x 64 rows of 50000 in bf16: 158 us, 5.2 TB/s; 64 x 20 of 32000 in fp32: 24.6 us, 6.7 TB/s).
+// reach the bar are looked through (128 x 64 rows of 50000 in bf16: 135 us, 6.1 TB/s; 64 x 20 of 32000 in fp32: 25 us, 6.6 TB/s).
 template <int FMT>
 __global__ __launch_bounds__(kSelectThreads, 8) void dba_select_part_kernel(const void *logits, SelectParams p)
 {
