@@ -142,6 +142,20 @@ def test_select_equal_logits_go_to_the_first(beam, dtype, V):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+def test_select_where_more_reach_the_bound_than_there_is_room_for(beam, dtype):
+    """Fewer lists than slots, so that every list's keys are looked at; and thousands of equal scores, of which the first count."""
+    logits, score, flags = a_beam(6, 2, 28, 22357, dtype)
+    check_select(beam, logits, score, None, 62)
+    logits = torch.zeros(2, 20, 40000, dtype=dtype)
+    logits[1, :, :100] = -1
+    score = torch.full((2, 20), -2.0)
+    score[1, :5] = -3.0                                # the sixth row's tokens from the hundredth on
+    got = [x.cpu() for x in beam.select(logits.cuda(), score.cuda(), None, 64, EOS, PAD)]
+    assert got[0][0].tolist() == list(range(64)) and got[1][0].tolist() == [0] * 64
+    assert got[0][1].tolist() == list(range(100, 164)) and got[1][1].tolist() == [5] * 64
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("V", [200, 1164, 20000, 70001])
 def test_select_where_the_best_lie_together(beam, dtype, V):
     """Tokens in the order of their frequency, up and down; coarse logits, of which many are equal; a block of tokens allowed."""
