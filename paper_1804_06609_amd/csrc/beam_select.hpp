@@ -258,30 +258,30 @@ __global__ __launch_bounds__(kSelectThreads, 8) void dba_select_part_kernel(cons
     }
     const float most_x = most ? float_from_ord(most) : 0.0f;
     // The sum: a few dozen terms a thread in fp32 (each is off by 1e-7 of itself, either way), the threads' in 64 bits.  The reference is
-    // the rounded product itself, so that no error of its own comes in; where that would overflow (logits at fp32's lowest value),
-    // two different logits are so far apart that a term is 0 or 1.
-    float sum;
+    // the rounded product itself, so that no error of its own comes in.  What that rounding leaves, though, grows with the logits: at a mask's -1e10 every
+    // term is 2^247.  So from 2^20 on, where it is still 0.1, logits are subtracted first, which is exact wherever a term is not 0.
     const float m2 = most_x * kLog2eHi;
-    const bool huge = !(fabsf(most_x) < 1e37f);
+    const bool huge = !(fabsf(most_x) < 0x1p20f);
+    float part_sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     if (!huge) {
-        float part_sum[4] = {exp2_above(edge, m2), 0.0f, 0.0f, 0.0f};
+        part_sum[0] = exp2_above(edge, m2);
 #pragma unroll
         for (int r = 0; r < R; ++r)
             if (has_round(r)) {
 #pragma unroll
                 for (int e = 0; e < N; ++e) part_sum[e & 3] += exp2_above(C::get(raw[r], e), m2);
             }
-        sum = (part_sum[0] + part_sum[1]) + (part_sum[2] + part_sum[3]);
     } else {
-        auto term = [&](float x) { return x < most_x ? 0.0f : x == most_x && x < INFINITY ? 1.0f : NAN; };
-        sum = term(edge);
-#pragma unroll 1
-        for (int r = 0; r < R && has_round(r); ++r) {
-            const uint4 again = load_round(r);
+        auto term = [&](float x) { return exp2_above(x - most_x, 0.0f); };
+        part_sum[0] = term(edge);
 #pragma unroll
-            for (int e = 0; e < N; ++e) sum += term(C::get(again, e));
-        }
+        for (int r = 0; r < R; ++r)
+            if (has_round(r)) {
+#pragma unroll
+                for (int e = 0; e < N; ++e) part_sum[e & 3] += term(C::get(raw[r], e));
+            }
     }
+    const float sum = (part_sum[0] + part_sum[1]) + (part_sum[2] + part_sum[3]);
     const double total = wave_sum_double((double)sum);
     if (lane == 0) s_sum[wave] = total;
     __syncthreads();

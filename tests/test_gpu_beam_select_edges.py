@@ -1,0 +1,57 @@
+"""-m gpu: selection from logits whose rows hold masks' fill values of any size.
+
+Tolerances are those of test_gpu_beam_ops.py: the score's rounding and 2^-22 for the exponentials.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from test_gpu_beam_ops import TYPES, U32, beam, check_select, gen, plain_select  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def around(x):
+    """x and its neighbours in fp32."""
+    return [float(np.nextafter(np.float32(x), np.float32(to))) for to in (-np.inf, np.inf)] + [float(x)]
+
+
+FILLS = [-1e4, -65504.0, 1e9, -1e9, 1e10, -1e10, -1e18, 1e18, -1e20, -1e30, 1e30, 1e36, -1e36] + [
+    s * x for e in (2.0 ** 10, 2.0 ** 20, 2.0 ** 24, 2.0 ** 30, 1e37) for x in around(e) for s in (1, -1)]
+V = 41000                                              # several parts of a row in every type
+
+
+def filled(dtype):
+    """A sentence for each fill value that the type holds: a row of nothing else; a row whose only other logits lie in its last part; a
+    row around the fill's size, of which the first half is nothing but that."""
+    fills = torch.tensor(FILLS, dtype=torch.float64).to(dtype)
+    fills = fills[torch.isfinite(fills)]
+    B, g = len(fills), gen(11)
+    x = fills[:, None, None].expand(B, 3, V).clone()
+    x[:, 1, V - 300:] = (torch.randn(B, 300, generator=g) * 2).to(dtype)
+    some = fills.double()[:, None] * torch.randint(4, 9, (B, V), generator=g) / 8
+    x[:, 2] = some.to(dtype)
+    x[:, 2, V // 2:] = torch.where(torch.rand(B, V - V // 2, generator=g) < 0.5, x[:, 2, V // 2:], (torch.randn(B, V - V // 2, generator=g) * 2).to(dtype))
+    score = torch.tensor([0.3, -4.5, -2.1])[None] - torch.rand(B, 3, generator=g)
+    return x, score
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("k_out", [1, 6, 64])
+def test_select_from_rows_of_fill_values(beam, dtype, k_out):  # noqa: F811
+    logits, score = filled(dtype)
+    check_select(beam, logits, score, None, k_out)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_no_row_of_fill_values_is_lost(beam, dtype):  # noqa: F811
+    """Every row by itself: its normaliser is finite, so k_out extensions come back."""
+    logits, score = filled(dtype)
+    one = logits.reshape(-1, 1, V)
+    got = [x.cpu() for x in beam.select(one.cuda(), score.reshape(-1, 1).cuda(), None, 4, 2, 0)]
+    assert (got[1] == 0).all() and (got[3] & 2 == 0).all()
+    want = plain_select(one, score.reshape(-1, 1), None, 4)[2]
+    near = np.abs(want) < 1e30
+    assert (np.abs(got[2].numpy() - want)[near] <= np.abs(want)[near] * U32 + 2.0 ** -22).all()
