@@ -50,7 +50,7 @@ __device__ __forceinline__ float exp2_above(float x, float m2)
     return __builtin_amdgcn_exp2f(fmaf(x, kLog2eLo, fmaf(x, kLog2eHi, -m2)));
 }
 
-template <int FMT> struct Chunk;       // 16 bytes of logits
+template <int FMT> struct Chunk;       // 16 bytes of logits; loose_t: at any element's address
 template <> struct Chunk<0> {
     static __device__ __forceinline__ float most(const uint4 &c)
     {
@@ -58,6 +58,7 @@ template <> struct Chunk<0> {
     }
     static constexpr int N = 4;
     typedef float elem_t;
+    typedef uint32_t loose_t __attribute__((ext_vector_type(4), aligned(4)));
     static __device__ __forceinline__ float get(const uint4 &c, int e) { return __uint_as_float(((const uint32_t *)&c)[e]); }
     static __device__ __forceinline__ float value(float x) { return x; }
     static constexpr uint32_t kNone = 0xFF800000u;
@@ -72,6 +73,7 @@ template <> struct Chunk<1> {
     }
     static constexpr int N = 8;
     typedef uint16_t elem_t;
+    typedef uint32_t loose_t __attribute__((ext_vector_type(4), aligned(2)));
     static __device__ __forceinline__ float get(const uint4 &c, int e)
     {
         const uint32_t w = ((const uint32_t *)&c)[e >> 1];
@@ -92,6 +94,7 @@ template <> struct Chunk<2> {
     }
     static constexpr int N = 8;
     typedef uint16_t elem_t;
+    typedef uint32_t loose_t __attribute__((ext_vector_type(4), aligned(2)));
     static __device__ __forceinline__ float get(const uint4 &c, int e)
     {
         const uint32_t w = ((const uint32_t *)&c)[e >> 1];
@@ -170,7 +173,7 @@ __device__ __forceinline__ uint32_t bound_of_kth(const uint32_t (&r)[J], int k, 
 
 // One part of one row.  Bound: HBM (the logits are read once), and with 16 bits the VALU nearly: an element takes five
 // instructions, one of them the exponential.  So nothing else is done element by element: addresses are the same for a whole wave
-// but for its lanes' 16 bytes, edges of a row that do not fill a chunk are single elements of the first wave, and of the chunks only those that
+// but for its lanes' 16 bytes, the end of a row that does not fill a chunk are single elements of the first wave, and of the chunks only those that
 // reach the bar are looked through (128 x 64 rows of 50000 in bf16: 135 us, 6.1 TB/s; 64 x 20 of 32000 in fp32: 25 us, 6.6 TB/s).
 template <int FMT>
 __global__ __launch_bounds__(kSelectThreads, 8) void dba_select_part_kernel(const void *logits, SelectParams p)
@@ -204,21 +207,24 @@ __global__ __launch_bounds__(kSelectThreads, 8) void dba_select_part_kernel(cons
         return;
     }
     const elem_t *src = static_cast<const elem_t *>(logits) + ((int64_t)b * p.sent_stride + (int64_t)h * p.row_stride);
-    // Chunks lie on the 16-byte grid of memory; the first starts `shift` elements before the row.  [full0, full1) lie in the row whole;
-    // the elements before and behind them are taken one by one, by the first 2N threads of the parts they lie in.
-    const int shift = (int)((reinterpret_cast<uintptr_t>(src) & 15) / sizeof(elem_t));
-    const uint4 *grid = reinterpret_cast<const uint4 *>(src - shift);
-    const int full0 = shift ? 1 : 0, full1 = (p.V + shift) / N;
-    const int c0 = part * p.part_chunks, c1 = min(c0 + p.part_chunks, full1);
+    // Chunks are counted from the row's start, wherever it lies in memory, so that rows that are alike are summed alike and their extensions are equal.
+    // (Of 16-byte loads only those at odd multiples of two bytes cost more: 128 x 64 rows of 50001 in bf16 171 us, by a 16-byte grid of memory, which
+    // sums rows of other offsets in other groups, 152; 64 x 20 of 32001 in fp32 35 either way.)  The elements behind the last whole chunk are taken one by one, by the
+    // first N threads of the part they lie in.
+    typedef typename C::loose_t loose_t;
+    const loose_t *chunks = reinterpret_cast<const loose_t *>(src);
+    auto chunk_at = [](const loose_t *at) { const loose_t v = *at; return make_uint4(v.x, v.y, v.z, v.w); };
+    const int whole = p.V / N;
+    const int c0 = part * p.part_chunks, c1 = min(c0 + p.part_chunks, whole);
     auto wave_chunk = [&](int r) { return c0 + wave * kWave + r * T; };
     auto has_round = [&](int r) { return wave_chunk(r) < c1; };       // the same for the whole wave
     auto none = [] { const uint32_t w = N == 4 ? C::kNone : C::kNone | (C::kNone << 16); return make_uint4(w, w, w, w); };
     auto load_round = [&](int r) {                     // what is not a whole chunk of this part is -inf
         const int cw = wave_chunk(r);
-        const uint4 *from = grid + cw;
-        if (cw >= full0 && cw + kWave <= c1) return from[(uint32_t)lane];
+        const loose_t *from = chunks + cw;
+        if (cw + kWave <= c1) return chunk_at(from + (uint32_t)lane);
         uint4 v = none();
-        if (cw + lane >= full0 && cw + lane < c1) v = from[(uint32_t)lane];
+        if (cw + lane < c1) v = chunk_at(from + (uint32_t)lane);
         return v;
     };
     uint4 raw[R];
@@ -226,13 +232,8 @@ __global__ __launch_bounds__(kSelectThreads, 8) void dba_select_part_kernel(cons
     for (int r = 0; r < R; ++r)
         if (has_round(r)) raw[r] = load_round(r);
     float edge = -INFINITY;                            // a single element
-    int edge_at = 0;
-    if (t < 2 * N) {
-        const int head = full1 == 0 ? p.V : shift ? N - shift : 0, tail = full1 == 0 ? 0 : (p.V + shift) % N;
-        const bool first = t < N;
-        edge_at = first ? t : p.V - tail + (t - N);
-        if (first ? part == 0 && t < head : c0 <= full1 && full1 - c0 < p.part_chunks && t - N < tail) edge = C::value(src[edge_at]);
-    }
+    const int edge_at = whole * N + t;
+    if (t < N && c0 <= whole && whole - c0 < p.part_chunks && edge_at < p.V) edge = C::value(src[edge_at]);
     float top = edge, most_of[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
@@ -319,7 +320,7 @@ __global__ __launch_bounds__(kSelectThreads, 8) void dba_select_part_kernel(cons
             const int i = i0 + lane;
             const bool is = i < queued * N;
             const float x = is ? C::value(elems[i]) : -INFINITY;
-            put(x >= bar, x, is ? s_queue_chunk[i / N] * N - shift + i % N : 0);
+            put(x >= bar, x, is ? s_queue_chunk[i / N] * N + i % N : 0);
         }
     }
     __syncthreads();
@@ -367,7 +368,7 @@ __global__ __launch_bounds__(kSelectThreads, 8) void dba_select_part_kernel(cons
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
                     const float x = C::get(again, e);
-                    if (x >= bar) f(make_key(x, (uint32_t)((wave_chunk(r) + lane) * N - shift + e)));
+                    if (x >= bar) f(make_key(x, (uint32_t)((wave_chunk(r) + lane) * N + e)));
                 }
             }
         };

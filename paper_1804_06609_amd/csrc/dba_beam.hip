@@ -53,7 +53,7 @@ SelectPlan select_plan(int B, int k_in, int k_out, int V, int format)
 {
     SelectPlan s;
     const int per_chunk = 16 / (int)elem_bytes(format);
-    const int chunks = (V + per_chunk - 1) / per_chunk + 1;        // a row that starts inside a chunk may touch one more
+    const int chunks = (V + per_chunk - 1) / per_chunk;
     const int most = kSelectThreads * kSelectChunks;
     s.nparts = (chunks + most - 1) / most;
     // whole rounds of the workgroup, where that leaves no part without a chunk

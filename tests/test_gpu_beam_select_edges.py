@@ -1,4 +1,4 @@
-"""-m gpu: selection from logits whose rows hold masks' fill values of any size.
+"""-m gpu: selection from logits whose rows hold masks' fill values of any size, and from equal rows wherever they lie in memory.
 
 Tolerances are those of test_gpu_beam_ops.py: the score's rounding and 2^-22 for the exponentials.
 """
@@ -55,3 +55,16 @@ def test_no_row_of_fill_values_is_lost(beam, dtype):  # noqa: F811
     want = plain_select(one, score.reshape(-1, 1), None, 4)[2]
     near = np.abs(want) < 1e30
     assert (np.abs(got[2].numpy() - want)[near] <= np.abs(want)[near] * U32 + 2.0 ** -22).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("V,k,k_out", [(9, 4, 4), (777, 5, 10), (1001, 64, 64), (32003, 7, 7), (50001, 5, 5), (50002, 6, 24)])
+def test_equal_rows_go_by_their_order(beam, dtype, V, k, k_out):  # noqa: F811
+    """Rows alike in logits and score, which start at different offsets from 16 bytes: equal extensions come in the order of the rows."""
+    logits = (torch.randn(6, 1, V, generator=gen(V)) * 2).to(dtype).expand(6, k, V).contiguous()
+    score = (-torch.rand(6, 1, generator=gen(k)) - 3).expand(6, k).contiguous()
+    check_select(beam, logits, score, None, k_out)
+    for lead, ld in ((1, V + 2), (3, V + 5)):
+        room = torch.full((6, k, ld + lead), math.nan, dtype=dtype)
+        room[:, :, lead:lead + V] = logits
+        check_select(beam, logits, score, None, k_out, room.cuda()[:, :, lead:lead + V])
