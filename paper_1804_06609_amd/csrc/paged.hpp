@@ -40,4 +40,13 @@ DBA_HD Span span_of(int prefix, int tree, int limit)
     return s;
 }
 
+// The same of the nodes up to `last` of a chain of n, which is the last n of the tree's tokens.
+DBA_HD Span span_of_chain(int prefix, int tree, int n, int last, int limit)
+{
+    Span s = span_of(prefix, tree, limit);
+    const int64_t seen = (int64_t)(tree < 0 ? 0 : tree) - n + last + 1, end = s.prefix + (seen < 0 ? 0 : seen);
+    if (end < s.end) s.end = (int)end;
+    return s;
+}
+
 }  // namespace dba

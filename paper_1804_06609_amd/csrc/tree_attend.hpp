@@ -35,12 +35,8 @@ struct AttendParams {
 __device__ __forceinline__ Span span_of_rows(const AttendParams &p, int b, int row_tile, int G, int &tree_all)
 {
     tree_all = p.tree ? max(p.tree[b], 0) : 0;
-    Span s = span_of(p.prefix[b], tree_all, p.max_len);
-    if (!p.mask) {
-        const int last = min((row_tile + 1) * p.tile_rows, p.n * G) - 1;
-        s.end = min(s.end, s.prefix + max(0, tree_all - p.n + last / G + 1));
-    }
-    return s;
+    return p.mask ? span_of(p.prefix[b], tree_all, p.max_len)
+                  : span_of_chain(p.prefix[b], tree_all, p.n, (min((row_tile + 1) * p.tile_rows, p.n * G) - 1) / G, p.max_len);
 }
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
