@@ -66,9 +66,10 @@ typedef struct dba_state {
 
 /*
  * dst[b, h] = src[b, backptr[b, h]] for every state; a back-pointer outside [0, k) (an empty slot has -1) clears the row.
- * In place, rows that stay where they are are neither read nor written.  dst and src of one state are the same or do not
- * overlap, and pieces of dst do not overlap each other.
- *   backptr_dev  device [B,k] int32 (as dba_step or dba_beam_select wrote it); must not lie in a state
+ * In place, rows that stay where they are are neither read nor written.  dst and src of one state are the same or have no byte in common,
+ * pieces of dst do not overlap each other, and no state's dst has a byte in common with another state's dst or src: the states are
+ * moved at the same time.  (Views of one tensor that interleave are apart.  Where they interleave in different strides, more than 65536 times, they count as overlapping.)
+ *   backptr_dev  device [B,k] int32 (as dba_step or dba_beam_select wrote it); must not lie in a dst
  *   states_host  host [n_states] (copied before the call returns)
  */
 DBA_API int dba_beam_reorder(int B, int k, const int32_t *backptr_dev, const dba_state *states_host, int n_states, void *hip_stream);

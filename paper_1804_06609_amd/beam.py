@@ -155,7 +155,8 @@ def _pieces(shape, strides, e: int):
 def reorder(backptr: torch.Tensor, states: Sequence[torch.Tensor], out: Optional[Sequence[torch.Tensor]] = None):
     """Every state [B, k, ...] (any type) follows backptr [B, k] int32: out[b, h] = state[b, backptr[b, h]], rows of a
     back-pointer outside [0, k) cleared.  out None: in place.  Views of the places in use do: behind the
-    second axis a state may have one more that is not dense (e.g. [B, k, heads, capacity, width][:, :, :, :t]).  Returns `out`."""
+    second axis a state may have one more that is not dense (e.g. [B, k, heads, capacity, width][:, :, :, :t]).  All are moved at the
+    same time: what is written lies in no other state, nor in its out.  Returns `out`."""
     lib = load()
     if backptr.dim() != 2:
         _fail("backptr must be [B, k]")

@@ -3,12 +3,15 @@
 #include <math.h>
 
 #include <algorithm>
+#include <memory>
+#include <new>
 
 #include "../../include/dba_beam.h"
 #include "beam_reorder.hpp"
 #include "beam_select.hpp"
 #include "cache_append.hpp"
 #include "entry.hpp"
+#include "places.hpp"
 #include "tree_attend.hpp"
 
 using namespace dba;
@@ -249,39 +252,45 @@ DBA_API int dba_beam_reorder(int B, int k, const int32_t *backptr_dev, const dba
         return set_error(DBA_EINVAL, "dba_beam_reorder: need 1 <= B <= 65535, 1 <= k <= %d, n_states >= 0", DBA_MAX_BEAM);
     if (!backptr_dev || (n_states > 0 && !states_host)) return set_error(DBA_EINVAL, "dba_beam_reorder: a pointer is NULL");
     // everything is looked at before anything is launched
+    struct Moved {
+        Places dst, src;
+        bool in_place, any;
+    };
+    Moved few[kReorderStates];
+    std::unique_ptr<Moved[]> many(n_states > kReorderStates ? new (std::nothrow) Moved[n_states] : nullptr);
+    if (n_states > kReorderStates && !many) return set_error(DBA_ENOMEM, "dba_beam_reorder: no host memory to look at %d states", n_states);
+    Moved *const moved = many ? many.get() : few;
     for (int i = 0; i < n_states; ++i) {
         const dba_state &s = states_host[i];
         if (s.segs < 0 || s.seg_bytes < 0) return set_error(DBA_EINVAL, "dba_beam_reorder: state %d has a negative size", i);
-        if (s.segs == 0 || s.seg_bytes == 0) continue;
+        Moved &m = moved[i];
+        m.any = s.segs != 0 && s.seg_bytes != 0;
+        if (!m.any) continue;
         if (!s.dst || !s.src) return set_error(DBA_EINVAL, "dba_beam_reorder: a pointer of state %d is NULL", i);
-        const int64_t count[3] = {B, k, s.segs};
-        const int64_t ds[3] = {s.dst_sent, s.dst_row, s.dst_seg}, ss[3] = {s.src_sent, s.src_row, s.src_seg};
-        __int128 d_end = s.seg_bytes, s_end = s.seg_bytes;
-        int order[3] = {0, 1, 2};
-        std::sort(order, order + 3, [&](int x, int y) { return ds[x] < ds[y]; });
-        for (int x = 0; x < 3; ++x) {
-            const int o = order[x];
-            if (count[o] == 1) continue;
-            if (ds[o] < d_end) return set_error(DBA_EINVAL, "dba_beam_reorder: pieces of state %d's dst overlap", i);
-            d_end += (__int128)ds[o] * (count[o] - 1);
-        }
-        for (int x = 0; x < 3; ++x) {
-            if (count[x] == 1) continue;
-            if (ss[x] < 0) return set_error(DBA_EINVAL, "dba_beam_reorder: state %d has a negative stride", i);
-            s_end += (__int128)ss[x] * (count[x] - 1);
-        }
-        if (d_end > ((__int128)1 << 62) || s_end > ((__int128)1 << 62))
-            return set_error(DBA_EINVAL, "dba_beam_reorder: state %d is larger than memory", i);
-        const unsigned char *d = static_cast<unsigned char *>(s.dst), *c = static_cast<const unsigned char *>(s.src);
-        if (d == c) {
-            for (int x = 0; x < 3; ++x)
-                if (count[x] > 1 && ds[x] != ss[x])
-                    return set_error(DBA_EINVAL, "dba_beam_reorder: state %d is reordered in place with two sets of strides", i);
-        } else if (d < c + (int64_t)s_end && c < d + (int64_t)d_end) {
+        m.dst = Places(s.dst, s.seg_bytes).axis(B, s.dst_sent).axis(k, s.dst_row).axis(s.segs, s.dst_seg);
+        m.src = Places(s.src, s.seg_bytes).axis(B, s.src_sent).axis(k, s.src_row).axis(s.segs, s.src_seg);
+        m.in_place = s.dst == s.src;
+        if (!m.dst.nested()) return set_error(DBA_EINVAL, "dba_beam_reorder: pieces of state %d's dst overlap", i);
+        if (m.src.axes && m.src.stride[m.src.axes - 1] < 0) return set_error(DBA_EINVAL, "dba_beam_reorder: state %d has a negative stride", i);
+        if (!m.dst.fits() || !m.src.fits()) return set_error(DBA_EINVAL, "dba_beam_reorder: state %d is larger than memory", i);
+        if (m.in_place) {
+            if ((B > 1 && s.dst_sent != s.src_sent) || (k > 1 && s.dst_row != s.src_row) || (s.segs > 1 && s.dst_seg != s.src_seg))
+                return set_error(DBA_EINVAL, "dba_beam_reorder: state %d is reordered in place with two sets of strides", i);
+        } else if (meet(m.dst, m.src)) {
             return set_error(DBA_EINVAL, "dba_beam_reorder: dst and src of state %d overlap", i);
         }
         if ((__int128)s.segs * s.seg_bytes > ((__int128)1 << 31))
             return set_error(DBA_EINVAL, "dba_beam_reorder: a row of state %d has more than 2 GB", i);
+    }
+    // states are moved at the same time, in any order
+    const Places back(backptr_dev, (int64_t)B * k * 4);
+    for (int i = 0; i < n_states; ++i) {
+        if (!moved[i].any) continue;
+        if (meet(moved[i].dst, back)) return set_error(DBA_EINVAL, "dba_beam_reorder: backptr_dev lies in state %d's dst", i);
+        for (int j = 0; j < i; ++j)
+            if (moved[j].any && (meet(moved[i].dst, moved[j].dst) || (!moved[j].in_place && meet(moved[i].dst, moved[j].src)) ||
+                                 (!moved[i].in_place && meet(moved[j].dst, moved[i].src))))
+                return set_error(DBA_EINVAL, "dba_beam_reorder: states %d and %d overlap where one is written", j, i);
     }
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     ReorderParams p;
