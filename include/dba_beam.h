@@ -42,8 +42,8 @@ extern "C" {
  *   flags_dev           device [B,k_in] uint8 of DBA_FLAG_* bits; NULL: all rows are live
  *   out_token_dev, out_backptr_dev, out_score_dev, out_flags_dev
  *                       device [B,k_out] int32, int32, fp32, uint8 as dba_step writes them: an empty slot has pad_id,
- *                       -1, -inf, DBA_FLAG_DEAD.  None may be NULL or lie in an input.
- *   workspace_dev       device, 256-byte aligned, at least dba_beam_select_workspace_bytes bytes; its content does not matter
+ *                       -1, -inf, DBA_FLAG_DEAD.  None may be NULL, lie in an input or the workspace, or overlap another.
+ *   workspace_dev       device, 256-byte aligned, at least dba_beam_select_workspace_bytes bytes; its content does not matter; no input lies in it
  */
 DBA_API size_t dba_beam_select_workspace_bytes(int B, int k_in, int k_out, int V, int logits_format);
 DBA_API int dba_beam_select(int B, int k_in, int k_out, int V, int eos_id, int pad_id, const void *logits_dev, int logits_format,

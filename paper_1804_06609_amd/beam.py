@@ -104,7 +104,7 @@ def _workspace(nbytes: int, like: torch.Tensor):
 def select(logits: torch.Tensor, score: torch.Tensor, flags: Optional[torch.Tensor], k_out: int, eos_id: int, pad_id: int,
            out: Optional[Sequence[torch.Tensor]] = None):
     """The new beam from logits [B, k_in, V] (fp32, fp16 or bf16; last axis dense), score [B, k_in] fp32 and flags [B, k_in] uint8 or
-    None: (token, backptr, score, flags), each [B, k_out] as dba_step writes them.  `out`: four tensors to write to."""
+    None: (token, backptr, score, flags), each [B, k_out] as dba_step writes them.  `out`: four tensors to write to, apart from each other and from what is read."""
     lib = load()
     shape, fmt = logits.shape, _FORMATS.get(logits.dtype)
     if len(shape) != 3 or fmt is None:

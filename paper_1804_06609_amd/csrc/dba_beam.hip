@@ -28,12 +28,6 @@ constexpr size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 constexpr int kMostRows = 1 << 22;          // tokens, or heads of tokens, of one sentence in a call
 constexpr int kMostLength = INT32_MAX - 1023;   // tokens that attention looks at: positions of the tiles behind them are ints, too
 
-bool overlaps(const void *a, size_t a_bytes, const void *b, size_t b_bytes)
-{
-    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-    return x < y + b_bytes && y < x + a_bytes;
-}
-
 int launched(const char *who, hipError_t e)
 {
     return e == hipSuccess ? DBA_OK : set_error(DBA_EHIP, "%s: launch failed: %s", who, hipGetErrorString(e));
@@ -216,11 +210,21 @@ DBA_API int dba_beam_select(int B, int k_in, int k_out, int V, int eos_id, int p
         return set_error(DBA_EINVAL, "dba_beam_select: workspace_dev must be 256-byte aligned");
     if (workspace_bytes < plan.total)
         return set_error(DBA_ENOMEM, "dba_beam_select: workspace has %zu bytes, %zu needed", workspace_bytes, plan.total);
-    const size_t rows_in = (size_t)B * k_in, rows_out = (size_t)B * k_out;
-    const struct { const void *at; size_t bytes; } outs[] = {{out_token_dev, rows_out * 4}, {out_backptr_dev, rows_out * 4}, {out_score_dev, rows_out * 4}, {out_flags_dev, rows_out}};
-    for (const auto &o : outs)
-        if (overlaps(o.at, o.bytes, score_dev, rows_in * 4) || (flags_dev && overlaps(o.at, o.bytes, flags_dev, rows_in)))
+    // the new beam is written while the old one is still read, its arrays and the workspace while each other are
+    const int64_t rows_in = (int64_t)B * k_in, rows_out = (int64_t)B * k_out, e = elem_bytes(logits_format);
+    const Places score(score_dev, rows_in * 4), flags(flags_dev, flags_dev ? rows_in : 0);
+    const Places logits = Places(logits_dev, V * e).axis(B, sent_stride * e).axis(k_in, row_stride * e), room(workspace_dev, (int64_t)plan.total);
+    const Places outs[] = {{out_token_dev, rows_out * 4}, {out_backptr_dev, rows_out * 4}, {out_score_dev, rows_out * 4}, {out_flags_dev, rows_out}};
+    for (const Places &o : outs)
+        if (meet(o, score) || meet(o, flags))
             return set_error(DBA_EINVAL, "dba_beam_select: the new beam lies in the old one's scores or flags");
+    for (const Places &o : outs) {
+        if (meet(o, logits)) return set_error(DBA_EINVAL, "dba_beam_select: the new beam lies in the logits");
+        if (meet(o, room)) return set_error(DBA_EINVAL, "dba_beam_select: the new beam lies in the workspace");
+        for (const Places *other = outs; other != &o; ++other)
+            if (meet(o, *other)) return set_error(DBA_EINVAL, "dba_beam_select: two arrays of the new beam overlap");
+    }
+    if (meet(room, score) || meet(room, flags) || meet(room, logits)) return set_error(DBA_EINVAL, "dba_beam_select: an input lies in the workspace");
     SelectParams p;
     p.score = score_dev;
     p.flags = flags_dev;
@@ -241,9 +245,9 @@ DBA_API int dba_beam_select(int B, int k_in, int k_out, int V, int eos_id, int p
     p.eos = eos_id;
     p.pad = pad_id;
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    const hipError_t e = logits_format == DBA_LOGP_F32 ? select_launch<0>(p, B, logits_dev, stream)
-                       : logits_format == DBA_LOGP_F16 ? select_launch<1>(p, B, logits_dev, stream) : select_launch<2>(p, B, logits_dev, stream);
-    return launched("dba_beam_select", e);
+    const hipError_t done = logits_format == DBA_LOGP_F32 ? select_launch<0>(p, B, logits_dev, stream)
+                          : logits_format == DBA_LOGP_F16 ? select_launch<1>(p, B, logits_dev, stream) : select_launch<2>(p, B, logits_dev, stream);
+    return launched("dba_beam_select", done);
 }
 
 DBA_API int dba_beam_reorder(int B, int k, const int32_t *backptr_dev, const dba_state *states_host, int n_states, void *hip_stream)
