@@ -101,9 +101,9 @@ typedef struct dba_heads {
  * pair j of the rot_dim first elements turns by the angle position * inv_freq[j], computed in 64 bits.  Pairs are
  * (j, j + rot_dim/2), or with interleaved != 0 (2j, 2j + 1).  Elements from rot_dim on are taken over as they are.  The rotation
  * is done in fp32 and rounded once.  Tokens outside [0, max_pages * page_size) or in a page that is not there are not written.
- *   k, v          the new tokens, heads as the cache's
- *   q, q_out      optional (both NULL or none): queries [B, n, q_heads, head_dim], rotated alike into q_out (which may be q);
- *                 rows from count[b] on become 0
+ *   k, v          the new tokens, heads as the cache's (they may lie in the pools, but not in places that this call writes)
+ *   q, q_out      optional (both NULL or none): queries [B, n, q_heads, head_dim], rotated alike into q_out (which may be q, and else has no
+ *                 byte in common with q, k and v); rows from count[b] on become 0
  *   first_dev     device [B] int32
  *   count_dev     device [B] int32; NULL: n everywhere
  *   position_dev  device [B, n] int32; NULL: first[b] + i
@@ -120,6 +120,7 @@ DBA_API int dba_cache_append(int B, int n, const dba_cache *cache, const dba_hea
  * the last n tokens of a chain).  A node that sees nothing gets 0 and a normaliser of -inf.
  *   q, out         [B, n, q_heads, head_dim]; q_heads a multiple of the cache's heads; n * q_heads <= 2^22, and B * heads times the
  *                  sixteens of n * q_heads / heads at most 2^28
+ *                  out may be q, and else has no byte in common with it; nor has it, or out_lse_dev, with places that are read, with each other or the workspace
  *   prefix_dev, tree_dev   device [B] int32; negative ones count as 0; tree_dev may be NULL (0 everywhere)
  *   mask_dev       device [B, n, mask_words] uint64, or NULL
  *   max_len        no sentence sees tokens from max_len on (at most max_pages * page_size and 2^31 - 1024); the launch is laid out for it

@@ -108,6 +108,22 @@ Paged paged_of(const dba_cache &c)
     return p;
 }
 
+// What a tensor [B, n, heads, head_dim], and a pool of pages, take up.
+Places places_of(const dba_heads &h, int B, int n, int heads, const dba_cache &c)
+{
+    const int64_t e = elem_bytes(c.format);
+    return Places(h.data, c.head_dim * e).axis(B, h.sent_stride * e).axis(n, h.token_stride * e).axis(heads, h.head_stride * e);
+}
+Places places_of(const void *pool, const dba_cache &c)
+{
+    const int64_t e = elem_bytes(c.format);
+    return Places(pool, c.head_dim * e).axis(c.n_pages, c.page_stride * e).axis(c.page_size, c.token_stride * e).axis(c.heads, c.head_stride * e);
+}
+bool same(const dba_heads &a, const dba_heads &b)
+{
+    return a.data == b.data && a.sent_stride == b.sent_stride && a.token_stride == b.token_stride && a.head_stride == b.head_stride;
+}
+
 HeadsAt heads_of(const dba_heads *h)
 {
     if (!h) return HeadsAt{nullptr, 0, 0, 0};
@@ -369,6 +385,14 @@ DBA_API int dba_cache_append(int B, int n, const dba_cache *cache, const dba_hea
     if (!first_dev) return set_error(DBA_EINVAL, "dba_cache_append: first_dev is NULL");
     if (rot_dim < 0 || rot_dim > cache->head_dim || rot_dim % 16) return set_error(DBA_EINVAL, "dba_cache_append: rot_dim must be a multiple of 16, at most head_dim");
     if (rot_dim && !inv_freq_dev) return set_error(DBA_EINVAL, "dba_cache_append: inv_freq_dev is NULL");
+    if (!places_of(cache->k, *cache).nested()) return set_error(DBA_EINVAL, "dba_cache_append: tokens of the cache overlap");
+    if (q) {
+        const Places to = places_of(*q_out, B, n, q_heads, *cache);
+        if (!to.nested()) return set_error(DBA_EINVAL, "dba_cache_append: pieces of q_out overlap");
+        if ((!same(*q, *q_out) && meet(to, places_of(*q, B, n, q_heads, *cache))) || meet(to, places_of(*k, B, n, cache->heads, *cache)) ||
+            meet(to, places_of(*v, B, n, cache->heads, *cache)))
+            return set_error(DBA_EINVAL, "dba_cache_append: q_out overlaps k, v or a part of q");
+    }
     AppendParams p;
     p.cache = paged_of(*cache);
     p.k_pages = static_cast<unsigned char *>(cache->k);
@@ -421,6 +445,12 @@ DBA_API int dba_tree_attend(int B, int n, int q_heads, const dba_heads *q, const
         if (!workspace_dev || misaligned(workspace_dev, 256)) return set_error(DBA_EINVAL, "dba_tree_attend: workspace_dev must be 256-byte aligned");
         if (workspace_bytes < need) return set_error(DBA_ENOMEM, "dba_tree_attend: workspace has %zu bytes, %zu needed", workspace_bytes, need);
     }
+    const Places to = places_of(*out, B, n, q_heads, *cache), from = places_of(*q, B, n, q_heads, *cache);
+    const Places lse(out_lse_dev, out_lse_dev ? (int64_t)B * n * q_heads * 4 : 0), room(workspace_dev, (int64_t)need);
+    if (!to.nested()) return set_error(DBA_EINVAL, "dba_tree_attend: pieces of out overlap");
+    if (!same(*q, *out) && meet(to, from)) return set_error(DBA_EINVAL, "dba_tree_attend: out overlaps a part of q");
+    if (meet(lse, to) || meet(lse, from)) return set_error(DBA_EINVAL, "dba_tree_attend: out_lse_dev lies in out or q");
+    if (meet(room, to) || meet(room, from) || meet(room, lse)) return set_error(DBA_EINVAL, "dba_tree_attend: q, out or out_lse_dev lies in the workspace");
     AttendParams p;
     p.cache = paged_of(*cache);
     p.k_pages = static_cast<const unsigned char *>(cache->k);

@@ -1,7 +1,10 @@
 """-m "not gpu": calls of the operators whose tensors share memory that is written are refused before the device is touched."""
+import ctypes
+
 import pytest
 
-from test_beam_ops_cpu import AT, _refused, _reorder, _select, _state
+from paper_1804_06609_amd import beam
+from test_beam_ops_cpu import AT, _append, _cache, _heads, _refused, _reorder, _select, _state
 
 MB = 1 << 20
 FAR = AT + 64 * MB
@@ -48,3 +51,35 @@ APART = dict(logits=FAR, rs=104, ss=500, score=AT, flags=AT + 4096, tok=AT + (1 
 ])
 def test_select_refuses_what_shares_memory(kw, frag):
     _refused(_select(**{**APART, **kw}), frag)
+
+
+# 2 sentences of 3 tokens of 8 query heads (4 of the cache's) of 64 in bf16: 8192, 1024 and 64 elements between them
+POOL = _cache(k=AT + 512 * MB, v=AT + 600 * MB)
+
+
+def _tensor(i, **kw):
+    return _heads(data=FAR + i * MB, **kw)
+
+
+@pytest.mark.parametrize("kw,frag", [
+    (dict(cache=_cache(page_stride=0)), "tokens of the cache"), (dict(cache=_cache(token_stride=0)), "tokens of the cache"), (dict(cache=_cache(head_stride=56)), "tokens of the cache"),
+    (dict(q_out=_tensor(3, s=0)), "pieces of q_out"), (dict(q_out=_tensor(3, t=0)), "pieces of q_out"), (dict(q_out=_tensor(3, h=56)), "pieces of q_out"),
+    (dict(q_out=_heads(data=FAR + 2 * MB + 16)), "overlaps"), (dict(q_out=_tensor(0)), "overlaps"), (dict(q_out=_heads(data=FAR + MB + 16384)), "overlaps"),
+    (dict(q_out=_heads(data=FAR + 2 * MB - 2 * 10240 + 128)), "overlaps"),
+])
+def test_append_refuses_what_shares_memory(kw, frag):
+    _refused(_append(**{**dict(cache=POOL, k=_tensor(0), v=_tensor(1), q=_tensor(2), q_out=_tensor(3)), **kw}), frag)
+
+
+@pytest.mark.parametrize("kw,frag", [
+    (dict(out=_tensor(3, s=0)), "pieces of out"), (dict(out=_tensor(3, t=0)), "pieces of out"), (dict(out=_tensor(3, h=56)), "pieces of out"),
+    (dict(out=_heads(data=FAR + 2 * MB + 16)), "part of q"), (dict(out=_tensor(2, t=512)), "part of q"), (dict(out=_tensor(9, s=0)), "pieces of out"),
+    (dict(lse=FAR + 2 * MB), "out_lse_dev"), (dict(lse=FAR + 3 * MB + 1024 * 2 * 2 + 1020), "out_lse_dev"),
+    (dict(ws=FAR + 2 * MB), "workspace"), (dict(ws=FAR + 3 * MB + 256), "workspace"), (dict(lse=FAR + 20 * MB), "workspace"),
+])
+def test_attend_refuses_what_shares_memory(kw, frag):
+    """Of one head of 10000 tokens, which takes a workspace."""
+    cache = _cache(k=AT + 512 * MB, v=AT + 600 * MB, max_pages=4096, table_stride=4096)
+    a = {**dict(q=_tensor(2), out=_tensor(3), lse=FAR + 4 * MB, ws=FAR + 20 * MB), **kw}
+    r = ctypes.byref
+    _refused(beam.load().dba_tree_attend(2, 3, 8, r(a["q"]), r(cache), AT, AT, AT, 1, 10000, 0.125, r(a["out"]), a["lse"], a["ws"], 1 << 40, None), frag)
