@@ -104,14 +104,39 @@ __device__ __forceinline__ uint32_t finite_of(uint32_t w)
     }
 }
 
-// The same of a chunk; true if there were any.
 template <int FMT>
-__device__ __forceinline__ bool make_finite(u32x4 &c)
+__device__ __forceinline__ u32x4 finite_of(u32x4 c)
 {
-    const u32x4 f = u32x4{finite_of<FMT>(c.x), finite_of<FMT>(c.y), finite_of<FMT>(c.z), finite_of<FMT>(c.w)};
-    const bool found = f.x != c.x || f.y != c.y || f.z != c.z || f.w != c.w;
-    c = f;
-    return found;
+    return u32x4{finite_of<FMT>(c.x), finite_of<FMT>(c.y), finite_of<FMT>(c.z), finite_of<FMT>(c.w)};
+}
+
+// Where the exponent of an element of `w` is all ones, so that it is not finite, the bit of its sign is set (others may be, too).
+template <int FMT> constexpr uint32_t kSignBits = FMT == 0 ? 0x80000000u : 0x80008000u;
+template <int FMT>
+__device__ __forceinline__ uint32_t not_finite(uint32_t w)
+{
+    constexpr uint32_t E = FMT == 0 ? 0x7F800000u : FMT == 1 ? 0x7C007C00u : 0x7F807F80u, LEAST = FMT == 0 ? 0x00800000u : FMT == 1 ? 0x04000400u : 0x00800080u;
+    return (w & E) + LEAST;
+}
+
+// Elements as what they do to a sum: 1 for an infinity, 128 for a negative one, 129 for a NaN, 0 for all else.  Of up to 64 elements, a sum of these tells
+// what theirs is.
+template <int FMT>
+__device__ __forceinline__ uint32_t effect_of(uint32_t w)
+{
+    if constexpr (FMT == 0) {
+        const float x = __uint_as_float(w);
+        return __float_as_uint(x != x ? 129.0f : x == INFINITY ? 1.0f : x == -INFINITY ? 128.0f : 0.0f);
+    } else {
+        constexpr uint32_t E = FMT == 1 ? 0x7C00u : 0x7F80u, ONE = FMT == 1 ? 0x3C00u : 0x3F80u, MANY = FMT == 1 ? 0x5800u : 0x4300u, BOTH = FMT == 1 ? 0x5808u : 0x4301u;
+        auto half = [](uint32_t h) { return (h & E) != E ? 0u : (h & 0x7FFFu) != E ? BOTH : h >> 15 ? MANY : ONE; };
+        return half(w & 0xFFFFu) | half(w >> 16) << 16;
+    }
+}
+__device__ __forceinline__ float sum_of_effects(float effects)
+{
+    const uint32_t n = (uint32_t)effects;
+    return n == 0 ? 0.0f : n < 128 ? INFINITY : n & 127 ? NAN : -INFINITY;
 }
 
 // Over a wave, without a trip through LDS.
@@ -205,7 +230,7 @@ __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) vo
     extern __shared__ __align__(16) unsigned char s_mem[];
     __shared__ float s_ml[4][16 * QT][2];
     __shared__ unsigned long long s_live[2][4];
-    __shared__ int s_bad;
+    __shared__ int s_bad[2][4];
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int c = lane & 15, g = lane >> 4;
     const uint32_t id = blockIdx.y * gridDim.x + blockIdx.x, turn = id / 8;
@@ -273,8 +298,7 @@ __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) vo
         const int pos = (u >= prefix_tiles ? span.prefix + (u - prefix_tiles) * TT : u * TT) + load0 + t * 16 + c;
         return (int64_t)page * p.cache.page_stride + (int64_t)(pos & ((1 << p.cache.page_shift) - 1)) * p.cache.token_stride + head_at;
     };
-    bool bad = false;                                  // this lane has met a value that is not finite
-    if (threadIdx.x == 0) s_bad = 0;
+    bool met = false;                                  // this wave has met a value of the tree that is not finite
     u32x4 kr[NT][KS][FC], vr[NT][KS][FC];
     // a chunk behind the head's end is read as its first: the queries have 0 there, and nobody asks for those outputs
     auto load = [&](const unsigned char *pool, u32x4 (&to)[KS][FC], int64_t at) {
@@ -286,6 +310,17 @@ __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) vo
                 const int d = k * 32 + g * 8 + f * NE;
                 to[k][f] = *reinterpret_cast<const u32x4 *>(src + (d < p.D ? d : 0));
             }
+    };
+
+    auto any_not_finite = [&](const u32x4 (&v)[KS][FC]) {      // of a wave's 16 tokens
+        uint32_t bits = 0;
+#pragma unroll
+        for (int k = 0; k < KS; ++k)
+#pragma unroll
+            for (int f = 0; f < FC; ++f)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) bits |= not_finite<FMT>(v[k][f][i]);
+        return __any((bits & kSignBits<FMT>) != 0);
     };
 
     // which rows see which tokens of tile u (bit t: token t)
@@ -330,8 +365,7 @@ __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) vo
     for (int u = first; u < u1; u += step) {
         const bool in_tree = u >= prefix_tiles;
         unsigned char *const kb = s_mem + buf * A::TILE, *const vb = s_v + (ROWS ? buf * A::TILE : 0);
-        // this wave's tokens of the tile: values into LDS, where those that are not there, and in the tree what is not finite,
-        // become 0 (a weight of 0 would not keep them out of the product)
+        // this wave's tokens of the tile: values into LDS, where those that are not there, and in the tree what is not finite, become 0
         unsigned long long live = 0;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
@@ -344,11 +378,12 @@ __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) vo
                     for (int f = 0; f < FC; ++f)
                         if (page[t] < 0) vr[t][k][f] = u32x4{0, 0, 0, 0};
             }
-            if (in_tree) {
+            if (in_tree && any_not_finite(vr[t])) {
+                met = true;
 #pragma unroll
                 for (int k = 0; k < KS; ++k)
 #pragma unroll
-                    for (int f = 0; f < FC; ++f) bad |= make_finite<FMT>(vr[t][k][f]);
+                    for (int f = 0; f < FC; ++f) vr[t][k][f] = finite_of<FMT>(vr[t][k][f]);
             }
 #pragma unroll
             for (int k = 0; k < KS; ++k)
@@ -423,7 +458,7 @@ __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) vo
                 for (int i = 0; i < 4; ++i) top = fmaxf(top, s[t][j][i]);
             top = fmaf(max_over_groups(top), sl2, -kWeightBits<FMT>);
             if (__any(top > m[j] + kWeightRoom<FMT>)) {
-                const float m1 = fmaxf(m[j], top);
+                const float m1 = top > m[j] + kWeightRoom<FMT> ? top : m[j];       // (a row's own: what others of the wave see is nothing to it)
                 const float keep = m1 == m[j] ? 1.0f : __builtin_amdgcn_exp2f(m[j] - m1);
                 m[j] = m1;
                 l[j] *= keep;
@@ -480,6 +515,109 @@ __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) vo
         if constexpr (ROWS) {
             if (A::BUFS == 1) __syncthreads();
             else buf ^= 1;
+        }
+    }
+
+    // Values of the tree that are not finite have been left out, since a weight of 0 would not keep them out of a product.  Whatever its weight, such a
+    // value makes an element of the rows that see it an infinity or a NaN.  So where there were any, the tree's tiles are gone through once more, their values as
+    // what they do to a sum, times 1 where they are seen.  (16 prompts of 500 to 2000 tokens asked for as 2000, 32 heads on 8 of 128 in bf16: 0.96 ms with zeros
+    // behind them, 1.45 to 1.56 with infinities, NaN or any bits.)
+    if constexpr (ROWS) {
+        if (lane == 0) s_bad[0][wave] = met;
+        __syncthreads();                               // (and nobody reads the last tiles any more)
+        met = __builtin_amdgcn_readfirstlane(s_bad[0][0] | s_bad[0][1] | s_bad[0][2] | s_bad[0][3]);
+    }
+    if (__builtin_expect(met, 0)) {
+        constexpr uint32_t ONE = FMT == 1 ? 0x3C00u : 0x3F80u;     // in 16 bits
+        // (What is used here is worked out anew: registers in which it were kept are wanted by the loop above.  32 drafts of 63 nodes 130 -> 122 us.)
+        const int lane1 = (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0)), c1 = lane1 & 15, g1 = lane1 >> 4;
+        for (int u = first + (max(prefix_tiles - first, 0) + step - 1) / step * step; u < u1; u += step) {
+            unsigned long long live = 0;
+            bool bad = false;
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const int x = (u - prefix_tiles) * TT + load0 + t * 16 + c1;
+                const int64_t at = x < tree ? token_offset(p.cache, b, span.prefix + x) : -1;
+                const E *src = reinterpret_cast<const E *>(p.v_pages) + (max(at, (int64_t)0) + head_at);
+                live |= (__ballot(at >= 0) & 0xFFFF) << (load0 + t * 16);
+                u32x4 v[KS][FC];
+#pragma unroll
+                for (int k = 0; k < KS; ++k)
+#pragma unroll
+                    for (int f = 0; f < FC; ++f) {
+                        const int d = k * 32 + g1 * 8 + f * NE;
+                        v[k][f] = *reinterpret_cast<const u32x4 *>(src + (d < p.D ? d : 0));
+                    }
+#pragma unroll
+                for (int k = 0; k < KS; ++k)
+#pragma unroll
+                    for (int f = 0; f < FC; ++f) {
+                        if (at < 0) v[k][f] = u32x4{0, 0, 0, 0};
+                        *reinterpret_cast<u32x4 *>(s_v + A::value_at(load0 + t * 16 + c1, (k * 4 + g1) * FC + f)) = v[k][f];
+                    }
+                bad |= any_not_finite(v);
+            }
+            if constexpr (ROWS) {
+                if (lane1 == 0) {
+                    s_live[0][wave] = live;
+                    s_bad[1][wave] = bad;
+                }
+                __syncthreads();
+                live = s_live[0][0] | s_live[0][1] | s_live[0][2] | s_live[0][3];
+                bad = __builtin_amdgcn_readfirstlane(s_bad[1][0] | s_bad[1][1] | s_bad[1][2] | s_bad[1][3]);
+            }
+            if (bad) {
+                unsigned long long sees[QT];
+                const int j0 = (u - prefix_tiles) * TT;
+#pragma unroll
+                for (int j = 0; j < QT; ++j) {
+                    const int node = min(row0 + j * 16 + c1, rows - 1) / G, last = tree_all - p.n + node - j0;
+                    const unsigned long long *words = p.mask + ((int64_t)b * p.n + node) * p.mask_words;
+                    sees[j] = live & (p.mask ? ((j0 >> 6) < p.mask_words ? words[j0 >> 6] >> (j0 & 63) : 0) : last < 0 ? 0 : last >= 63 ? ~0ull : (2ull << last) - 1);
+                }
+#pragma unroll
+                for (int d = 0; d < DT; ++d) {
+                    f32x4 e[QT];
+#pragma unroll
+                    for (int j = 0; j < QT; ++j) e[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 1
+                    for (int t = 0; t < CT; t += FMT == 0 ? 1 : 2) {
+                        if constexpr (FMT == 0) {
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const uint32_t x = *reinterpret_cast<const uint32_t *>(s_v + A::value_at(t * 16 + 4 * g1 + i, d * 4 + (c1 >> 2)) + (c1 & 3) * 4);
+#pragma unroll
+                                for (int j = 0; j < QT; ++j)
+                                    e[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(effect_of<FMT>(x)), (sees[j] >> (t * 16 + g1 * 4 + i)) & 1 ? 1.0f : 0.0f, e[j], 0, 0, 0);
+                            }
+                        } else {
+                            typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+                            struct { i16x4 lo, hi; } v;
+                            const int token = t * 16 + 4 * g1 + (c1 >> 2), in = (c1 & 3) * 8;
+                            v.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(s_v + A::value_at(token, d * 2 + (in >> 4)) + (in & 15)));
+                            v.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(s_v + A::value_at(token + 16, d * 2 + (in >> 4)) + (in & 15)));
+                            Frag<FMT> vf, w;
+                            vf.c[0] = __builtin_bit_cast(u32x4, v);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) vf.c[0][i] = effect_of<FMT>(vf.c[0][i]);
+#pragma unroll
+                            for (int j = 0; j < QT; ++j) {
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) {
+                                    const uint32_t two = (uint32_t)(sees[j] >> ((t + i / 2) * 16 + g1 * 4 + i % 2 * 2));
+                                    w.c[0][i] = (two & 1 ? ONE : 0) | (two & 2 ? ONE << 16 : 0);
+                                }
+                                e[j] = mfma32<FMT>(vf, w, e[j]);
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int j = 0; j < QT; ++j)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) o[j][d][i] += sum_of_effects(e[j][i]);
+                }
+            }
+            if constexpr (ROWS) __syncthreads();
         }
     }
 
@@ -574,31 +712,6 @@ __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) vo
             }
         }
     }
-
-    // Values of the tree that are not finite have been left out.  Whatever its weight, such a value makes an element of the rows that
-    // see it an infinity or a NaN: those elements are written once more.  (Slow, and only where there is one.)
-    if (__any(bad) && lane == 0) s_bad = 1;
-    __syncthreads();
-    if (!s_bad) return;
-    const int t0 = max(0, u0 - prefix_tiles) * TT, t1 = min(tree, (u1 - prefix_tiles) * TT);
-    const int r0 = row_tile * p.tile_rows, r1 = min(rows, r0 + p.tile_rows);
-    for (int hd = head0; hd < head0 + SIDE; ++hd)
-        for (int x = (int)threadIdx.x; x < (r1 - r0) * p.D; x += 256) {
-            const int r = r0 + x / p.D, e = x % p.D, node = r / G;
-            float v = 0.0f;
-            for (int t = t0; t < t1; ++t) {
-                if (p.mask ? (t >> 6) >= p.mask_words || !((p.mask[((int64_t)b * p.n + node) * p.mask_words + (t >> 6)] >> (t & 63)) & 1)
-                           : t > tree_all - p.n + node)
-                    continue;
-                const int64_t at = token_offset(p.cache, b, (int64_t)span.prefix + t);
-                if (at < 0) continue;
-                const float y = (float)reinterpret_cast<const E *>(p.v_pages)[at + (int64_t)hd * p.cache.head_stride + e];
-                if (!(fabsf(y) < INFINITY)) v += y;
-            }
-            if (v == 0.0f) continue;
-            if (!whole) p.part_o[(part_of(hd) + r) * p.D + e] = v;
-            else reinterpret_cast<E *>(p.out.data)[(int64_t)b * p.out.sent + (int64_t)node * p.out.token + (int64_t)(hd * G + r % G) * p.out.head + e] = (E)v;
-        }
 }
 
 // Joins the parts of a row: 2^(m_s - m) O_s and 2^(m_s - m) l_s added up over its parts s.  Of a part, a lane takes four elements, and as many parts

@@ -1,8 +1,11 @@
 """-m gpu: attention over a tree at the edges of what it accepts.  Tolerances are those of test_gpu_beam_ops.py."""
+import math
+
+import numpy as np
 import pytest
 import torch
 
-from test_gpu_beam_ops import TYPES, a_cache, beam, gen, near, plain_attend  # noqa: F401
+from test_gpu_beam_ops import TYPES, a_cache, beam, gen, near, plain_attend, random_mask  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 MOST = 2**31 - 1
@@ -35,3 +38,97 @@ def test_attend_into_its_queries(beam, dtype, B, n, Hq, Hkv, D, length):  # noqa
     got, lse2 = beam.attend(q[:, :, 1:-1], *args, out=q[:, :, 1:-1], return_lse=True)
     assert torch.equal(q[:, :, 1:-1], want) and torch.equal(lse, lse2) and got.data_ptr() == q[:, :, 1:-1].data_ptr()
     assert torch.equal(q[:, :, 0], kept[:, :, 0]) and torch.equal(q[:, :, -1], kept[:, :, -1])
+
+
+INF, NAN = math.inf, math.nan
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("B,n,Hq,Hkv,D,prefix,tree,masked", [
+    (2, 3, 2, 2, 64, 20, 90, True), (2, 1, 4, 4, 8, 0, 300, False), (2, 20, 4, 2, 64, 65, 200, True), (2, 50, 2, 2, 64, 3, 120, True), (1, 90, 4, 2, 64, 70, 250, False),
+    (2, 8, 4, 2, 128, 5, 150, True), (1, 50, 2, 2, 128, 40, 130, True), (2, 70, 4, 1, 128, 30, 200, True), (1, 130, 3, 3, 80, 0, 130, False),
+    (2, 5, 4, 2, 256, 33, 100, True), (1, 70, 4, 2, 256, 9, 140, False), (130, 2, 8, 8, 64, 3, 40, True), (1, 6, 1, 1, 96, 10, 3000, True)])
+def test_attend_values_that_are_not_finite(beam, dtype, B, n, Hq, Hkv, D, prefix, tree, masked):  # noqa: F811
+    """Elements of the tree's values, here and there, are infinities or NaN: an element of a node is what the sum of those it sees is, and
+    as good as ever if it sees none."""
+    page, rng = 8, np.random.RandomState(n + D)
+    k_pages, v_pages, table = a_cache(3, B, prefix + tree, Hkv, D, page, dtype)
+    q = torch.randn(B, n, Hq, D, generator=gen(4)).to(dtype).cuda()
+    mask, bits = random_mask(5, B, n, -(-tree // 64), 0.3)
+    sees = lambda b, i, j: bits[b, i, j] if masked else j <= tree - n + i
+    p, t = (torch.full((B,), x, dtype=torch.int32) for x in (prefix, tree))
+    clean = v_pages.clone()
+    effect = np.zeros((2, B, n, Hkv, D), bool)                            # an infinity is seen; a negative one
+    for b in range(B):
+        for _ in range(12):
+            j, h, d, x = rng.randint(tree), rng.randint(Hkv), rng.randint(D), (INF, -INF, NAN)[rng.randint(3)]
+            at = int(table[b, (prefix + j) // page]), (prefix + j) % page, h, d
+            if not torch.isfinite(v_pages[at]):
+                continue
+            clean[at], v_pages[at] = 0, x
+            for i in range(n):
+                if sees(b, i, j):
+                    effect[0, b, i, h, d] |= x != -INF
+                    effect[1, b, i, h, d] |= x != INF
+    out, lse, tol, lse_tol = plain_attend(q, k_pages, clean, table, p, t, sees, D ** -0.5)
+    got, got_lse = beam.attend(q, k_pages, v_pages, table.cuda(), p.cuda(), t.cuda(), mask.cuda() if masked else None, return_lse=True)
+    plus, minus = (torch.from_numpy(e).repeat_interleave(Hq // Hkv, dim=2) for e in effect)
+    assert (plus | minus).any() and not (plus | minus).all()
+    g = got.cpu().double()
+    assert torch.equal(torch.isnan(g), plus & minus) and torch.equal(g == INF, plus & ~minus) and torch.equal(g == -INF, minus & ~plus)
+    near(torch.where(plus | minus, 0.0, g), got_lse, (torch.where(plus | minus, 0.0, out), lse, tol, lse_tol))
+
+
+def ragged_prompt(dtype, B, n, Hq, Hkv, D, page, fill):
+    """Prompts of n / 4 to n tokens, all asked for as n: behind each is `fill`, or None: whatever bits."""
+    lens = torch.linspace(n // 4, n, B).int()
+    k_pages, _, table = a_cache(6, B, n, Hkv, D, page, dtype)
+    k_pages = k_pages.contiguous()
+    place = torch.full((len(k_pages), page), True)
+    for b in range(B):
+        for t in range(int(lens[b])):
+            place[table[b, t // page], t % page] = False
+    place = place[:, :, None, None].expand(k_pages.shape).cuda()
+    if fill is None:
+        bits = torch.randint(0, 256, (k_pages.numel() * k_pages.element_size(),), dtype=torch.uint8, generator=gen(7)).cuda().view(dtype).reshape(k_pages.shape)
+        k_pages = torch.where(place, bits, k_pages)
+    else:
+        k_pages = k_pages.masked_fill(place, fill)
+    q = torch.randn(B, n, Hq, D, generator=gen(8)).to(dtype).cuda()
+    zero, whole = torch.zeros(B, dtype=torch.int32), torch.full((B,), n, dtype=torch.int32)
+    return lens, (q, k_pages, k_pages, table.cuda(), zero.cuda(), whole.cuda())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("Hq,Hkv,D", [(4, 2, 64), (4, 1, 128)])
+def test_attend_of_a_ragged_prompt_with_anything_behind_it(beam, dtype, Hq, Hkv, D):  # noqa: F811
+    """The nodes of a sentence's own tokens come out bit for bit as where zeros lie behind them."""
+    lens, args = ragged_prompt(dtype, 3, 200, Hq, Hkv, D, 16, 0.0)
+    want, want_lse = beam.attend(*args, max_len=200, return_lse=True)
+    assert torch.isfinite(want).all()
+    for fill in (NAN, INF, -INF, None):
+        _, other = ragged_prompt(dtype, 3, 200, Hq, Hkv, D, 16, fill)
+        got, lse = beam.attend(*other, max_len=200, return_lse=True)
+        for b in range(3):
+            m = int(lens[b])
+            assert torch.equal(got[b, :m], want[b, :m]) and torch.equal(lse[b, :m], want_lse[b, :m]), (fill, b)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_attend_of_a_ragged_prompt_takes_no_longer_for_what_lies_behind_it(beam, dtype):  # noqa: F811
+    """A tile of 64 tokens that holds such values takes a few times as long; a walk over its tokens for every element took 70 times."""
+    times = {}
+    for fill in (0.0, NAN, INF, None):
+        _, args = ragged_prompt(dtype, 4, 400, 8, 2, 64, 16, fill)
+        best = math.inf
+        for _ in range(5):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            beam.attend(*args, max_len=400)
+            a.record()
+            for _ in range(5):
+                beam.attend(*args, max_len=400)
+            b.record()
+            b.synchronize()
+            best = min(best, a.elapsed_time(b))
+        times[fill] = best
+    assert all(t <= 8 * times[0.0] for t in times.values()), times
