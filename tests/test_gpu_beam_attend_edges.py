@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 import torch
 
-from test_gpu_beam_ops import TYPES, a_cache, beam, gen, near, plain_attend, random_mask  # noqa: F401
+from test_gpu_beam_ops import TYPES, U, U32, a_cache, beam, gen, near, plain_attend, random_mask, rows_of  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 MOST = 2**31 - 1
@@ -132,3 +132,27 @@ def test_attend_of_a_ragged_prompt_takes_no_longer_for_what_lies_behind_it(beam,
             best = min(best, a.elapsed_time(b))
         times[fill] = best
     assert all(t <= 8 * times[0.0] for t in times.values()), times
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("B,n,Hq,Hkv,D,length", [(2, 5, 8, 4, 64, 400), (2, 16, 4, 2, 64, 300), (2, 16, 4, 2, 128, 300), (1, 1, 4, 4, 128, 6000), (2, 3, 6, 2, 80, 500), (2, 4, 8, 2, 256, 300),
+                                                 (140, 2, 8, 8, 64, 40)])
+def test_attend_of_few_rows_is_rounded_once(beam, dtype, B, n, Hq, Hkv, D, length):  # noqa: F811
+    """Up to 32 rows a head (16 of 256): the weights' rounding does not show.  With u the type's half step, A = sum p |v| and e the scores' error (test_gpu_beam_ops.py):
+    the result is off by u |o|, and a weight by u^2 of itself, 4 e, 2^-20 and the sum's L u32."""
+    k_pages, v_pages, table = a_cache(1, B, length, Hkv, D, 16, dtype)
+    q = torch.randn(B, n, Hq, D, generator=gen(2)).to(dtype).cuda()
+    got = beam.attend(q, k_pages, v_pages, table.cuda(), torch.full((B,), length, dtype=torch.int32).cuda()).cpu().double()
+    u, scale, kp, vp = U[dtype], D ** -0.5, k_pages.cpu(), v_pages.cpu()
+    off = mean = 0.0
+    for b in range(B):
+        k, v = rows_of(kp, table, b, length), rows_of(vp, table, b, length)
+        for h in range(Hq):
+            x, kk, vv = q[b, :, h].cpu().double(), k[:, h * Hkv // Hq], v[:, h * Hkv // Hq]
+            p = (x @ kk.T * scale).softmax(dim=1)
+            want = p @ vv
+            e = (D + 8) * U32 * (x.abs() @ kk.abs().T).amax(dim=1, keepdim=True) * scale
+            tol = u * want.abs() + (p @ vv.abs()) * (u * u + 4 * e + 2.0 ** -20 + length * U32)
+            assert ((got[b, :, h] - want).abs() <= tol).all(), float(((got[b, :, h] - want).abs() - tol).max())
+            off, mean = off + float((got[b, :, h] - want).square().sum()), mean + float((want.to(dtype).double() - want).square().sum())
+    assert off <= 1.05 ** 2 * mean                                      # as far from it as its own rounding
