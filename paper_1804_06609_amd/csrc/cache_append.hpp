@@ -27,7 +27,7 @@ constexpr int kAppendThreads = 256;
 
 // cos and sin of position * inv_freq.  The angle in turns is formed and reduced in 64 bits: a position of a million leaves an fp32
 // angle no better than 0.06 radians.
-__device__ __forceinline__ float2 turn_of(int position, float inv_freq)
+__device__ __forceinline__ float2 turn_of(int64_t position, float inv_freq)
 {
     const double turns = (double)position * ((double)inv_freq * 0.159154943091895335768883763);
     const float x = (float)(2.0 * (turns - rint(turns)));      // in half turns
@@ -59,7 +59,7 @@ __global__ __launch_bounds__(kAppendThreads) void dba_append_kernel(AppendParams
     const int b = (int)blockIdx.y, i = (int)blockIdx.x, t = (int)threadIdx.x, T = (int)blockDim.x;
     const bool there = !p.count || i < p.count[b];
     const int64_t at = (int64_t)p.first[b] + i;
-    const int position = p.position ? p.position[(int64_t)b * p.n + i] : (int)at;
+    const int64_t position = p.position ? p.position[(int64_t)b * p.n + i] : at;       // (first + i may pass 2^31: such a token has no place, but a query)
     const int64_t slot = there ? token_offset(p.cache, b, at) : -1;
     const int chunks = p.D / N, pairs = (chunks + 1) / 2, half = p.rot / 2, heads = p.q_heads + 2 * p.heads;
     const int items = heads * pairs;
