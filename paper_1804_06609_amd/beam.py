@@ -4,7 +4,8 @@
 cache, rotated on the way) and `attend` (a tree's nodes over that cache).  All enqueue their work on the current stream of
 the current device, where their tensors have to be, and return without waiting; workspaces come from torch's allocator on that
 stream.  A tensor that was made on another stream is the caller's to wait for, as with any torch operator.
-Nothing of the methods runs here, and there is no fallback: without the built library the calls raise.  None has a gradient.
+Nothing of the methods runs here, and there is no fallback: without the built library the calls raise.  None has a gradient, and
+inputs that require one are refused where torch would record it.
 """
 from __future__ import annotations
 
@@ -53,6 +54,7 @@ def _pack_states(fields: int):
 
 
 _F32, _I32, _U8, _empty_like, _CONTIGUOUS = torch.float32, torch.int32, torch.uint8, torch.empty_like, torch.contiguous_format
+_grad_enabled = torch.is_grad_enabled
 _FORMATS = {torch.float32: _b.DBA_LOGP_F32, torch.float16: _b.DBA_LOGP_F16, torch.bfloat16: _b.DBA_LOGP_BF16}
 
 _lib = None
@@ -73,6 +75,11 @@ def load() -> ctypes.CDLL:
 
 def _fail(text: str):
     raise _b.DbaError(_b.DBA_EINVAL, text)
+
+
+def _no_gradient():
+    """What came out would be cut off from tensors that require a gradient without a word."""
+    _fail("this operator has no gradient: call it under torch.no_grad(), or on detached tensors")
 
 
 def _stream(x: torch.Tensor) -> int:
@@ -106,6 +113,8 @@ def select(logits: torch.Tensor, score: torch.Tensor, flags: Optional[torch.Tens
     """The new beam from logits [B, k_in, V] (fp32, fp16 or bf16; last axis dense), score [B, k_in] fp32 and flags [B, k_in] uint8 or
     None: (token, backptr, score, flags), each [B, k_out] as dba_step writes them.  `out`: four tensors to write to, apart from each other and from what is read."""
     lib = load()
+    if _grad_enabled() and (logits.requires_grad or score.requires_grad):
+        _no_gradient()
     shape, fmt = logits.shape, _FORMATS.get(logits.dtype)
     if len(shape) != 3 or fmt is None:
         _fail("logits must be [B, k, V] of fp32, fp16 or bf16 with a dense last axis")
@@ -160,13 +169,17 @@ def reorder(backptr: torch.Tensor, states: Sequence[torch.Tensor], out: Optional
     lib = load()
     if backptr.dim() != 2:
         _fail("backptr must be [B, k]")
+    out = states if out is None else out
+    if len(out) != len(states):
+        _fail("as many tensors out as states")
+    if _grad_enabled():
+        for s in states:
+            if s.requires_grad:
+                _no_gradient()
     B, k = backptr.shape
     stream = _stream(backptr)
     device = backptr.get_device()
     back = _ints("backptr", backptr, backptr.shape, device)
-    out = states if out is None else out
-    if len(out) != len(states):
-        _fail("as many tensors out as states")
     table = []                                         # the fields of dba_state, one state after another
     rows = B * k or 1
     for s, d in zip(states, out):
@@ -232,6 +245,8 @@ def append(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: tor
     int32, or first[b] + i) and inv_freq (fp32; None: no rotation).  q [B, n, q_heads, head_dim] is rotated alike into q_out (a new
     tensor if None; q itself is allowed), which is returned."""
     lib = load()
+    if _grad_enabled() and (k.requires_grad or v.requires_grad or (q is not None and q.requires_grad) or (inv_freq is not None and inv_freq.requires_grad)):
+        _no_gradient()
     stream = _stream(k)
     shape, dtype, device = k.shape, k.dtype, k.get_device()
     if len(shape) != 4:
@@ -268,6 +283,8 @@ def attend(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, table:
     the last n tokens of a chain.  scale: head_dim ** -0.5 if None.  max_len: no sentence has more tokens (the table's capacity
     if None; a close bound makes a better launch).  Returns out, or (out, lse [B, n, q_heads] fp32)."""
     lib = load()
+    if _grad_enabled() and (q.requires_grad or k_pages.requires_grad or v_pages.requires_grad):
+        _no_gradient()
     stream = _stream(q)
     shape, dtype, device = q.shape, q.dtype, q.get_device()
     if len(shape) != 4:
