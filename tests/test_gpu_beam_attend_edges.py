@@ -156,3 +156,25 @@ def test_attend_of_few_rows_is_rounded_once(beam, dtype, B, n, Hq, Hkv, D, lengt
             assert ((got[b, :, h] - want).abs() <= tol).all(), float(((got[b, :, h] - want).abs() - tol).max())
             off, mean = off + float((got[b, :, h] - want).square().sum()), mean + float((want.to(dtype).double() - want).square().sum())
     assert off <= 1.05 ** 2 * mean                                      # as far from it as its own rounding
+
+
+@pytest.mark.parametrize("B,heads", [(2000, 33), (2100, 64)])
+def test_attend_in_more_workgroups_than_one_axis_takes(beam, B, heads):  # noqa: F811
+    """One token a sentence and head, one or two heads a workgroup: more than 65536 of them."""
+    D, page, most = 8, 16, 16
+    lens = torch.randint(0, most + 1, (B,), generator=gen(1), dtype=torch.int32)
+    pages = torch.randn(2, B, page, heads, D, generator=gen(2)).bfloat16()
+    table = torch.randperm(B, generator=gen(3)).int()[:, None]
+    q = torch.randn(B, 1, heads, D, generator=gen(4)).bfloat16()
+    got, lse = beam.attend(q.cuda(), pages[0].cuda(), pages[1].cuda(), table.cuda(), lens.cuda(), return_lse=True)
+    k, v = (p[table[:, 0].long()].double().transpose(1, 2) for p in pages)      # [B, heads, page, D]
+    x = (k * q.double().transpose(1, 2)).sum(dim=3) * D ** -0.5
+    x = x.masked_fill(torch.arange(page)[None, None] >= lens[:, None, None], -INF)
+    want_lse = x.logsumexp(dim=2)
+    p = (x - want_lse.clamp(min=-1e30)[..., None]).exp()
+    want, room = (p[..., None] * v).sum(dim=2), (p[..., None] * v.abs()).sum(dim=2)
+    e = (D + 8) * U32 * float((k.abs() * q.double().abs().transpose(1, 2)).sum(dim=3).max()) * D ** -0.5
+    tol = U[torch.bfloat16] * want.abs() + room * (U[torch.bfloat16] + 4 * e + 2.0 ** -20 + most * U32)
+    assert ((got[:, 0].cpu().double() - want).abs() <= tol).all()
+    seen = want_lse > -INF
+    assert torch.equal(lse[:, 0].cpu() > -INF, seen) and ((lse[:, 0].cpu().double() - want_lse)[seen].abs() <= 2 * e + 2.0 ** -20 + most * U32 + U32 * want_lse[seen].abs()).all()

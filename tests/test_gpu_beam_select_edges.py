@@ -68,3 +68,30 @@ def test_equal_rows_go_by_their_order(beam, dtype, V, k, k_out):  # noqa: F811
         room = torch.full((6, k, ld + lead), math.nan, dtype=dtype)
         room[:, :, lead:lead + V] = logits
         check_select(beam, logits, score, None, k_out, room.cuda()[:, :, lead:lead + V])
+
+
+def best_of_many(logits, score, k_out):
+    """(token, backptr, score) of one sentence in 64 bits, without a sort of everything."""
+    x = logits.double()
+    s = (torch.log_softmax(x, dim=1) + score.double()[:, None]).flatten().numpy()
+    at = np.nonzero(s >= np.partition(s, len(s) - k_out)[len(s) - k_out])[0]
+    at = at[np.lexsort((at, -s[at]))][:k_out]
+    return at % logits.shape[1], at // logits.shape[1], s[at]
+
+
+@pytest.mark.parametrize("k_out", [1, 40, 64])
+def test_select_from_more_parts_than_the_second_launch_holds(beam, k_out):  # noqa: F811
+    """64 rows of 17 parts; in the second sentence every part has the same best, and most rows are equal."""
+    k, V = 64, 152000
+    logits = torch.randn(2, k, V, generator=gen(1)) * 2
+    logits[1] = -1.0
+    logits[1, :, ::1000] = 3.0
+    score = -torch.rand(2, k, generator=gen(2)) * 4 - 5
+    score[1] = -5.0
+    score[1, :6] = -9.0
+    got = [x.cpu().numpy() for x in beam.select(logits.cuda(), score.cuda(), None, k_out, 2, 0)]
+    for b in range(2):
+        token, back, s = best_of_many(logits[b], score[b], k_out)
+        assert np.array_equal(got[0][b], token) and np.array_equal(got[1][b], back), b
+        assert (np.abs(got[2][b] - s) <= np.abs(s) * U32 + 2.0 ** -22).all()
+        assert np.array_equal(got[3][b], (token == 2).astype(np.uint8))
