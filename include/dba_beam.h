@@ -68,7 +68,8 @@ typedef struct dba_state {
  * dst[b, h] = src[b, backptr[b, h]] for every state; a back-pointer outside [0, k) (an empty slot has -1) clears the row.
  * In place, rows that stay where they are are neither read nor written.  dst and src of one state are the same or have no byte in common,
  * pieces of dst do not overlap each other, and no state's dst has a byte in common with another state's dst or src: the states are
- * moved at the same time.  (Views of one tensor that interleave are apart.  Where they interleave in different strides, more than 65536 times, they count as overlapping.)
+ * moved at the same time.  (Views of one tensor that interleave are apart.  Where they interleave in different strides, more than
+ * 65536 times, they count as overlapping.)
  *   backptr_dev  device [B,k] int32 (as dba_step or dba_beam_select wrote it); must not lie in a dst
  *   states_host  host [n_states] (copied before the call returns)
  */
@@ -120,13 +121,16 @@ DBA_API int dba_cache_append(int B, int n, const dba_cache *cache, const dba_hea
  * the last n tokens of a chain).  A node that sees nothing gets 0 and a normaliser of -inf.
  *   q, out         [B, n, q_heads, head_dim]; q_heads a multiple of the cache's heads; n * q_heads <= 2^22, and B * heads times the
  *                  sixteens of n * q_heads / heads at most 2^28
- *                  out may be q, and else has no byte in common with it; nor has it, or out_lse_dev, with places that are read, with each other or the workspace
+ *                  out may be q, and else has no byte in common with it; nor has it, or out_lse_dev, with places that are read, with
+ *                  each other or with the workspace
  *   prefix_dev, tree_dev   device [B] int32; negative ones count as 0; tree_dev may be NULL (0 everywhere)
  *   mask_dev       device [B, n, mask_words] uint64, or NULL
  *   max_len        no sentence sees tokens from max_len on (at most max_pages * page_size and 2^31 - 1024); the launch is laid out for it
  *   out_lse_dev    device [B, n, q_heads] fp32: log of the sum of the exponentials; may be NULL
  *   workspace_dev  device, 256-byte aligned, at least dba_tree_attend_workspace_bytes bytes (which may be 0)
- * What masked places, and places behind the end, hold never matters, NaN and infinities included.
+ * What masked places, and places behind the end, hold never matters, NaN and infinities included.  Where a token is seen, an element of
+ * its values that is not finite makes that element of the node's output an infinity or a NaN, whatever its weight, and a key that is
+ * not finite may make all of them NaN.
  */
 DBA_API size_t dba_tree_attend_workspace_bytes(int B, int n, int q_heads, const dba_cache *cache, int max_len);
 DBA_API int dba_tree_attend(int B, int n, int q_heads, const dba_heads *q, const dba_cache *cache, const int32_t *prefix_dev,

@@ -32,7 +32,7 @@ struct SelectParams {
 
 constexpr int kSelectThreads = 256;    // of the first launch
 // 16-byte chunks a thread keeps in registers: as many as 64 registers have room for, since a workgroup's chain of barriers takes 9 us however much it has read
-// (rows of 50000 in 16 bits in three parts instead of four: 158 -> 135 us; with ten registers spill)
+// (when this was chosen, rows of 50000 in 16 bits in three parts instead of four: 158 -> 135 us; with ten registers spill)
 constexpr int kSelectChunks = 9;
 constexpr int kSelectQueue = 256;      // chunks it looks through for keys
 constexpr int kSelectKeys = 1024;      // keys it chooses from
@@ -174,7 +174,8 @@ __device__ __forceinline__ uint32_t bound_of_kth(const uint32_t (&r)[J], int k, 
 // One part of one row.  Bound: HBM (the logits are read once), and with 16 bits the VALU nearly: an element takes five
 // instructions, one of them the exponential.  So nothing else is done element by element: addresses are the same for a whole wave
 // but for its lanes' 16 bytes, the end of a row that does not fill a chunk are single elements of the first wave, and of the chunks only those that
-// reach the bar are looked through (128 x 64 rows of 50000 in bf16: 135 us, 6.1 TB/s; 64 x 20 of 32000 in fp32: 25 us, 6.6 TB/s).
+// reach the bar are looked through (128 x 64 rows of 50000 in bf16, 86 % of which are read: 138 to 155 us from run to run, 5.1 to 4.6 TB/s;
+// all of them: 148 to 168, 5.5 to 4.9; 64 x 20 of 32000 in fp32, 87 %: 25.4 us, 5.6 TB/s, all: 27.8, 5.9 TB/s).
 template <int FMT>
 __global__ __launch_bounds__(kSelectThreads, 8) void dba_select_part_kernel(const void *logits, SelectParams p)
 {
@@ -416,7 +417,7 @@ __device__ __forceinline__ double double_from_ord(u64 o)
 }
 
 // One sentence: normalisers, then the k_out best of what its rows' parts have handed on.  Bound: latency, a chain of loads and barriers through
-// code that no other launch has left in the instruction cache (5 us for 5 lists, 9.4 for 80, 18 for 256 with k_out = 64).
+// code that no other launch has left in the instruction cache (4.7 us for 5 lists, 9.1 for 80, 18.5 for 192 with k_out = 64).
 template <int T>
 __global__ __launch_bounds__(T) void dba_select_sentence_kernel(SelectParams p)
 {

@@ -136,10 +136,10 @@ HeadsAt heads_of(const dba_heads *h)
 // 182 and 184 with shared tiles).  The token axis is cut into as many parts as fill the GPU once: each part costs a start-up of several
 // trips to memory, and twice as many were slower (one sentence of 29000 tokens 59 against 43 us, five of 21600 56 against 39),
 // but for shared tiles, whose sentences' lengths matter more than that.  There the first part of a sentence has a quarter more than an even share, so that
-// fewer sentences have rows to join and what comes last is short (32 sentences of 500 to 4000 tokens, 63 nodes of 32 heads: 127 us; even parts
+// fewer sentences have rows to join and what comes last is short (when this was chosen, 32 sentences of 500 to 4000 tokens, 63 nodes of 32 heads: 127 us; even parts
 // 144, half as much again 135, one part a sentence 147, three 153).  Parts have four tiles at least, three with heads of 256, or joining costs more than
 // they save (11 sentences of 930 tokens, 32 nodes, parts of 1, 2, 4, 8 tiles: 34, 28, 25, 29 us; one of 4000 tokens, fp32: 82, 83, 59, 93).
-// Two heads a workgroup (SIDE) halve the workgroups: 1024 heads of 64 in two rounds of 512 or in one 83 and 75 us, of 128 81 and 74, 1024 of 256 in four rounds or
+// Two heads a workgroup (SIDE) halve the workgroups, then: 1024 heads of 64 in two rounds of 512 or in one 83 and 75 us, of 128 81 and 74, 1024 of 256 in four rounds or
 // two 122 and 116, 2048 of 32 66 and 62; but 1200 of 80, in three rounds or in two of which the second is nearly empty, 75 and 82, and 512 of 128, which then need
 // parts to fill the GPU, 110 and 117.
 AttendPlan attend_plan(int B, int n, int q_heads, const dba_cache &c, int max_len)

@@ -229,16 +229,16 @@ struct AttendShape {
 };
 
 // Bound: without ROWS memory; each token is read once.  A pool with the heads of a token side by side gives 128 or 256 bytes at a time (64 sentences of
-// 20 branches, heads of 64: 68 us, 4.7 TB/s; 4 of 57000 tokens, heads of 128: 187 us, 5.0 TB/s), one with a head's tokens side by side
-// more (the second 172 us).  With ROWS the issue slots: a tile of 64 tokens and 32 rows of 128 takes a wave 64 matrix instructions
-// and 350 others (32 sentences of 500 to 4000 tokens, 63 nodes of 32 heads: 122 us, 0.6 PFLOP/s of fp16).
+// 20 branches, heads of 64: 65.7 us, 4.8 TB/s; 4 of 57000 tokens, heads of 128: 186 us, 5.1 TB/s), one with a head's tokens side by side
+// more (the second and its join 172 us instead of 193).  With ROWS the issue slots: a tile of 64 tokens and 32 rows of 128 takes a wave 64 matrix instructions
+// and 340 others of the VALU (32 sentences of 500 to 4000 tokens, 63 nodes of 32 heads: 125 us, 0.6 PFLOP/s of fp16).
 //
 // SIDE: heads of a workgroup.  With two, waves 0 and 2 have the first, 1 and 3 the second: a longer stretch of memory where the heads of a token lie
-// side by side, and twice the tiles a wave for the same start and end (83 -> 75 us in the first case above; four heads 106).
+// side by side, and twice the tiles a wave for the same start and end (when this was chosen, a call of the first case above took 83 -> 75 us, with four heads 106).
 //
 // Workgroups come to the eight XCDs in turn.  The row tiles of one part of one head, which read the same tokens, are put behind each
 // other on one XCD, whose L2 then serves all but the first (63 nodes, 8 query heads to one, 32 sentences of 500 to 4000 tokens:
-// 225 -> 140 us).  There the parts of the token axis vary slowest, so that what is left of short sentences comes last; where
+// 225 -> 140 us when this was chosen).  There the parts of the token axis vary slowest, so that what is left of short sentences comes last; where
 // tokens are read once they vary fastest (4 sentences of 50000 and more: 186 instead of 199 us).
 template <int FMT, int DP, int QT, bool ROWS, int SIDE>
 __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) void dba_attend_kernel(AttendParams p)
