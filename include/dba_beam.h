@@ -6,6 +6,13 @@
  *   dba_cache_append    new keys and values into a paged cache, rotated by their position on the way
  *   dba_tree_attend     attention of the nodes of a tree of hypotheses (or of drafted tokens) over that cache
  *
+ * and, for long prompts,
+ *
+ *   dba_cache_append_normed   appending with norms of queries and keys by head, and positions of several axes
+ *   dba_shared_attend         attention behind a prefix that all sentences of a batch have in common
+ *   dba_cache_weigh           how much attention each cached token has had
+ *   dba_cache_evict           the tokens that had the most stay, in other pages
+ *
  * The cache of a sentence holds its shared prefix and, behind it, every token that any hypothesis has generated; what a
  * hypothesis sees of those is a row of mask bits (its ancestors).  So the cache never moves when the beam is
  * reordered: dba_beam_reorder moves the mask rows, and recurrent states where a decoder has them.
@@ -136,6 +143,85 @@ DBA_API size_t dba_tree_attend_workspace_bytes(int B, int n, int q_heads, const 
 DBA_API int dba_tree_attend(int B, int n, int q_heads, const dba_heads *q, const dba_cache *cache, const int32_t *prefix_dev,
                             const int32_t *tree_dev, const uint64_t *mask_dev, int mask_words, int max_len, float scale,
                             const dba_heads *out, float *out_lse_dev, void *workspace_dev, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * dba_cache_append with queries and keys normed by head before they are rotated, and with positions of several axes.  With norms
+ *     y = x / sqrt(mean x^2 + eps) * weight
+ * over the head_dim elements of each head of q and of k (an L2 norm is this one with weights of head_dim ** -0.5); the rotation turns y, all in fp32, squares
+ * added up in 64 bits, and the result is rounded once.  Without norms (NULL) the results are those of dba_cache_append.
+ *   norms        host, may be NULL
+ *   position_dev device [B, n, axes] int32; NULL (axis_dev is NULL then): first[b] + i
+ *   axis_dev     device [rot_dim / 2] int32: pair j turns by position[.., axis[j]] * inv_freq[j], and not at all where axis[j] lies outside [0, axes);
+ *                NULL: axes is 1, which all pairs go by
+ * All else is as for dba_cache_append.
+ */
+typedef struct dba_norms {
+    const void *q_weight, *k_weight; /* device, 16-byte aligned: head_dim elements for each head, or for all; NULL: 1 */
+    int64_t q_stride, k_stride;      /* elements between the weights of heads, a multiple of 16 bytes; 0: one for all heads */
+    int format;                      /* of the weights: the cache's or DBA_LOGP_F32 */
+    float eps;                       /* at least 1e-37 */
+} dba_norms;
+
+DBA_API int dba_cache_append_normed(int B, int n, const dba_cache *cache, const dba_heads *k, const dba_heads *v, int q_heads, const dba_heads *q,
+                                    const dba_heads *q_out, const dba_norms *norms, const int32_t *first_dev, const int32_t *count_dev,
+                                    const int32_t *position_dev, int axes, const int32_t *axis_dev, const float *inv_freq_dev, int rot_dim,
+                                    int interleaved, void *hip_stream);
+
+/*
+ * dba_tree_attend of sentences that have their first tokens in common: every node sees the shared_len[0] first tokens of the pages of
+ * shared_table, and behind them what dba_tree_attend lets it see of its sentence's own cache.  The common tokens are read for all sentences
+ * together; their pages lie in the same pools.
+ *   shared_table_dev  device [shared_pages] int32 (shared_pages * page_size < 2^31)
+ *   shared_len_dev    device [1] int32; a negative one counts as 0
+ *   max_shared        no common tokens are seen from here on (1 to shared_pages * page_size and 2^31 - 1024); the launch is laid out for it
+ *   workspace_dev     device, 256-byte aligned, at least dba_shared_attend_workspace_bytes bytes (0: the arguments are refused)
+ * B * n * q_heads <= 2^26.  All else is as for dba_tree_attend; what is said there of values that are not finite holds for the common tokens, too.
+ */
+DBA_API size_t dba_shared_attend_workspace_bytes(int B, int n, int q_heads, const dba_cache *cache, int shared_pages, int max_shared, int max_len);
+DBA_API int dba_shared_attend(int B, int n, int q_heads, const dba_heads *q, const dba_cache *cache, const int32_t *shared_table_dev, int shared_pages,
+                              const int32_t *shared_len_dev, int max_shared, const int32_t *prefix_dev, const int32_t *tree_dev,
+                              const uint64_t *mask_dev, int mask_words, int max_len, float scale, const dba_heads *out, float *out_lse_dev,
+                              void *workspace_dev, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * out[b, s, t] = score[b, s, t] + sum exp(scale * q[b, i, h] . k[b, t, h / (q_heads / heads)] - lse[b, i, h]) over the nodes i < min(n, count[b]) that see
+ * token t, as dba_tree_attend says, and over the query heads h that share head s of the cache (by_head != 0), or all (s is 0 only).  With the normalisers of
+ * dba_tree_attend or dba_shared_attend the summands are attention weights.  Sums are fp32, in a fixed order.  A node's head whose lse is not finite
+ * adds nothing.  Tokens that are not there, behind the sentence's end or from max_len on keep their score.
+ *   q, prefix_dev, tree_dev, mask_dev, mask_words, scale, n, q_heads   as for dba_tree_attend; cache->v is not read
+ *   lse_dev      device [B, n, q_heads] fp32
+ *   count_dev    device [B] int32; NULL: n everywhere
+ *   max_len      1 to max_pages * page_size, at most width
+ *   score_dev, out_dev  device [B, 1 or heads, width] fp32 with strides between sentences and heads, last axis dense; width <= 2^28.  out_dev may be
+ *                score_dev (same strides), and else has no byte in common with it, q, lse_dev or mask_dev
+ */
+DBA_API int dba_cache_weigh(int B, int n, int q_heads, const dba_heads *q, const float *lse_dev, const dba_cache *cache, const int32_t *prefix_dev,
+                            const int32_t *tree_dev, const uint64_t *mask_dev, int mask_words, const int32_t *count_dev, int max_len, float scale,
+                            int by_head, const float *score_dev, int64_t score_sent, int64_t score_head, float *out_dev, int64_t out_sent,
+                            int64_t out_head, int width, void *hip_stream);
+
+/*
+ * Of the prefix[b] first tokens of a sentence's cache, stay = min(keep, budget[b], as many as are there) are taken over into the pages of a new table, and
+ * behind them the tree[b] ones that follow, all in their order; the sentence's cache is then new_table with new_prefix[b] = stay and the same tree.  The first
+ * `sinks` and the last `recent` of the prefix go before all others; among either kind the greater score goes first, of equal ones the
+ * lower place, a NaN behind all numbers.  With by_head each head of the cache chooses its own tokens (they then lie side by side with others than before).
+ * Tokens in pages that are not there do not stay; tokens that a new page is missing for are not written, nor are places of the tree whose old page is missing.
+ * The old pages stay as they were.  A page of new_table must not be one that is read, nor be there twice; else what the new pages hold is undefined.
+ *   new_table_dev   device [B, new_max_pages] int32 with a stride between sentences; new_max_pages * page_size < 2^31
+ *   score_dev       device [B, 1 or heads, width] fp32 as for dba_cache_weigh; max_len <= width <= 2^28
+ *   prefix_dev, tree_dev   device [B] int32; negative ones count as 0, tree_dev may be NULL; tokens from max_len on are not there
+ *   keep            at least 1
+ *   budget_dev      device [B] int32, negative ones count as 0; NULL: keep everywhere
+ *   new_prefix_dev  device [B] int32
+ *   new_score_dev   device [B, 1 or heads, width] fp32: the scores of the tokens at their new places, 0 behind them; may be NULL
+ *   workspace_dev   device, 256-byte aligned, at least dba_cache_evict_workspace_bytes bytes (0: the arguments are refused)
+ * No result has a byte in common with another, the workspace or what is read.
+ */
+DBA_API size_t dba_cache_evict_workspace_bytes(int B, const dba_cache *cache, int by_head, int keep, int max_len);
+DBA_API int dba_cache_evict(int B, const dba_cache *cache, const int32_t *new_table_dev, int64_t new_table_stride, int new_max_pages, int by_head,
+                            const float *score_dev, int64_t score_sent, int64_t score_head, const int32_t *prefix_dev, const int32_t *tree_dev, int keep,
+                            const int32_t *budget_dev, int sinks, int recent, int max_len, int32_t *new_prefix_dev, float *new_score_dev,
+                            int64_t new_sent, int64_t new_head, int width, void *workspace_dev, size_t workspace_bytes, void *hip_stream);
 
 #ifdef __cplusplus
 }

@@ -1,8 +1,9 @@
 """The operators of include/dba_beam.h on torch tensors: marshalling and device-memory plumbing only.
 
 `select` (the new beam from logits), `reorder` (states follow the back-pointers), `append` (keys and values into a paged
-cache, rotated on the way) and `attend` (a tree's nodes over that cache).  All enqueue their work on the current stream of
-the current device, where their tensors have to be, and return without waiting; workspaces come from torch's allocator on that
+cache, normed and rotated on the way), `attend` (a tree's nodes over that cache), `attend_shared` (the same behind a prefix that the
+whole batch has in common), `weigh` (how much attention each cached token has had) and `evict` (those that had the most
+stay, in other pages).  All enqueue their work on the current stream of the current device, where their tensors have to be, and return without waiting; workspaces come from torch's allocator on that
 stream.  A tensor that was made on another stream is the caller's to wait for, as with any torch operator.
 Nothing of the methods runs here, and there is no fallback: without the built library the calls raise.  None has a gradient, and
 inputs that require one are refused where torch would record it.
@@ -42,10 +43,23 @@ _SIGNATURES = {
     "dba_cache_append": (_I, [_I, _I, _P, _P, _P, _I] + [_P] * 6 + [_I, _I, _P]),
     "dba_tree_attend_workspace_bytes": (_Z, [_I, _I, _I, _P, _I]),
     "dba_tree_attend": (_I, [_I, _I, _I] + [_P] * 5 + [_I, _I, ctypes.c_float] + [_P] * 3 + [_Z, _P]),
+    "dba_cache_append_normed": (_I, [_I, _I, _P, _P, _P, _I] + [_P] * 6 + [_I, _P, _P, _I, _I, _P]),
+    "dba_shared_attend_workspace_bytes": (_Z, [_I, _I, _I, _P, _I, _I, _I]),
+    "dba_shared_attend": (_I, [_I, _I, _I, _P, _P, _P, _I, _P, _I, _P, _P, _P, _I, _I, ctypes.c_float] + [_P] * 3 + [_Z, _P]),
+    "dba_cache_weigh": (_I, [_I, _I, _I] + [_P] * 6 + [_I, _P, _I, ctypes.c_float, _I, _P, _L, _L, _P, _L, _L, _I, _P]),
+    "dba_cache_evict_workspace_bytes": (_Z, [_I, _P, _I, _I, _I]),
+    "dba_cache_evict": (_I, [_I, _P, _P, _L, _I, _I, _P, _L, _L, _P, _P, _I, _P, _I, _I, _I, _P, _P, _L, _L, _I, _P, _Z, _P]),
 }
+
+
+class _Norms(ctypes.Structure):
+    _fields_ = [("q_weight", _P), ("k_weight", _P), ("q_stride", _L), ("k_stride", _L), ("format", _I), ("eps", ctypes.c_float)]
+
+
 # the same structures as bytes, which are made in half the time
 _pack_cache = struct.Struct("@3P4q6i").pack
 _pack_heads = struct.Struct("@P3q").pack
+_pack_norms = struct.Struct("@2P2qif").pack
 
 
 @functools.lru_cache(maxsize=256)
@@ -240,11 +254,18 @@ def _heads(name: str, x: torch.Tensor, shape, dtype, device: int) -> bytes:
 
 def append(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor, first: torch.Tensor,
            count: Optional[torch.Tensor] = None, *, position: Optional[torch.Tensor] = None, inv_freq: Optional[torch.Tensor] = None,
-           interleaved: bool = False, q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+           interleaved: bool = False, q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None, axis: Optional[torch.Tensor] = None,
+           eps: Optional[float] = None, q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
     """k, v [B, n, heads, head_dim] become tokens first[b] .. of the cache (count[b] of them, or n), k rotated by its position ([B, n]
     int32, or first[b] + i) and inv_freq (fp32; None: no rotation).  q [B, n, q_heads, head_dim] is rotated alike into q_out (a new
-    tensor if None; q itself is allowed), which is returned."""
+    tensor if None; q itself is allowed), which is returned.
+
+    With axis ([rot_dim / 2] int32) positions are [B, n, axes] and pair j goes by axis[j] of them.  With eps, queries and keys are
+    normed by head before they are rotated: x / sqrt(mean x^2 + eps), times q_weight or k_weight where there is one ([head_dim], or one
+    for each head [heads, head_dim]; of the queries' type or fp32)."""
     lib = load()
+    if axis is not None or eps is not None or q_weight is not None or k_weight is not None:
+        return _append_normed(lib, k, v, k_pages, v_pages, table, first, count, position, inv_freq, interleaved, q, q_out, axis, eps, q_weight, k_weight)
     if _grad_enabled() and (k.requires_grad or v.requires_grad or (q is not None and q.requires_grad) or (inv_freq is not None and inv_freq.requires_grad)):
         _no_gradient()
     stream = _stream(k)
@@ -273,6 +294,72 @@ def append(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: tor
                                    _ints("first", first, (B,), device), _ints("count", count, (B,), device),
                                    _ints("position", position, (B, n), device), freq, rot, interleaved, stream))
     return q_out
+
+
+def _weights(name: str, w: Optional[torch.Tensor], heads: int, D: int, device: int):
+    """(address, elements between heads) of the weights of norms."""
+    if w is None:
+        return 0, 0
+    if w.shape != (D,) and w.shape != (heads, D) or not w.is_contiguous() or w.get_device() != device:
+        _fail(f"{name} must be contiguous, [head_dim] or [heads, head_dim], on the device of the others")
+    return w.data_ptr(), D if w.dim() == 2 and heads > 1 else 0
+
+
+def _append_normed(lib, k, v, k_pages, v_pages, table, first, count, position, inv_freq, interleaved, q, q_out, axis, eps, q_weight, k_weight):
+    """`append` where there are norms, or positions of several axes."""
+    if _grad_enabled() and any(x is not None and x.requires_grad for x in (k, v, q, inv_freq, q_weight, k_weight)):
+        _no_gradient()
+    stream = _stream(k)
+    shape, dtype, device = k.shape, k.dtype, k.get_device()
+    if len(shape) != 4:
+        _fail("k must be [B, n, heads, head_dim]")
+    B, n, heads, D = shape
+    cache = _cache(k_pages, v_pages, table, B, dtype, device)
+    if k_pages.shape[2:] != (heads, D):
+        _fail("k has other heads than the cache")
+    qh = oh = None
+    q_heads = 0
+    if q is not None:
+        if q.dim() != 4:
+            _fail("q must be [B, n, q_heads, head_dim]")
+        q_heads = q.shape[2]
+        if q_out is None:
+            q_out = _empty_like(q, memory_format=_CONTIGUOUS)
+        qh, oh = _heads("q", q, (B, n, q_heads, D), dtype, device), _heads("q_out", q_out, (B, n, q_heads, D), dtype, device)
+    rot, freq, norms, axes = 0, None, None, 1
+    if inv_freq is not None:
+        if inv_freq.dtype is not _F32 or inv_freq.dim() != 1 or not inv_freq.is_contiguous() or inv_freq.get_device() != device:
+            _fail("inv_freq must be a contiguous fp32 tensor [rot_dim / 2]")
+        rot, freq = 2 * inv_freq.shape[0], inv_freq.data_ptr()
+    if axis is not None:
+        if position is None or position.dim() != 3 or inv_freq is None:
+            _fail("axis goes with positions [B, n, axes] and inv_freq")
+        axes = position.shape[2]
+    if eps is not None:
+        kinds = {w.dtype for w in (q_weight, k_weight) if w is not None} or {dtype}
+        kind = kinds.pop()
+        if kinds or (kind is not dtype and kind is not _F32):
+            _fail("weights of norms must be of one type, the queries' or fp32")
+        a, sa = _weights("q_weight", q_weight, q_heads, D, device)
+        c, sc = _weights("k_weight", k_weight, heads, D, device)
+        norms = _pack_norms(a, c, sa, sc, _FORMATS[kind], eps)
+    elif q_weight is not None or k_weight is not None:
+        _fail("weights of norms go with eps")
+    _b._check(lib.dba_cache_append_normed(B, n, cache, _heads("k", k, shape, dtype, device), _heads("v", v, shape, dtype, device), q_heads, qh, oh, norms,
+                                          _ints("first", first, (B,), device), _ints("count", count, (B,), device),
+                                          _ints("position", position, (B, n) if axis is None else (B, n, axes), device), axes,
+                                          _ints("axis", axis, (rot // 2,), device), freq, rot, interleaved, stream))
+    return q_out
+
+
+def _mask(mask: Optional[torch.Tensor], B: int, n: int, device: int):
+    """(words of a node, address, whether there is a mask without a bit)."""
+    if mask is None:
+        return 0, None, False
+    if mask.dtype is not torch.int64 or mask.dim() != 3 or mask.shape[:2] != (B, n) or not mask.is_contiguous() or mask.get_device() != device:
+        _fail("mask must be a contiguous int64 tensor [B, n, words] on the device of the others")
+    words = mask.shape[2]
+    return words, mask.data_ptr() if words else None, not words
 
 
 def attend(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor, prefix: torch.Tensor,
@@ -313,3 +400,121 @@ def attend(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, table:
                                   _ints("tree", tree, (B,), device), bits, words, max_len, D ** -0.5 if scale is None else scale,
                                   _heads("out", out, shape, dtype, device), lse.data_ptr() if return_lse else None, at, nbytes, stream))
     return (out, lse) if return_lse else out
+
+
+def attend_shared(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, shared: torch.Tensor, shared_len: torch.Tensor, table: torch.Tensor,
+                  prefix: torch.Tensor, tree: Optional[torch.Tensor] = None, mask: Optional[torch.Tensor] = None, *, scale: Optional[float] = None,
+                  max_shared: Optional[int] = None, max_len: Optional[int] = None, out: Optional[torch.Tensor] = None, return_lse: bool = False):
+    """`attend` of sentences that have their first tokens in common: every node sees the shared_len ([1] int32) first tokens of the pages
+    `shared` ([pages] int32, of the same pools), read once for the whole batch, and what `attend` lets it see of its sentence's own. max_shared:
+    there are no more common tokens (the pages' capacity if None).  All else is as for `attend`; the normaliser is that of both together."""
+    lib = load()
+    if _grad_enabled() and (q.requires_grad or k_pages.requires_grad or v_pages.requires_grad):
+        _no_gradient()
+    stream = _stream(q)
+    shape, dtype, device = q.shape, q.dtype, q.get_device()
+    if len(shape) != 4:
+        _fail("q must be [B, n, q_heads, head_dim]")
+    B, n, heads, D = shape
+    cache = _cache(k_pages, v_pages, table, B, dtype, device)
+    if k_pages.shape[3] != D:
+        _fail("q has another head_dim than the cache")
+    if shared.dim() != 1:
+        _fail("shared must be [pages]")
+    if out is None:
+        out = _empty_like(q, memory_format=_CONTIGUOUS)
+    words, bits, blind = _mask(mask, B, n, device)
+    if blind:                                              # nothing of the tree is seen
+        tree = None
+    lse = q.new_empty((B, n, heads), dtype=_F32) if return_lse else None
+    page, pages = k_pages.shape[1], shared.shape[0]
+    if max_len is None:
+        max_len = min(table.shape[1] * page, 2**31 - 1024)
+    if max_shared is None:
+        max_shared = min(pages * page, 2**31 - 1024)
+    nbytes = lib.dba_shared_attend_workspace_bytes(B, n, heads, cache, pages, max_shared, max_len)
+    ws, at = _workspace(nbytes, q)
+    _b._check(lib.dba_shared_attend(B, n, heads, _heads("q", q, shape, dtype, device), cache, _ints("shared", shared, shared.shape, device), pages,
+                                    _ints("shared_len", shared_len, (1,), device), max_shared, _ints("prefix", prefix, (B,), device),
+                                    _ints("tree", tree, (B,), device), bits, words, max_len, D ** -0.5 if scale is None else scale,
+                                    _heads("out", out, shape, dtype, device), lse.data_ptr() if return_lse else None, at, nbytes, stream))
+    return (out, lse) if return_lse else out
+
+
+def _scores(name: str, x: torch.Tensor, shape, device: int):
+    """(address, strides of sentences and heads) of fp32 scores [B, 1 or heads, width]."""
+    if x.dtype is not _F32 or x.shape != shape or x.get_device() != device:
+        _fail(f"{name} must be an fp32 tensor {tuple(shape)} on the device of the others")
+    sent, head, one = x.stride()
+    if one != 1 and shape[2] > 1:
+        _fail(f"{name} must have a dense last axis")
+    return x.data_ptr(), sent if shape[0] > 1 else 0, head if shape[1] > 1 else 0
+
+
+def weigh(score: torch.Tensor, q: torch.Tensor, lse: torch.Tensor, k_pages: torch.Tensor, table: torch.Tensor, prefix: torch.Tensor,
+          tree: Optional[torch.Tensor] = None, mask: Optional[torch.Tensor] = None, *, count: Optional[torch.Tensor] = None,
+          scale: Optional[float] = None, max_len: Optional[int] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """score [B, heads, width] (a score for each head of the cache) or [B, 1, width] (one for all), fp32, plus the attention weight that each cached
+    token has from q [B, n, q_heads, head_dim] with normalisers lse [B, n, q_heads], as `attend` or `attend_shared` returned them, of nodes that
+    see it; nodes from count[b] on do not count, nor does a head whose lse is not finite.  In place, or into `out`, which is returned."""
+    lib = load()
+    if _grad_enabled() and (score.requires_grad or q.requires_grad or lse.requires_grad or k_pages.requires_grad):
+        _no_gradient()
+    stream = _stream(q)
+    shape, dtype, device = q.shape, q.dtype, q.get_device()
+    if len(shape) != 4:
+        _fail("q must be [B, n, q_heads, head_dim]")
+    B, n, heads, D = shape
+    cache = _cache(k_pages, k_pages, table, B, dtype, device)
+    kv_heads = k_pages.shape[2]
+    if k_pages.shape[3] != D:
+        _fail("q has another head_dim than the cache")
+    if lse.dtype is not _F32 or lse.shape != (B, n, heads) or not lse.is_contiguous() or lse.get_device() != device:
+        _fail("lse must be a contiguous fp32 tensor [B, n, q_heads] on the device of the others")
+    if score.dim() != 3 or score.shape[1] not in (1, kv_heads):
+        _fail("score must be [B, heads of the cache, width] or [B, 1, width]")
+    rows = (B, score.shape[1], score.shape[2])
+    out = score if out is None else out
+    words, bits, blind = _mask(mask, B, n, device)
+    if blind:
+        tree = None
+    if max_len is None:
+        max_len = min(table.shape[1] * k_pages.shape[1], rows[2])
+    _b._check(lib.dba_cache_weigh(B, n, heads, _heads("q", q, shape, dtype, device), lse.data_ptr(), cache, _ints("prefix", prefix, (B,), device),
+                                  _ints("tree", tree, (B,), device), bits, words, _ints("count", count, (B,), device), max_len,
+                                  D ** -0.5 if scale is None else scale, rows[1] == kv_heads, *_scores("score", score, rows, device),
+                                  *_scores("out", out, rows, device), rows[2], stream))
+    return out
+
+
+def evict(score: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor, new_table: torch.Tensor, prefix: torch.Tensor,
+          tree: Optional[torch.Tensor] = None, *, keep: int, budget: Optional[torch.Tensor] = None, sinks: int = 0, recent: int = 0,
+          max_len: Optional[int] = None, new_score: Optional[torch.Tensor] = None):
+    """Of the prefix[b] first tokens of each sentence's cache min(keep, budget[b]) move into the pages of new_table ([B, pages] int32, other pages of the
+    same pools), and the tree[b] ones behind them: the `sinks` first and the `recent` last ones before all others, then those of the greatest
+    score ([B, heads, width]: each head of the cache chooses its own, or [B, 1, width]), all in their order.  Returns the new prefix [B] int32 and
+    the scores of the tokens at their new places, 0 behind them (new_score, or a new tensor like score)."""
+    lib = load()
+    if _grad_enabled() and (score.requires_grad or k_pages.requires_grad or v_pages.requires_grad):
+        _no_gradient()
+    stream = _stream(score)
+    device = score.get_device()
+    if score.dim() != 3 or k_pages.dim() != 4 or score.shape[1] not in (1, k_pages.shape[2]):
+        _fail("score must be [B, heads of the cache, width] or [B, 1, width]")
+    rows = B, heads, width = tuple(score.shape)
+    cache = _cache(k_pages, v_pages, table, B, k_pages.dtype, device)
+    if new_table.dtype is not _I32 or new_table.dim() != 2 or new_table.shape[0] != B or new_table.stride(1) != 1 or new_table.get_device() != device:
+        _fail("new_table must be an int32 tensor [B, pages] with a dense last axis, on the device of the others")
+    if new_score is None:
+        new_score = _empty_like(score, memory_format=_CONTIGUOUS)
+    new_prefix = prefix.new_empty((B,))
+    by_head = heads == k_pages.shape[2]
+    if max_len is None:
+        max_len = min(table.shape[1] * k_pages.shape[1], width)
+    nbytes = lib.dba_cache_evict_workspace_bytes(B, cache, by_head, keep, max_len)
+    ws, at = _workspace(nbytes, score)
+    _b._check(lib.dba_cache_evict(B, cache, new_table.data_ptr(), new_table.stride(0) if B > 1 else new_table.shape[1], new_table.shape[1], by_head,
+                                  *_scores("score", score, rows, device), _ints("prefix", prefix, (B,), device), _ints("tree", tree, (B,), device), keep,
+                                  _ints("budget", budget, (B,), device), sinks, recent, max_len, new_prefix.data_ptr(),
+                                  *_scores("new_score", new_score, rows, device), width, at, nbytes, stream))
+    return new_prefix, new_score

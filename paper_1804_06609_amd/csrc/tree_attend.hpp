@@ -28,6 +28,7 @@ struct AttendParams {
     int row_tiles, tile_rows;          // workgroups along the rows, rows of each
     int splits, chunk;                 // workgroups along the token axis, tiles of each
     int pairs, groups;                 // sentences times heads, or pairs of them; times splits
+    int per;                           // with PARTS: nodes that q has side by side; the next ones lie a sentence further on
     float scale;
 };
 
@@ -240,7 +241,9 @@ struct AttendShape {
 // other on one XCD, whose L2 then serves all but the first (63 nodes, 8 query heads to one, 32 sentences of 500 to 4000 tokens:
 // 225 -> 140 us when this was chosen).  There the parts of the token axis vary slowest, so that what is left of short sentences comes last; where
 // tokens are read once they vary fastest (4 sentences of 50000 and more: 186 instead of 199 us).
-template <int FMT, int DP, int QT, bool ROWS, int SIDE>
+//
+// PARTS: results are always left as parts, for another join; and the nodes of several sentences may be taken for those of one.
+template <int FMT, int DP, int QT, bool ROWS, int SIDE, bool PARTS = false>
 __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) void dba_attend_kernel(AttendParams p)
 {
     typedef AttendShape<FMT, DP, QT, ROWS> A;
@@ -284,7 +287,8 @@ __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) vo
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
         const int r = row0 + t * 16 + c, node = min(r, rows - 1) / G, h = head * G + min(r, rows - 1) % G;
-        const E *src = reinterpret_cast<const E *>(p.q.data) + ((int64_t)b * p.q.sent + (int64_t)node * p.q.token + (int64_t)h * p.q.head);
+        const int sent = PARTS ? b + node / p.per : b, token = PARTS ? node % p.per : node;
+        const E *src = reinterpret_cast<const E *>(p.q.data) + ((int64_t)sent * p.q.sent + (int64_t)token * p.q.token + (int64_t)h * p.q.head);
         mask_row[t] = p.mask ? p.mask + ((int64_t)b * p.n + node) * p.mask_words : nullptr;
         chain[t] = tree_all - p.n + node;
 #pragma unroll
@@ -650,7 +654,7 @@ __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) vo
     }
 
     // results: [rows, D] of the output, or this split's part
-    const bool whole = tiles <= p.chunk;               // no other part has anything
+    const bool whole = !PARTS && tiles <= p.chunk;     // no other part has anything
     auto part_of = [&](int hd) { return (((size_t)b * p.heads + hd) * p.splits + split) * rows; };
     auto put_row = [&](int hd, int r, float mm, float ll) {        // statistics of a row
         if (!whole) {
