@@ -148,7 +148,7 @@ DBA_API int dba_tree_attend(int B, int n, int q_heads, const dba_heads *q, const
  * dba_cache_append with queries and keys normed by head before they are rotated, and with positions of several axes.  With norms
  *     y = x / sqrt(mean x^2 + eps) * weight
  * over the head_dim elements of each head of q and of k (an L2 norm is this one with weights of head_dim ** -0.5); the rotation turns y, all in fp32, squares
- * added up in 64 bits, and the result is rounded once.  Without norms (NULL) the results are those of dba_cache_append.
+ * added up in 64 bits, and the result is rounded once.  Without norms (NULL) the formula is dba_cache_append's.
  *   norms        host, may be NULL
  *   position_dev device [B, n, axes] int32; NULL (axis_dev is NULL then): first[b] + i
  *   axis_dev     device [rot_dim / 2] int32: pair j turns by position[.., axis[j]] * inv_freq[j], and not at all where axis[j] lies outside [0, axes);
@@ -194,11 +194,13 @@ DBA_API int dba_shared_attend(int B, int n, int q_heads, const dba_heads *q, con
  *   max_len      1 to max_pages * page_size, at most width
  *   score_dev, out_dev  device [B, 1 or heads, width] fp32 with strides between sentences and heads, last axis dense; width <= 2^28.  out_dev may be
  *                score_dev (same strides), and else has no byte in common with it, q, lse_dev or mask_dev
+ *   workspace_dev  device, 256-byte aligned, at least dba_cache_weigh_workspace_bytes bytes (which may be 0); none of these lies in it
  */
+DBA_API size_t dba_cache_weigh_workspace_bytes(int B, int n, int q_heads, const dba_cache *cache, int by_head, int max_len);
 DBA_API int dba_cache_weigh(int B, int n, int q_heads, const dba_heads *q, const float *lse_dev, const dba_cache *cache, const int32_t *prefix_dev,
                             const int32_t *tree_dev, const uint64_t *mask_dev, int mask_words, const int32_t *count_dev, int max_len, float scale,
                             int by_head, const float *score_dev, int64_t score_sent, int64_t score_head, float *out_dev, int64_t out_sent,
-                            int64_t out_head, int width, void *hip_stream);
+                            int64_t out_head, int width, void *workspace_dev, size_t workspace_bytes, void *hip_stream);
 
 /*
  * Of the prefix[b] first tokens of a sentence's cache, stay = min(keep, budget[b], as many as are there) are taken over into the pages of a new table, and

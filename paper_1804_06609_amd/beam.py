@@ -46,7 +46,8 @@ _SIGNATURES = {
     "dba_cache_append_normed": (_I, [_I, _I, _P, _P, _P, _I] + [_P] * 6 + [_I, _P, _P, _I, _I, _P]),
     "dba_shared_attend_workspace_bytes": (_Z, [_I, _I, _I, _P, _I, _I, _I]),
     "dba_shared_attend": (_I, [_I, _I, _I, _P, _P, _P, _I, _P, _I, _P, _P, _P, _I, _I, ctypes.c_float] + [_P] * 3 + [_Z, _P]),
-    "dba_cache_weigh": (_I, [_I, _I, _I] + [_P] * 6 + [_I, _P, _I, ctypes.c_float, _I, _P, _L, _L, _P, _L, _L, _I, _P]),
+    "dba_cache_weigh": (_I, [_I, _I, _I] + [_P] * 6 + [_I, _P, _I, ctypes.c_float, _I, _P, _L, _L, _P, _L, _L, _I, _P, _Z, _P]),
+    "dba_cache_weigh_workspace_bytes": (_Z, [_I, _I, _I, _P, _I, _I]),
     "dba_cache_evict_workspace_bytes": (_Z, [_I, _P, _I, _I, _I]),
     "dba_cache_evict": (_I, [_I, _P, _P, _L, _I, _I, _P, _L, _L, _P, _P, _I, _P, _I, _I, _I, _P, _P, _L, _L, _I, _P, _Z, _P]),
 }
@@ -480,10 +481,13 @@ def weigh(score: torch.Tensor, q: torch.Tensor, lse: torch.Tensor, k_pages: torc
         tree = None
     if max_len is None:
         max_len = min(table.shape[1] * k_pages.shape[1], rows[2])
+    by_head = rows[1] == kv_heads
+    nbytes = 0 if by_head else lib.dba_cache_weigh_workspace_bytes(B, n, heads, cache, by_head, max_len)
+    ws, at = _workspace(nbytes, q)
     _b._check(lib.dba_cache_weigh(B, n, heads, _heads("q", q, shape, dtype, device), lse.data_ptr(), cache, _ints("prefix", prefix, (B,), device),
                                   _ints("tree", tree, (B,), device), bits, words, _ints("count", count, (B,), device), max_len,
-                                  D ** -0.5 if scale is None else scale, rows[1] == kv_heads, *_scores("score", score, rows, device),
-                                  *_scores("out", out, rows, device), rows[2], stream))
+                                  D ** -0.5 if scale is None else scale, by_head, *_scores("score", score, rows, device),
+                                  *_scores("out", out, rows, device), rows[2], at, nbytes, stream))
     return out
 
 

@@ -31,11 +31,24 @@ const char *weights_fault(const void *data, int64_t stride, int format)
     return misaligned(data, 16) || stride < 0 || stride % unit ? "weights of norms and their stride must be multiples of 16 bytes, not negative" : nullptr;
 }
 
-template <int FMT>
-hipError_t normed_launch(const NormedParams &p, bool norm, bool wide, dim3 grid, unsigned threads, hipStream_t stream)
+template <int FMT, int TOKENS, bool INTERLEAVED>
+hipError_t normed_tokens(const NormedParams &p, bool norm, bool wide, int B, unsigned threads, hipStream_t stream)
 {
-    const auto kernel = !norm ? dba_append_normed_kernel<FMT, false, false> : wide ? dba_append_normed_kernel<FMT, true, true> : dba_append_normed_kernel<FMT, true, false>;
-    return launch(kernel, grid, dim3(threads), 0, stream, p);
+    const auto kernel = !norm ? dba_append_normed_kernel<FMT, false, false, TOKENS, INTERLEAVED>
+                      : wide ? dba_append_normed_kernel<FMT, true, true, TOKENS, INTERLEAVED> : dba_append_normed_kernel<FMT, true, false, TOKENS, INTERLEAVED>;
+    return launch(kernel, dim3((unsigned)((p.a.n + TOKENS - 1) / TOKENS), (unsigned)B), dim3(threads), 0, stream, p);
+}
+
+// A wave for each unit where there are few tokens; several tokens a workgroup where that leaves workgroups enough.
+template <int FMT>
+hipError_t normed_launch(const NormedParams &p, bool norm, bool wide, int B, hipStream_t stream)
+{
+    const int units = p.q_units + 2 * p.k_units, most = kNormedThreads / 64, turns = (units + most - 1) / most;
+    const unsigned threads = 64u * (unsigned)((units + turns - 1) / turns);
+    const bool many = (int64_t)p.a.n * B >= 1024 * kNormedTokens && p.a.n >= kNormedTokens;
+    const auto go = p.a.interleaved ? many ? normed_tokens<FMT, kNormedTokens, true> : normed_tokens<FMT, 1, true>
+                                    : many ? normed_tokens<FMT, kNormedTokens, false> : normed_tokens<FMT, 1, false>;
+    return go(p, norm, wide, B, threads, stream);
 }
 
 // ---- attention behind a common prefix ------------------------------------------------------------------------------
@@ -82,16 +95,31 @@ void lay_out(AttendParams &p, const AttendPlan &plan, int B, const dba_cache &c)
 
 // ---- weighing -------------------------------------------------------------------------------------------------------
 
-template <int FMT, int DP>
-hipError_t weigh_one(const WeighParams &p, int B, int tokens, hipStream_t stream)
+// Up to WeighFew::MOST rows a head the waves go through tokens, else through rows.  Of the former a workgroup has as few tokens as fill the GPU
+// (kWeighGroups workgroups), but two tiles a wave at least, and sums that fit into LDS.
+constexpr int kWeighGroups = 3072, kWeighChunk = 2048;
+
+template <int FMT, int DP, bool FULL>
+hipError_t weigh_one(WeighParams p, int B, int tokens, hipStream_t stream)
 {
+    const int rows = p.n * (p.q_heads / p.heads);
+    if (rows <= WeighFew<FMT, DP>::MOST) {
+        constexpr int turn = 4 * WeighFew<FMT, DP>::TF;
+        const int64_t groups = std::max<int64_t>(1, kWeighGroups / ((int64_t)B * p.heads)), even = (tokens + groups - 1) / groups;
+        p.chunk = (int)std::min<int64_t>(kWeighChunk / turn * turn, std::max<int64_t>(2 * turn, (even + turn - 1) / turn * turn));
+        const auto kernel = rows <= 64 || WeighFew<FMT, DP>::MOST <= 64 ? dba_weigh_few_kernel<FMT, DP, FULL, 1> : dba_weigh_few_kernel<FMT, DP, FULL, WeighFew<FMT, DP>::MOST <= 64 ? 1 : 2>;
+        return launch(kernel, dim3((unsigned)((tokens + p.chunk - 1) / p.chunk), (unsigned)p.heads, (unsigned)B), dim3(256),
+                      (size_t)WeighFew<FMT, DP>::lds(rows, p.chunk), stream, p);
+    }
     const unsigned blocks = (unsigned)((tokens + WeighShape<FMT, DP>::TG - 1) / WeighShape<FMT, DP>::TG);
-    return launch(dba_weigh_kernel<FMT, DP>, dim3(blocks, p.by_head ? (unsigned)p.heads : 1u, (unsigned)B), dim3(256), 0, stream, p);
+    return launch(dba_weigh_kernel<FMT, DP, FULL>, dim3(blocks, (unsigned)p.heads, (unsigned)B), dim3(256), 0, stream, p);
 }
 template <int FMT>
 hipError_t weigh_launch(const WeighParams &p, int B, int tokens, hipStream_t stream)
 {
-    return p.D <= 64 ? weigh_one<FMT, 64>(p, B, tokens, stream) : p.D <= 128 ? weigh_one<FMT, 128>(p, B, tokens, stream) : weigh_one<FMT, 256>(p, B, tokens, stream);
+    const auto go = p.D == 64 ? weigh_one<FMT, 64, true> : p.D < 64 ? weigh_one<FMT, 64, false> : p.D == 128 ? weigh_one<FMT, 128, true>
+                  : p.D < 128 ? weigh_one<FMT, 128, false> : p.D == 256 ? weigh_one<FMT, 256, true> : weigh_one<FMT, 256, false>;
+    return go(p, B, tokens, stream);
 }
 
 // Rows of scores [B, heads_s, width].
@@ -176,18 +204,18 @@ DBA_API int dba_cache_append_normed(int B, int n, const dba_cache *cache, const 
     p.kw = WeightsAt{norms ? static_cast<const unsigned char *>(norms->k_weight) : nullptr, norms ? norms->k_stride : 0};
     p.axis = axis_dev;
     p.axes = axes;
-    p.eps = norms ? (double)norms->eps : 0.0;
+    p.eps = norms ? norms->eps : 0.0f;
+    p.per_element = 1.0f / (float)cache->head_dim;
     const int pairs = (p.a.D * (int)elem_bytes(cache->format) / 16 + 1) / 2;
     p.lane_bits = 0;
     while ((1 << p.lane_bits) < pairs) ++p.lane_bits;
     p.lanes = 1 << p.lane_bits;
-    const int64_t items = (int64_t)(p.a.q_heads + 2 * p.a.heads) << p.lane_bits;
-    const unsigned threads = (unsigned)std::min<int64_t>(kAppendThreads, (items + 63) / 64 * 64);
+    p.q_units = ((p.a.q_heads << p.lane_bits) + 63) / 64;
+    p.k_units = ((p.a.heads << p.lane_bits) + 63) / 64;
     const bool wide = norms && norms->format != cache->format;
-    const dim3 grid((unsigned)n, (unsigned)B);
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    const hipError_t e = cache->format == DBA_LOGP_F32 ? normed_launch<0>(p, norms, false, grid, threads, stream)
-                       : cache->format == DBA_LOGP_F16 ? normed_launch<1>(p, norms, wide, grid, threads, stream) : normed_launch<2>(p, norms, wide, grid, threads, stream);
+    const hipError_t e = cache->format == DBA_LOGP_F32 ? normed_launch<0>(p, norms, false, B, stream)
+                       : cache->format == DBA_LOGP_F16 ? normed_launch<1>(p, norms, wide, B, stream) : normed_launch<2>(p, norms, wide, B, stream);
     return launched(who, e);
 }
 
@@ -262,10 +290,16 @@ DBA_API int dba_shared_attend(int B, int n, int q_heads, const dba_heads *q, con
     return launched(who, e);
 }
 
+DBA_API size_t dba_cache_weigh_workspace_bytes(int B, int n, int q_heads, const dba_cache *cache, int by_head, int max_len)
+{
+    if (attend_fault(B, n, q_heads, cache, max_len) || max_len > kMostTokens || by_head || cache->heads == 1) return 0;
+    return align256((size_t)B * cache->heads * max_len * 4);
+}
+
 DBA_API int dba_cache_weigh(int B, int n, int q_heads, const dba_heads *q, const float *lse_dev, const dba_cache *cache, const int32_t *prefix_dev,
                             const int32_t *tree_dev, const uint64_t *mask_dev, int mask_words, const int32_t *count_dev, int max_len, float scale,
                             int by_head, const float *score_dev, int64_t score_sent, int64_t score_head, float *out_dev, int64_t out_sent,
-                            int64_t out_head, int width, void *hip_stream)
+                            int64_t out_head, int width, void *workspace_dev, size_t workspace_bytes, void *hip_stream)
 {
     static const char *const who = "dba_cache_weigh";
     const char *fault = attend_fault(B, n, q_heads, cache, max_len);
@@ -285,6 +319,14 @@ DBA_API int dba_cache_weigh(int B, int n, int q_heads, const dba_heads *q, const
     if (meet(to, places_of(*q, B, n, q_heads, *cache)) || meet(to, Places(lse_dev, (int64_t)B * n * q_heads * 4)) ||
         (mask_dev && meet(to, Places(mask_dev, (int64_t)B * n * mask_words * 8))))
         return set_error(DBA_EINVAL, "%s: out_dev lies in q, lse_dev or mask_dev", who);
+    const size_t need = dba_cache_weigh_workspace_bytes(B, n, q_heads, cache, by_head, max_len);
+    if (need) {
+        if (!workspace_dev || misaligned(workspace_dev, 256)) return set_error(DBA_EINVAL, "%s: workspace_dev must be 256-byte aligned", who);
+        if (workspace_bytes < need) return set_error(DBA_ENOMEM, "%s: workspace has %zu bytes, %zu needed", who, workspace_bytes, need);
+        const Places room(workspace_dev, (int64_t)need);
+        if (meet(room, was) || meet(room, to) || meet(room, places_of(*q, B, n, q_heads, *cache)) || meet(room, Places(lse_dev, (int64_t)B * n * q_heads * 4)))
+            return set_error(DBA_EINVAL, "%s: scores, q or lse_dev lie in the workspace", who);
+    }
     WeighParams p;
     p.cache = paged_of(*cache);
     p.k_pages = static_cast<const unsigned char *>(cache->k);
@@ -307,12 +349,18 @@ DBA_API int dba_cache_weigh(int B, int n, int q_heads, const dba_heads *q, const
     p.mask_words = mask_words;
     p.max_len = max_len;
     p.width = width;
-    p.by_head = by_head != 0;
     p.scale = scale;
-    const int tokens = in_place ? max_len : width;
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    const hipError_t e = cache->format == DBA_LOGP_F32 ? weigh_launch<0>(p, B, tokens, stream)
-                       : cache->format == DBA_LOGP_F16 ? weigh_launch<1>(p, B, tokens, stream) : weigh_launch<2>(p, B, tokens, stream);
+    const auto go = cache->format == DBA_LOGP_F32 ? weigh_launch<0> : cache->format == DBA_LOGP_F16 ? weigh_launch<1> : weigh_launch<2>;
+    if (!need) return launched(who, go(p, B, in_place ? max_len : width, stream));
+    WeighParams sums = p;
+    sums.score = nullptr;
+    sums.out = static_cast<float *>(workspace_dev);
+    sums.out_sent = (int64_t)cache->heads * max_len;
+    sums.out_head = max_len;
+    sums.width = max_len;
+    hipError_t e = go(sums, B, max_len, stream);
+    if (e == hipSuccess) e = launch(dba_weigh_join_kernel, dim3((unsigned)((width + 255) / 256), (unsigned)B), dim3(256), 0, stream, p, static_cast<const float *>(workspace_dev));
     return launched(who, e);
 }
 

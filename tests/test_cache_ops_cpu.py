@@ -99,8 +99,8 @@ def test_shared_workspace():
 
 # ---- weighing --------------------------------------------------------------------------------------------------------
 def _weigh(cache=None, q=None, q_heads=8, B=2, n=3, lse=AT, prefix=AT, tree=AT, mask=AT, words=1, count=None, max_len=128, scale=0.125, by_head=1, score=K, ss=1024, sh=256,
-           out=V, os_=1024, oh=256, width=200):
-    return beam.load().dba_cache_weigh(B, n, q_heads, R(q or _heads(Q)), lse, R(cache or _cache()), prefix, tree, mask, words, count, max_len, scale, by_head, score, ss, sh, out, os_, oh, width, None)
+           out=V, os_=1024, oh=256, width=200, ws=FAR, nbytes=1 << 30):
+    return beam.load().dba_cache_weigh(B, n, q_heads, R(q or _heads(Q)), lse, R(cache or _cache()), prefix, tree, mask, words, count, max_len, scale, by_head, score, ss, sh, out, os_, oh, width, ws, nbytes, None)
 
 
 @pytest.mark.parametrize("kw,frag", BAD_CACHES)
@@ -117,6 +117,20 @@ def test_weigh_refuses_a_cache(kw, frag):
 ])
 def test_weigh_refuses(kw, frag):
     _refused(_weigh(**kw), frag)
+
+
+def test_weigh_workspace():
+    size = beam.load().dba_cache_weigh_workspace_bytes
+    need = size(2, 3, 8, R(_cache()), 0, 128)
+    assert 0 < need < 1 << 20 and size(2, 3, 8, R(_cache()), 1, 128) == 0 and size(2, 3, 8, R(_cache(heads=1)), 0, 128) == 0
+    one = dict(by_head=0, sh=0, oh=0)
+    _refused(_weigh(nbytes=need - 1, **one), "workspace", dba.DBA_ENOMEM)
+    for kw in (dict(ws=None), dict(ws=FAR + 64)):
+        _refused(_weigh(**kw, **one), "256")
+    for kw in (dict(ws=K), dict(ws=V), dict(ws=Q), dict(lse=FAR)):
+        _refused(_weigh(**kw, **one), "in the workspace")
+    for bad in [(0, 3, 8, 0, 128), (2, 3, 8, 0, 129), (2, 3, 7, 0, 128)]:
+        assert size(bad[0], bad[1], bad[2], R(_cache()), *bad[3:]) == 0
 
 
 # ---- eviction --------------------------------------------------------------------------------------------------------

@@ -1,7 +1,8 @@
 """-m gpu: appending with norms and several axes, attention behind a common prefix, weighing and eviction of cached tokens, against plain statements in 64 bits.
 
 Tolerances.  u is half a step of the result's type (2^-24, 2^-11, 2^-8 of the value), u32 that of fp32.
-  append      a normed element is a product of three fp32 factors, one of them rounded: 4 u32 |y|; the rotation of those
+  append      squares are added up in fp32, eight in a row at most, then over two such rows and 32 lanes, and the mean is one more step: 15 u32 of
+              it, half of which its root has; the root's reciprocal is good to a step (2 u32), and two products follow: 12 u32 |y|; the rotation of those
               8 u32 (|y0| + |y1|) as without norms, and one rounding: u |z|, or half a step of the type's subnormals: below 2^-14 fp16 has steps of
               2^-24 whatever the value (e.g. -2.0894e-05 is rounded by 2.70e-08, which is more than 2^-11 of it and less than 2^-25).
   shared      as attention in test_gpu_beam_ops.py, over all tokens of both kinds; the join adds one fp32 product and sum a part, which L u32 A holds.
@@ -36,7 +37,7 @@ def normed_rotated(x, weight, eps, position, axis, inv_freq, interleaved):
     y, tol = x.double(), torch.zeros_like(x, dtype=torch.float64)
     if eps is not None:
         y = y / (y.square().mean(dim=-1, keepdim=True) + eps).sqrt() * (1.0 if weight is None else weight.double())
-        tol = 4 * U32 * y.abs()
+        tol = 12 * U32 * y.abs()
     r = len(inv_freq)
     if axis is not None:
         pos = torch.stack([position[:, a] if 0 <= a < position.shape[1] else torch.zeros(len(x)) for a in axis.tolist()], dim=1).double()
@@ -127,6 +128,7 @@ def test_append_norms_of_any_size(beam, dtype):  # noqa: F811
 
 @pytest.mark.parametrize("dtype", TYPES)
 def test_append_without_norms_or_axes_to_speak_of_is_append(beam, dtype):  # noqa: F811
+    """Each is 4 u32 (|x0| + |x1|) and a rounding from the definition at most (as in test_gpu_beam_ops.py; the angles are the same)."""
     k_pages, v_pages, table = a_cache(1, 2, 64, 2, 64, 8, dtype)
     qkv = torch.randn(2, 6, 8, 64, generator=gen(4)).to(dtype).cuda()
     inv, position = torch.rand(32, generator=gen(5)).cuda(), torch.randint(0, 90000, (2, 6), generator=gen(6)).int().cuda()
@@ -136,7 +138,10 @@ def test_append_without_norms_or_axes_to_speak_of_is_append(beam, dtype):  # noq
     a = beam.append(qkv[:, :, 4:6], qkv[:, :, 6:], *ref, table.cuda(), first, position=position, **more)
     b = beam.append(qkv[:, :, 4:6], qkv[:, :, 6:], k_pages, v_pages, table.cuda(), first, position=position[:, :, None].contiguous(),
                     axis=torch.zeros(32, dtype=torch.int32).cuda(), **more)
-    assert torch.equal(a, b) and torch.equal(ref[0], k_pages) and torch.equal(ref[1], v_pages)
+    for x, y in ((a, b), (ref[0], k_pages)):
+        x, y = x.double(), y.double()
+        assert ((x - y).abs() <= 2 * U[dtype] * x.abs() + 8 * U32 * (x.abs() + x.roll(32, dims=-1).abs()) * 2 ** 0.5 + 2 * LEAST[dtype]).all()
+    assert torch.equal(ref[1], v_pages)
 
 
 # ---- attention behind a common prefix --------------------------------------------------------------------------------
