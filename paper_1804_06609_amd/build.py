@@ -13,7 +13,7 @@ SOURCES = [os.path.join(CSRC, f) for f in (
     "dba.hip", "dba_beam.hip", "dba_cache.hip", "dba_attend_f32.hip", "dba_attend_f16.hip", "dba_attend_bf16.hip")]
 DEPS = SOURCES + [os.path.join(CSRC, f) for f in (
     "dba_kernels.hpp", "wave_topk.hpp", "host_blocks.hpp", "entry.hpp", "paged.hpp", "places.hpp", "beam_select.hpp", "beam_reorder.hpp",
-    "cache_append.hpp", "append_normed.hpp", "cache_weigh.hpp", "cache_evict.hpp", "cache_args.hpp", "tree_attend.hpp", "shared_attend.hpp",
+    "cache_append.hpp", "append_normed.hpp", "cache_weigh.hpp", "cache_evict.hpp", "cache_args.hpp", "tree_attend.hpp", "shared_attend.hpp", "common_attend.hpp",
     "tree_attend_launch.hpp")] + [
     os.path.join(os.path.dirname(HERE), "include", f) for f in ("dba.h", "dba_debug.h", "dba_beam.h")]
 

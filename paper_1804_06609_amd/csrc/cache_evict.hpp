@@ -18,9 +18,6 @@ struct EvictParams {
     int heads, heads_s, chunks, elem;  // chunks: of 16 bytes, of a head
 };
 
-constexpr int kChooseThreads = 1024, kChooseWaves = kChooseThreads / 64;
-constexpr int kDigits = 2048, kCopies = 2;
-
 // Inclusive sum over the lanes up to this one.
 __device__ __forceinline__ uint32_t wave_sum_up_to(uint32_t v)
 {
@@ -33,179 +30,359 @@ __device__ __forceinline__ uint32_t wave_sum_up_to(uint32_t v)
     return v;
 }
 
-// One workgroup per sentence and row of scores.  Scores are ranked as 32-bit images in their order (a NaN behind all others); the `need`-th greatest is found
-// digit by digit, 11, 11 and 10 bits, from a histogram in LDS, and what lies above it, with as many of its equals as there is room for, first ones
-// first, is listed in the order of the places.  A wave has a stretch of its own, so that places come from counts of waves and ballots.
-//
-// Up to kChooseThreads * NK tokens the images stay in registers; beyond, each pass reads them again.
-// Bound: latency; scores are a small part of what the move behind it takes.
-template <int NK>
-__global__ __launch_bounds__(kChooseThreads) void dba_evict_choose_kernel(EvictParams p)
+// The same in every thread: the sum over a workgroup of W waves, which all wait.
+template <int W>
+__device__ __forceinline__ uint32_t sum_of_all(uint32_t v, uint32_t (&s_wave)[W])
 {
-    __shared__ uint32_t s_hist[kCopies][kDigits];
-    __shared__ uint32_t s_wave[2][kChooseWaves];
+    v = wave_sum_up_to(v);
+    if (lane_id() == 63) s_wave[threadIdx.x >> 6] = v;
+    __syncthreads();
+    uint32_t all = 0;
+    for (int w = 0; w < W; ++w) all += s_wave[w];
+    __syncthreads();
+    return all;
+}
+
+// What a choice goes by.
+struct Choice {
+    int P;                             // tokens to choose from, some of which may not be there
+    int stay;                          // so many stay
+    uint32_t need;                     // of the kind that the choice is among
+    bool all, among_safe;              // all are there; the choice is among the first and last ones, since there is no room for all of those
+};
+
+// Scores are ranked as 32-bit images in their order, from 1 on (a NaN, behind all others); 0 is a token that is not asked about.
+__device__ __forceinline__ bool evict_present(const EvictParams &p, int b, int x) { return token_offset(p.from, b, x) >= 0; }
+__device__ __forceinline__ bool evict_safe(const EvictParams &p, const Choice &c, int x) { return x < p.sinks || x >= c.P - p.recent; }
+__device__ __forceinline__ uint32_t evict_key(const EvictParams &p, const Choice &c, int b, int x, float s)
+{
+    if (evict_safe(p, c, x) != c.among_safe || !(c.all || evict_present(p, b, x))) return 0;
+    return s != s ? 1u : ord_from_float(s);
+}
+
+// By a whole workgroup of W waves, every thread with the same result.
+template <int W>
+__device__ __forceinline__ Choice evict_choice(const EvictParams &p, int b, uint32_t (&s_wave)[W])
+{
+    Choice c;
+    c.P = span_of(p.prefix[b], 0, p.max_len).prefix;
+    // tokens that are there
+    const int t = (int)threadIdx.x, pages = c.P > 0 ? ((c.P - 1) >> p.from.page_shift) + 1 : 0;
+    uint32_t mine = 0;
+    for (int g = t; g < pages; g += 64 * W) {
+        const int first = g << p.from.page_shift;
+        if (evict_present(p, b, first)) mine += (uint32_t)min(1 << p.from.page_shift, c.P - first);
+    }
+    const int there = (int)sum_of_all<W>(mine, s_wave);
+    c.all = there == c.P;
+    c.stay = min(p.budget ? min(p.keep, max(p.budget[b], 0)) : p.keep, there);
+    // the first and the last ones go before all others
+    int safe = (int)min((int64_t)c.P, (int64_t)min(p.sinks, c.P) + min(p.recent, c.P));
+    if (!c.all) {
+        mine = 0;
+        for (int x = t; x < c.P; x += 64 * W) mine += evict_safe(p, c, x) && evict_present(p, b, x);
+        safe = (int)sum_of_all<W>(mine, s_wave);
+    }
+    c.among_safe = safe >= c.stay;
+    c.need = (uint32_t)(c.among_safe ? c.stay : c.stay - safe);
+    return c;
+}
+
+// The images are found digit by digit: 11, 11 and 10 bits.
+constexpr int kDigits = 2048;
+struct Digit {
+    int shift, bits;
+};
+__device__ __forceinline__ Digit digit_of(int pass) { return pass == 0 ? Digit{21, 11} : pass == 1 ? Digit{10, 11} : Digit{0, 10}; }
+
+// Adds a wave's keys to the counts of their digits; a wave of equals is one addition.
+__device__ __forceinline__ void count_digit(uint32_t *hist, bool in, uint32_t digit)
+{
+    const unsigned long long who = __ballot(in);
+    if (who == 0) return;
+    const uint32_t one = (uint32_t)__builtin_amdgcn_readlane((int)digit, __builtin_ctzll(who));
+    if (__ballot(in && digit == one) == who) {
+        if (lane_id() == 0) atomicAdd(&hist[one], (uint32_t)__popcll(who));
+    } else if (in) {
+        atomicAdd(&hist[digit], 1u);
+    }
+}
+
+// The digit that holds the `need`-th greatest, how many of it are needed, and how many there are.  Thread t has the counts of some digits next to each other,
+// thread 0 the greatest ones: n[0] is of digit kDigits - 1 - PER t, the next of one less.
+template <int W, int PER>
+__device__ __forceinline__ void find_digit(const uint32_t (&n)[PER], uint32_t need, uint32_t (&s_wave)[W], uint32_t (&s_found)[3])
+{
+    uint32_t sum = 0;
+#pragma unroll
+    for (int x = 0; x < PER; ++x) sum += n[x];
+    const uint32_t up = wave_sum_up_to(sum);
+    if (lane_id() == 63) s_wave[threadIdx.x >> 6] = up;
+    __syncthreads();
+    uint32_t before = up - sum;
+    for (int w = 0; w < (int)(threadIdx.x >> 6); ++w) before += s_wave[w];
+    if (before < need && before + sum >= need) {
+        uint32_t digit = 0, left = 0, count = 0;
+        bool found = false;
+#pragma unroll
+        for (int x = 0; x < PER; ++x) {
+            if (!found && before + n[x] >= need) {
+                digit = (uint32_t)(kDigits - 1 - PER * (int)threadIdx.x - x);
+                left = need - before;
+                count = n[x];
+                found = true;
+            }
+            before += n[x];
+        }
+        s_found[0] = digit;
+        s_found[1] = left;
+        s_found[2] = count;
+    }
+    __syncthreads();
+}
+
+// The least image that stays, and how many of its equals do, the first ones.
+struct Bar {
+    uint32_t least, equals;
+};
+
+// Writes the places of those of a wave's 64 tokens from x0 on that stay; s0 and e0: tokens sure to stay, and equal to the bar, before them.
+__device__ __forceinline__ void list_wave(const EvictParams &p, const Choice &c, const Bar &bar, int b, int32_t *list, int x, bool in, uint32_t key, uint32_t &s0, uint32_t &e0)
+{
+    const bool sure = in && (key > bar.least || (key == 0 && !c.among_safe && evict_safe(p, c, x) && (c.all || evict_present(p, b, x)))), tied = in && key == bar.least;
+    const unsigned long long who = __ballot(sure), same = __ballot(tied), below = (1ull << lane_id()) - 1;
+    const uint32_t e = e0 + (uint32_t)__popcll(same & below), place = s0 + (uint32_t)__popcll(who & below) + min(e, bar.equals);
+    if ((sure || (tied && e < bar.equals)) && place < (uint32_t)p.cap) list[place] = x;
+    s0 += (uint32_t)__popcll(who);
+    e0 += (uint32_t)__popcll(same);
+}
+// How many are sure to stay, and equal to the bar: the same for tokens that are not listed here.
+__device__ __forceinline__ uint2 count_of(const EvictParams &p, const Choice &c, const Bar &bar, int b, int x, uint32_t key)
+{
+    return make_uint2(key > bar.least || (key == 0 && !c.among_safe && evict_safe(p, c, x) && (c.all || evict_present(p, b, x))), key == bar.least);
+}
+
+// One workgroup of W waves per sentence and row of scores of up to 64 W NK tokens, whose images stay in registers.  A wave has a stretch of its own, so that
+// places come from counts of waves and ballots.
+// Bound: latency, a chain of fifteen to twenty-five barriers; scores are a small part of what the move behind it takes.
+template <int W, int NK>
+__global__ __launch_bounds__(64 * W) void dba_evict_choose_kernel(EvictParams p)
+{
+    __shared__ uint32_t s_hist[kDigits];
+    __shared__ uint32_t s_wave[2][W];
     __shared__ uint32_t s_found[3];
     const int lane = lane_id(), t = (int)threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const int b = (int)blockIdx.y, head = (int)blockIdx.x;
-    const int P = span_of(p.prefix[b], 0, p.max_len).prefix;
     const float *const score = p.score + ((int64_t)b * p.score_sent + (int64_t)head * p.score_head);
-    auto sum_of_all = [&](uint32_t v, int slot) -> uint32_t {      // the same in every thread; a barrier on both sides
-        v = wave_sum_up_to(v);
-        if (lane == 63) s_wave[slot][wave] = v;
-        __syncthreads();
-        uint32_t all = 0;
-        for (int w = 0; w < kChooseWaves; ++w) all += s_wave[slot][w];
-        __syncthreads();
-        return all;
-    };
-    auto present = [&](int x) { return token_offset(p.from, b, x) >= 0; };
-    auto is_safe = [&](int x) { return x < p.sinks || x >= P - p.recent; };
-
-    // tokens that are there
-    const int pages = P > 0 ? ((P - 1) >> p.from.page_shift) + 1 : 0;
-    uint32_t mine = 0;
-    for (int g = t; g < pages; g += kChooseThreads) {
-        const int first = g << p.from.page_shift;
-        if (present(first)) mine += (uint32_t)min(1 << p.from.page_shift, P - first);
-    }
-    const int there = (int)sum_of_all(mine, 0);
-    const bool all = there == P;
-    const int budget = p.budget ? min(p.keep, max(p.budget[b], 0)) : p.keep;
-    const int stay = min(budget, there);
-    if (head == 0 && t == 0) p.new_prefix[b] = stay;
-    if (stay == 0) return;
-    // the first and the last ones go before all others
-    int safe = (int)min((int64_t)P, (int64_t)min(p.sinks, P) + min(p.recent, P));
-    if (!all) {
-        mine = 0;
-        for (int x = t; x < P; x += kChooseThreads) mine += is_safe(x) && present(x);
-        safe = (int)sum_of_all(mine, 1);
-    }
-    const bool among_safe = safe >= stay;              // there is no room for all of them
-    uint32_t need = (uint32_t)(among_safe ? stay : stay - safe);
-
-    constexpr int kMost = kChooseThreads * NK;         // tokens of a turn
-    const int turns = (P + kMost - 1) / kMost;
-    uint32_t key[NK];
-    int base = 0, reach = 0;                           // of this turn: the wave's first token, 64s of tokens a wave
-    auto load = [&](int turn) {
-        const int first = turn * kMost, n = min(kMost, P - first);
-        reach = (n + kChooseThreads - 1) / kChooseThreads;
-        base = first + wave * reach * 64;
+    const int P = span_of(p.prefix[b], 0, p.max_len).prefix;
+    const int reach = (P + 64 * W - 1) / (64 * W), base = wave * reach * 64 + lane;        // 64s of tokens a wave; this lane's first
+    float s[NK];
 #pragma unroll
-        for (int x = 0; x < NK; ++x) {
-            key[x] = 0;                                // not asked about
-            if (x < reach) {
-                const int at = base + x * 64 + lane;
-                if (at < first + n && is_safe(at) == among_safe && (all || present(at))) {
-                    const float s = score[at];
-                    key[x] = s != s ? 1u : ord_from_float(s);
-                }
-            }
-        }
-    };
-    if (turns == 1) load(0);
-    uint32_t known = 0, bar = 0, equals = 0;           // the bits found; the least that stays; how many of its equals
+    for (int x = 0; x < NK; ++x) s[x] = x < reach && base + x * 64 < P ? score[base + x * 64] : 0.0f;      // (asked for before all else)
+    const Choice c = evict_choice<W>(p, b, s_wave[0]);
+    if (head == 0 && t == 0) p.new_prefix[b] = c.stay;
+    if (c.stay == 0) return;
+    uint32_t key[NK];
+#pragma unroll
+    for (int x = 0; x < NK; ++x) key[x] = x < reach && base + x * 64 < P ? evict_key(p, c, b, base + x * 64, s[x]) : 0;
+    uint32_t known = 0, need = c.need;
+    Bar bar = {0, 0};
 #pragma unroll 1
     for (int pass = 0; pass < 3; ++pass) {
-        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
-        for (int x = t; x < kDigits; x += kChooseThreads)
-            for (int k = 0; k < kCopies; ++k) s_hist[k][x] = 0;
+        const Digit d = digit_of(pass);
+        for (int x = t; x < kDigits; x += 64 * W) s_hist[x] = 0;
         __syncthreads();
-        for (int turn = 0; turn < turns; ++turn) {
-            if (turns > 1) load(turn);
 #pragma unroll
-            for (int x = 0; x < NK; ++x) {
-                if (x >= reach) continue;
-                const bool in = key[x] != 0 && (pass == 0 || (key[x] >> (shift + bits)) == known);
-                const uint32_t digit = (key[x] >> shift) & ((1u << bits) - 1);
-                const unsigned long long who = __ballot(in);
-                if (who == 0) continue;
-                const uint32_t one = (uint32_t)__builtin_amdgcn_readlane((int)digit, __builtin_ctzll(who));
-                if (__ballot(in && digit == one) == who) {     // a wave of equals is one addition
-                    if (lane == 0) atomicAdd(&s_hist[wave % kCopies][one], (uint32_t)__popcll(who));
-                } else if (in) {
-                    atomicAdd(&s_hist[wave % kCopies][digit], 1u);
-                }
-            }
-        }
+        for (int x = 0; x < NK; ++x)
+            if (x < reach) count_digit(s_hist, key[x] != 0 && (pass == 0 || key[x] >> (d.shift + d.bits) == known), key[x] >> d.shift & ((1u << d.bits) - 1));
         __syncthreads();
-        // from the greatest digit down: thread t has two of them
-        const int hi = kDigits - 1 - 2 * t, lo = hi - 1;
-        uint32_t n_hi = 0, n_lo = 0;
+        constexpr int PER = kDigits / (64 * W);
+        uint32_t n[PER];
 #pragma unroll
-        for (int k = 0; k < kCopies; ++k) {
-            n_hi += s_hist[k][hi];
-            n_lo += s_hist[k][lo];
-        }
-        const uint32_t up = wave_sum_up_to(n_hi + n_lo);
-        if (lane == 63) s_wave[0][wave] = up;
-        __syncthreads();
-        uint32_t before = up - n_hi - n_lo;
-        for (int w = 0; w < wave; ++w) before += s_wave[0][w];
-        if (before < need && before + n_hi + n_lo >= need) {
-            const bool in_hi = before + n_hi >= need;
-            s_found[0] = (uint32_t)(in_hi ? hi : lo);
-            s_found[1] = need - before - (in_hi ? 0 : n_hi);
-            s_found[2] = in_hi ? n_hi : n_lo;
-        }
-        __syncthreads();
-        known = known << bits | s_found[0];
+        for (int x = 0; x < PER; ++x) n[x] = s_hist[kDigits - 1 - PER * t - x];
+        find_digit<W, PER>(n, need, s_wave[0], s_found);
+        known = known << d.bits | s_found[0];
         need = s_found[1];
-        bar = max(known << shift, 1u);             // (images start at 1)
-        equals = need;
-        if (s_found[2] == need) {                  // all that are alike so far stay
-            equals = 0xFFFFFFFFu;
+        bar = {max(known << d.shift, 1u), need};
+        if (s_found[2] == need) {                      // all that are alike so far stay
+            bar.equals = 0xFFFFFFFFu;
             break;
         }
     }
-
-    // the list
+    uint32_t n_sure = 0, n_tied = 0;
+#pragma unroll
+    for (int x = 0; x < NK; ++x) {
+        if (x >= reach) continue;
+        const uint2 n = base + x * 64 < P ? count_of(p, c, bar, b, base + x * 64, key[x]) : make_uint2(0, 0);
+        n_sure += (uint32_t)__popcll(__ballot(n.x));
+        n_tied += (uint32_t)__popcll(__ballot(n.y));
+    }
+    if (lane == 0) {
+        s_wave[0][wave] = n_sure;
+        s_wave[1][wave] = n_tied;
+    }
+    __syncthreads();
+    uint32_t s0 = 0, e0 = 0;
+    for (int w = 0; w < wave; ++w) {
+        s0 += s_wave[0][w];
+        e0 += s_wave[1][w];
+    }
     int32_t *const list = p.list + ((int64_t)b * p.heads_s + head) * p.cap;
-    uint32_t listed = 0, tied = 0;                     // by the turns before
-    for (int turn = 0; turn < turns; ++turn) {
-        if (turns > 1) load(turn);
-        const int last = min(P, (turn + 1) * kMost);
-        // sure to stay, and equal to the bar
-        auto sure = [&](int x) {
-            const int at = base + x * 64 + lane;
-            return key[x] > bar || (key[x] == 0 && !among_safe && at < last && is_safe(at) && (all || present(at)));
-        };
-        uint32_t n_sure = 0, n_tied = 0;
 #pragma unroll
-        for (int x = 0; x < NK; ++x) {
-            if (x >= reach) continue;
-            n_sure += (uint32_t)__popcll(__ballot(sure(x)));
-            n_tied += (uint32_t)__popcll(__ballot(key[x] == bar));
-        }
-        __syncthreads();
-        if (lane == 0) {
-            s_wave[0][wave] = n_sure;
-            s_wave[1][wave] = n_tied;
-        }
-        __syncthreads();
-        uint32_t s0 = listed, e0 = tied;
-        for (int w = 0; w < kChooseWaves; ++w) {
-            const uint32_t a = s_wave[0][w], c = s_wave[1][w];
-            if (w < wave) {
-                s0 += a;
-                e0 += c;
+    for (int x = 0; x < NK; ++x)
+        if (x < reach) list_wave(p, c, bar, b, list, base + x * 64, base + x * 64 < P, key[x], s0, e0);
+}
+
+// Longer rows in three launches, with a workgroup for each kEvictPart tokens: counts of the first digit; the bar, from those counts and the tokens of that digit; the list.
+constexpr int kEvictWaves = 16, kEvictPart = 4096, kEvictPer = kEvictPart / (64 * kEvictWaves);
+
+constexpr int kEvictFew = 4096;        // tokens of the first digit that are kept rather than looked for once more
+
+struct EvictLong {
+    uint32_t *hist;                    // [B, heads_s, parts, kDigits]
+    uint32_t *found;                   // [B, heads_s, 2]: the bar
+    int parts;
+};
+
+__global__ __launch_bounds__(64 * kEvictWaves) void dba_evict_count_kernel(EvictParams p, EvictLong l)
+{
+    __shared__ uint32_t s_hist[kDigits], s_wave[kEvictWaves];
+    const int t = (int)threadIdx.x, b = (int)blockIdx.z, head = (int)blockIdx.y, first = (int)blockIdx.x * kEvictPart;
+    const float *const score = p.score + ((int64_t)b * p.score_sent + (int64_t)head * p.score_head);
+    const Choice c = evict_choice<kEvictWaves>(p, b, s_wave);
+    if (head == 0 && blockIdx.x == 0 && t == 0) p.new_prefix[b] = c.stay;
+    for (int x = t; x < kDigits; x += 64 * kEvictWaves) s_hist[x] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int x = 0; x < kEvictPer; ++x) {
+        const int at = first + x * 64 * kEvictWaves + t;
+        const uint32_t key = at < c.P ? evict_key(p, c, b, at, score[at]) : 0;
+        count_digit(s_hist, key != 0, key >> digit_of(0).shift);
+    }
+    __syncthreads();
+    uint32_t *const out = l.hist + (((int64_t)b * p.heads_s + head) * l.parts + blockIdx.x) * kDigits;
+    for (int x = t; x < kDigits; x += 64 * kEvictWaves) out[x] = s_hist[x];
+}
+
+__global__ __launch_bounds__(64 * kEvictWaves) void dba_evict_bar_kernel(EvictParams p, EvictLong l)
+{
+    __shared__ uint32_t s_hist[kDigits], s_key[kEvictFew], s_wave[kEvictWaves], s_found[3], s_few;
+    const int t = (int)threadIdx.x, b = (int)blockIdx.y, head = (int)blockIdx.x;
+    const float *const score = p.score + ((int64_t)b * p.score_sent + (int64_t)head * p.score_head);
+    const Choice c = evict_choice<kEvictWaves>(p, b, s_wave);
+    if (c.stay == 0) return;
+    constexpr int PER = kDigits / (64 * kEvictWaves);
+    uint32_t n[PER] = {}, known = 0, need = c.need, few = 0;      // few: of the first digit, so many in s_key
+    const uint32_t *const hist = l.hist + ((int64_t)b * p.heads_s + head) * l.parts * kDigits;
+    const int parts = (c.P + kEvictPart - 1) / kEvictPart;
+    constexpr int PARTS = 8;                           // whose loads are under way
+    for (int part = 0; part < parts; part += PARTS) {
+        uint32_t y[PARTS][PER];
+#pragma unroll
+        for (int z = 0; z < PARTS; ++z)
+#pragma unroll
+            for (int x = 0; x < PER; ++x) y[z][x] = hist[(int64_t)min(part + z, parts - 1) * kDigits + kDigits - 1 - PER * t - x];
+#pragma unroll
+        for (int z = 0; z < PARTS; ++z)
+#pragma unroll
+            for (int x = 0; x < PER; ++x) n[x] += part + z < parts ? y[z][x] : 0;
+    }
+    Bar bar = {0, 0};
+#pragma unroll 1
+    for (int pass = 0; pass < 3; ++pass) {
+        const Digit d = digit_of(pass);
+        if (pass > 0) {
+            for (int x = t; x < kDigits; x += 64 * kEvictWaves) s_hist[x] = 0;
+            if (t == 0) s_few = 0;
+            __syncthreads();
+            constexpr int U = 16;                      // loads under way
+            for (int x0 = 0; x0 < (few ? 0 : c.P); x0 += U * 64 * kEvictWaves) {
+                float s[U];
+#pragma unroll
+                for (int x = 0; x < U; ++x) s[x] = score[min(x0 + x * 64 * kEvictWaves + t, c.P - 1)];
+#pragma unroll
+                for (int x = 0; x < U; ++x) {
+                    const int at = x0 + x * 64 * kEvictWaves + t;
+                    const uint32_t key = s[x] != s[x] ? 1u : ord_from_float(s[x]);
+                    bool in = at < c.P && key >> (d.shift + d.bits) == known;
+                    if (!__any(in)) continue;
+                    if (in) in = evict_key(p, c, b, at, s[x]) != 0;
+                    count_digit(s_hist, in, key >> d.shift & ((1u << d.bits) - 1));
+                    if (in && pass == 1 && s_found[2] <= kEvictFew) s_key[atomicAdd(&s_few, 1u)] = key;
+                }
             }
-            listed += a;
-            tied += c;
-        }
-        const unsigned long long below = (1ull << lane) - 1;
+            if (few)
+                for (uint32_t x = t; x < ((few + 63) & ~63u); x += 64 * kEvictWaves)
+                    count_digit(s_hist, x < few && s_key[x] >> (d.shift + d.bits) == known, s_key[min(x, few - 1)] >> d.shift & ((1u << d.bits) - 1));
+            __syncthreads();
+            if (pass == 1) few = s_few;
 #pragma unroll
-        for (int x = 0; x < NK; ++x) {
-            if (x >= reach) continue;
-            const bool is_sure = sure(x), is_tied = key[x] == bar;
-            const unsigned long long who = __ballot(is_sure), same = __ballot(is_tied);
-            const uint32_t e = e0 + (uint32_t)__popcll(same & below), place = s0 + (uint32_t)__popcll(who & below) + min(e, equals);
-            if ((is_sure || (is_tied && e < equals)) && place < (uint32_t)p.cap) list[place] = base + x * 64 + lane;
-            s0 += (uint32_t)__popcll(who);
-            e0 += (uint32_t)__popcll(same);
+            for (int x = 0; x < PER; ++x) n[x] = s_hist[kDigits - 1 - PER * t - x];
+        }
+        find_digit<kEvictWaves, PER>(n, need, s_wave, s_found);
+        known = known << d.bits | s_found[0];
+        need = s_found[1];
+        bar = {max(known << d.shift, 1u), need};
+        if (s_found[2] == need) {
+            bar.equals = 0xFFFFFFFFu;
+            break;
         }
     }
+    if (t == 0) {
+        l.found[((int64_t)b * p.heads_s + head) * 2] = bar.least;
+        l.found[((int64_t)b * p.heads_s + head) * 2 + 1] = bar.equals;
+    }
+}
+
+__global__ __launch_bounds__(64 * kEvictWaves) void dba_evict_list_kernel(EvictParams p, EvictLong l)
+{
+    __shared__ uint32_t s_wave[2][kEvictWaves];
+    const int lane = lane_id(), t = (int)threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6), b = (int)blockIdx.z, head = (int)blockIdx.y, first = (int)blockIdx.x * kEvictPart;
+    const float *const score = p.score + ((int64_t)b * p.score_sent + (int64_t)head * p.score_head);
+    const Choice c = evict_choice<kEvictWaves>(p, b, s_wave[0]);
+    if (c.stay == 0 || first >= c.P) return;
+    const Bar bar = {l.found[((int64_t)b * p.heads_s + head) * 2], l.found[((int64_t)b * p.heads_s + head) * 2 + 1]};
+    // what lies before this part is counted once more, which is less than a launch for it
+    uint32_t before_sure = 0, before_tied = 0;
+    constexpr int U = 16;
+    for (int x0 = 0; x0 < first; x0 += U * 64 * kEvictWaves) {
+        float s[U];
+#pragma unroll
+        for (int x = 0; x < U; ++x) s[x] = score[min(x0 + x * 64 * kEvictWaves + t, first - 1)];
+#pragma unroll
+        for (int x = 0; x < U; ++x) {
+            const int at = x0 + x * 64 * kEvictWaves + t;
+            const uint32_t image = s[x] != s[x] ? 1u : ord_from_float(s[x]);
+            const bool safe = evict_safe(p, c, at), asked = safe == c.among_safe, here = at < first && (c.all || evict_present(p, b, min(at, first - 1)));
+            before_sure += here && (asked ? image > bar.least : !c.among_safe);
+            before_tied += here && asked && image == bar.least;
+        }
+    }
+    before_sure = sum_of_all<kEvictWaves>(before_sure, s_wave[0]);
+    before_tied = sum_of_all<kEvictWaves>(before_tied, s_wave[1]);
+    const int base = first + wave * kEvictPer * 64 + lane;
+    uint32_t key[kEvictPer], n_sure = 0, n_tied = 0;
+#pragma unroll
+    for (int x = 0; x < kEvictPer; ++x) {
+        const int at = base + x * 64;
+        key[x] = at < c.P ? evict_key(p, c, b, at, score[at]) : 0;
+        const uint2 n = at < c.P ? count_of(p, c, bar, b, at, key[x]) : make_uint2(0, 0);
+        n_sure += (uint32_t)__popcll(__ballot(n.x));
+        n_tied += (uint32_t)__popcll(__ballot(n.y));
+    }
+    if (lane == 0) {
+        s_wave[0][wave] = n_sure;
+        s_wave[1][wave] = n_tied;
+    }
+    __syncthreads();
+    uint32_t s0 = before_sure, e0 = before_tied;
+    for (int w = 0; w < wave; ++w) {
+        s0 += s_wave[0][w];
+        e0 += s_wave[1][w];
+    }
+    int32_t *const list = p.list + ((int64_t)b * p.heads_s + head) * p.cap;
+#pragma unroll
+    for (int x = 0; x < kEvictPer; ++x) list_wave(p, c, bar, b, list, base + x * 64, base + x * 64 < c.P, key[x], s0, e0);
 }
 
 constexpr int kMoveThreads = 256, kMoveItems = 4;      // chunks of keys, and of values, that a thread has under way
@@ -220,32 +397,63 @@ __global__ __launch_bounds__(kMoveThreads) void dba_evict_move_kernel(EvictParam
     const int stay = p.new_prefix[b], total = stay + (span.end - span.prefix);
     const int32_t *const list = p.list + (int64_t)b * p.heads_s * p.cap;
     const uint32_t per_token = (uint32_t)(p.heads * p.chunks);
-    const uint64_t items = (uint64_t)total * per_token, step = (uint64_t)gridDim.x * kMoveThreads * kMoveItems;
-    for (uint64_t x0 = (uint64_t)blockIdx.x * kMoveThreads * kMoveItems; x0 < items; x0 += step) {
-        const int j0 = (int)(x0 / per_token);
-        const uint32_t in0 = (uint32_t)(x0 - (uint64_t)j0 * per_token), left = (uint32_t)min((uint64_t)kMoveThreads * kMoveItems, items - x0);
-        u32x4_t k[kMoveItems], v[kMoveItems];
-        int64_t to[kMoveItems];
+    const uint64_t items = (uint64_t)total * per_token, turn = kMoveThreads * kMoveItems, step = (uint64_t)gridDim.x * turn;
+    // what a turn needs is asked for ahead: where its tokens come from two turns, their pages one
+    int src[kMoveItems];
+    int64_t from[kMoveItems], to[kMoveItems];          // bytes; to: -1: nothing to move
+    auto item = [&](uint64_t x0, int u, int &j, uint32_t &h, uint32_t &c) -> bool {
+        const uint64_t j0 = x0 / per_token;             // (the same for all)
+        const uint32_t x = (uint32_t)(x0 - j0 * per_token) + (uint32_t)(u * kMoveThreads + t), tokens = x / per_token, in = x - tokens * per_token;
+        j = (int)j0 + (int)tokens;
+        h = in / (uint32_t)p.chunks;
+        c = in - h * (uint32_t)p.chunks;
+        return x0 + (uint64_t)(u * kMoveThreads + t) < items;
+    };
+    auto ask_source = [&](uint64_t x0) {
 #pragma unroll
         for (int u = 0; u < kMoveItems; ++u) {
-            const uint32_t x = (uint32_t)(u * kMoveThreads + t), tokens = (in0 + x) / per_token;
-            to[u] = -1;
-            if (x >= left) continue;
-            const int j = j0 + (int)tokens;
-            const uint32_t in = in0 + x - tokens * per_token, h = in / (uint32_t)p.chunks, c = in - h * (uint32_t)p.chunks;
-            const int src = j < stay ? list[(p.heads_s > 1 ? (int64_t)h * p.cap : 0) + j] : span.prefix + (j - stay);
-            const int64_t from = token_offset(p.from, b, src), at = token_offset(p.to, b, j);
-            if (from < 0 || at < 0) continue;
-            const int64_t inside = ((int64_t)h * p.from.head_stride) * p.elem + (int64_t)c * 16;
-            k[u] = *reinterpret_cast<const u32x4_t *>(p.k_pages + from * p.elem + inside);
-            v[u] = *reinterpret_cast<const u32x4_t *>(p.v_pages + from * p.elem + inside);
-            to[u] = at * p.elem + inside;
+            int j;
+            uint32_t h, c;
+            src[u] = -1;
+            if (item(x0, u, j, h, c)) src[u] = j < stay ? list[(p.heads_s > 1 ? (int64_t)h * p.cap : 0) + j] : span.prefix + (j - stay);
+        }
+    };
+    auto ask_pages = [&](uint64_t x0) {
+#pragma unroll
+        for (int u = 0; u < kMoveItems; ++u) {
+            int j;
+            uint32_t h, c;
+            item(x0, u, j, h, c);
+            const int64_t old = token_offset(p.from, b, src[u]), at = src[u] < 0 ? -1 : token_offset(p.to, b, j), inside = (int64_t)h * p.from.head_stride * p.elem + (int64_t)c * 16;
+            from[u] = old * p.elem + inside;
+            to[u] = old < 0 || at < 0 ? -1 : at * p.elem + inside;
+        }
+    };
+    const uint64_t first = (uint64_t)blockIdx.x * turn;
+    if (first < items) {
+        ask_source(first);
+        ask_pages(first);
+        ask_source(first + step);
+    }
+    for (uint64_t x0 = first; x0 < items; x0 += step) {
+        u32x4_t k[kMoveItems], v[kMoveItems];
+        int64_t at[kMoveItems];
+#pragma unroll
+        for (int u = 0; u < kMoveItems; ++u) {
+            at[u] = to[u];
+            if (to[u] < 0) continue;
+            k[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(p.k_pages + from[u]));
+            v[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(p.v_pages + from[u]));
+        }
+        if (x0 + step < items) {
+            ask_pages(x0 + step);
+            ask_source(x0 + 2 * step);
         }
 #pragma unroll
         for (int u = 0; u < kMoveItems; ++u) {
-            if (to[u] < 0) continue;
-            *reinterpret_cast<u32x4_t *>(p.k_pages + to[u]) = k[u];
-            *reinterpret_cast<u32x4_t *>(p.v_pages + to[u]) = v[u];
+            if (at[u] < 0) continue;
+            __builtin_nontemporal_store(k[u], reinterpret_cast<u32x4_t *>(p.k_pages + at[u]));
+            __builtin_nontemporal_store(v[u], reinterpret_cast<u32x4_t *>(p.v_pages + at[u]));
         }
     }
     if (!p.new_score) return;

@@ -69,11 +69,41 @@ const char *shared_fault(int B, int n, int q_heads, const dba_cache *cache, int 
     return nullptr;
 }
 
+// Many rows over common tokens: how many rows a wave, and how many parts of the token axis.  A part costs about kPartTiles tiles to begin with and to write and join;
+// workgroups come in rounds.
+constexpr int kPartTiles = 3;
+
+AttendPlan common_plan(int nodes, int q_heads, const dba_cache &c, int max_shared)
+{
+    AttendPlan a = attend_plan(1, nodes, q_heads, c, max_shared);
+    if (!a.shared || c.format == DBA_LOGP_F32 || a.DP > 128 || c.page_size < 16 || c.token_stride >= 1 << 25) return a;     // (a wave's 16 tokens lie in a page, within 2^31 bytes)
+    const int rows = nodes * (q_heads / c.heads);
+    a.dense = true;
+    a.side = 1;
+    a.QT = 1;
+    a.tile = 64;
+    a.tile_rows = 128 * a.QT;
+    a.row_tiles = (rows + a.tile_rows - 1) / a.tile_rows;
+    const int tiles = (int)(((int64_t)max_shared + 63) / 64), resident = 512;
+    const int64_t units = (int64_t)a.row_tiles * c.heads;
+    int64_t best = INT64_MAX;
+    for (int splits = 1; splits <= 64 && splits <= tiles; ++splits) {
+        const int chunk = (tiles + splits - 1) / splits;
+        const int64_t cost = (units * splits + resident - 1) / resident * (chunk + kPartTiles);
+        if (cost < best) {
+            best = cost;
+            a.chunk = chunk;
+            a.splits = (tiles + chunk - 1) / chunk;
+        }
+    }
+    return a;
+}
+
 SharedPlan shared_plan(int B, int n, int q_heads, const dba_cache &c, int max_shared, int max_len)
 {
     SharedPlan s;
     s.own = attend_plan(B, n, q_heads, c, max_len);
-    s.common = attend_plan(1, B * n, q_heads, c, max_shared);
+    s.common = common_plan(B * n, q_heads, c, max_shared);
     const size_t own = attend_rows_of(B, n, q_heads, s.own), common = attend_rows_of(B, n, q_heads, s.common);
     s.own_o = 0;
     s.own_ml = s.own_o + align256(own * c.head_dim * 4);
@@ -364,6 +394,24 @@ DBA_API int dba_cache_weigh(int B, int n, int q_heads, const dba_heads *q, const
     return launched(who, e);
 }
 
+// The workspace: lists, and for long rows counts of digits and bars.
+struct EvictPlan {
+    int parts;                         // 0: rows are short
+    size_t hist_at, found_at, total;
+};
+constexpr int kShortRow = 16384;
+
+static EvictPlan evict_plan(int B, int heads_s, int keep, int max_len)
+{
+    EvictPlan e;
+    const size_t rows = (size_t)B * heads_s;
+    e.parts = max_len <= kShortRow ? 0 : (max_len + kEvictPart - 1) / kEvictPart;
+    e.hist_at = align256(rows * std::min(keep, max_len) * 4);
+    e.found_at = e.hist_at + align256(rows * e.parts * kDigits * 4);
+    e.total = e.found_at + (e.parts ? align256(rows * 8) : 0);
+    return e;
+}
+
 static const char *evict_fault(int B, const dba_cache *cache, int keep, int max_len)
 {
     const char *fault = cache_fault(cache);
@@ -375,8 +423,7 @@ static const char *evict_fault(int B, const dba_cache *cache, int keep, int max_
 
 DBA_API size_t dba_cache_evict_workspace_bytes(int B, const dba_cache *cache, int by_head, int keep, int max_len)
 {
-    if (evict_fault(B, cache, keep, max_len)) return 0;
-    return align256((size_t)B * (by_head ? cache->heads : 1) * std::min(keep, max_len) * 4);
+    return evict_fault(B, cache, keep, max_len) ? 0 : evict_plan(B, by_head ? cache->heads : 1, keep, max_len).total;
 }
 
 DBA_API int dba_cache_evict(int B, const dba_cache *cache, const int32_t *new_table_dev, int64_t new_table_stride, int new_max_pages, int by_head,
@@ -436,9 +483,19 @@ DBA_API int dba_cache_evict(int B, const dba_cache *cache, const int32_t *new_ta
     p.elem = (int)elem_bytes(cache->format);
     p.chunks = cache->head_dim * p.elem / 16;
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    const dim3 choose((unsigned)heads_s, (unsigned)B);
-    const auto kernel = max_len <= 4 * kChooseThreads ? dba_evict_choose_kernel<4> : max_len <= 16 * kChooseThreads ? dba_evict_choose_kernel<16> : dba_evict_choose_kernel<64>;
-    hipError_t e = launch(kernel, choose, dim3(kChooseThreads), 0, stream, p);
+    const EvictPlan plan = evict_plan(B, heads_s, keep, max_len);
+    hipError_t e;
+    if (!plan.parts) {
+        const auto kernel = max_len <= 1024 ? dba_evict_choose_kernel<4, 4> : max_len <= 4096 ? dba_evict_choose_kernel<8, 8> : dba_evict_choose_kernel<16, 16>;
+        e = launch(kernel, dim3((unsigned)heads_s, (unsigned)B), dim3(max_len <= 1024 ? 256u : max_len <= 4096 ? 512u : 1024u), 0, stream, p);
+    } else {
+        unsigned char *const ws = static_cast<unsigned char *>(workspace_dev);
+        const EvictLong l = {reinterpret_cast<uint32_t *>(ws + plan.hist_at), reinterpret_cast<uint32_t *>(ws + plan.found_at), plan.parts};
+        const dim3 parts((unsigned)plan.parts, (unsigned)heads_s, (unsigned)B), threads(64 * kEvictWaves);
+        e = launch(dba_evict_count_kernel, parts, threads, 0, stream, p, l);
+        if (e == hipSuccess) e = launch(dba_evict_bar_kernel, dim3((unsigned)heads_s, (unsigned)B), threads, 0, stream, p, l);
+        if (e == hipSuccess) e = launch(dba_evict_list_kernel, parts, threads, 0, stream, p, l);
+    }
     if (e == hipSuccess) {
         // (without a tree no more than keep tokens are moved)
         const int64_t items = (int64_t)(tree_dev ? max_len : p.cap) * p.heads * p.chunks, turn = kMoveThreads * kMoveItems;

@@ -1,5 +1,6 @@
 // Launches of the attention kernels of one format; each format is a source file of its own, which compile side by side.
 #pragma once
+#include "common_attend.hpp"
 #include "entry.hpp"
 #include "shared_attend.hpp"
 #include "tree_attend.hpp"
@@ -54,11 +55,28 @@ hipError_t attend_launch(const AttendParams &p, const AttendPlan &plan, int B, h
                   dim3(256), 0, stream, p, plan.tile, __builtin_ctz((unsigned)plan.tile_rows));
 }
 
+template <int FMT, int DP, int RB>
+hipError_t common_one(const AttendParams &p, hipStream_t stream)
+{
+    constexpr int lds = CommonShape<DP, RB>::LDS;
+    if constexpr (lds > 65536) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&dba_common_kernel<FMT, DP, RB>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        if (e != hipSuccess) return e;
+    }
+    return launch(dba_common_kernel<FMT, DP, RB>, dim3((unsigned)p.groups * (unsigned)p.row_tiles), dim3(256), lds, stream, p);
+}
+
 // Both kinds of parts, and their join.
 template <int FMT>
 hipError_t shared_launch(const SharedParams &p, const AttendPlan &own, const AttendPlan &common, int B, hipStream_t stream)
 {
-    hipError_t e = attend_widths<FMT, true>(p.common, common, stream);
+    hipError_t e = hipSuccess;
+    if (!common.dense) {
+        e = attend_widths<FMT, true>(p.common, common, stream);
+    } else if constexpr (FMT != 0) {
+        e = common.DP == 64 ? common.QT == 2 ? common_one<FMT, 64, 2>(p.common, stream) : common_one<FMT, 64, 1>(p.common, stream)
+                            : common.QT == 2 ? common_one<FMT, 128, 2>(p.common, stream) : common_one<FMT, 128, 1>(p.common, stream);
+    }
     if (e == hipSuccess) e = attend_widths<FMT, true>(p.own, own, stream);
     if (e != hipSuccess) return e;
     const int rows = p.own.n * (p.own.q_heads / p.own.heads), Q = (int64_t)B * p.own.heads * rows >= 16384 ? 4 : 1;
