@@ -32,9 +32,9 @@ __device__ __forceinline__ void load_to_lds(const void *from, void *to)
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) unsigned int *)from, (__attribute__((address_space(3))) unsigned int *)to, 16, 0, 0);
 }
 
-// Four waves of 32 RB rows each, tiles of 64 tokens in LDS twice.  Of a token's 16-byte chunks, which a wave's lanes put side by side, each reads one of another place, so
+// Four waves of 32 rows each, tiles of 64 tokens in LDS twice.  Of a token's 16-byte chunks, which a wave's lanes put side by side, each reads one of another place, so
 // that 16 lanes that read a chunk of 16 keys, or 32 that read 64 bytes of four tokens' values, meet all 64 banks.
-template <int DP, int RB>
+template <int DP>
 struct CommonShape {
     static constexpr int TT = 64, ROW = DP * 2, CH = ROW / 16;
     static constexpr int KS = DP / 16, DB = DP / 32;
@@ -45,15 +45,16 @@ struct CommonShape {
 };
 
 // As in dba_attend_kernel both products are transposed and the weights stay in registers: S^T = K Q^T leaves a lane with 16 tokens of one row for each 32 of them, which in
-// their order are what O^T = V^T P^T takes, V^T coming out of LDS through the transposing read.  With 64 rows a wave (RB = 2) what is read of LDS is half
-// of what a matrix instruction every 32 clocks leaves time for; with 32, the matrix units, LDS and the VALU are all near their bounds.
+// their order are what O^T = V^T P^T takes, V^T coming out of LDS through the transposing read.  The path of a tile that is all there has no branch but the one around
+// new maxima, and 170 instructions of the VALU beside 32 matrix ones.
 //
-// Bound: the matrix units and the VALU's exponentials alike: a tile of 64 tokens and 64 rows of 128 is 64 instructions of 32 clocks of the former, and 64 exponentials of 16
-// clocks and 230 other instructions of 4 of the latter.
-template <int FMT, int DP, int RB>
-__global__ __launch_bounds__(256, RB == 2 && DP == 128 ? 1 : 2) void dba_common_kernel(AttendParams p)
+// Bound: LDS, whose reads take 64 bytes a clock (a counter of its busy clocks says nine tenths of the time; 8192 rows of 128 over 8000 tokens, 4 heads: 173 us, 0.77
+// PFLOP/s).  64 rows a wave would halve what is read of it, but a wave alone on its SIMD has nothing to fill the waits with (209 us), and two have not the registers: with a half of
+// each tile's tokens for either, 35 spilled ones make every tile wait for the next one's loads (267 us).
+template <int FMT, int DP>
+__global__ __launch_bounds__(256, 2) void dba_common_kernel(AttendParams p)
 {
-    typedef CommonShape<DP, RB> A;
+    typedef CommonShape<DP> A;
     typedef typename Elem<FMT>::type E;
     constexpr int KS = A::KS, DB = A::DB, TT = A::TT;
     extern __shared__ __align__(16) unsigned char s_mem[];
@@ -71,23 +72,22 @@ __global__ __launch_bounds__(256, RB == 2 && DP == 128 ? 1 : 2) void dba_common_
         row_tile = (int)(blockIdx.x / (uint32_t)p.groups);
     }
     const int head = group % p.heads, split = group / p.heads;
-    const int G = p.q_heads / p.heads, rows = p.n * G, row0 = row_tile * p.tile_rows + wave * 32 * RB;
+    const int G = p.q_heads / p.heads, rows = p.n * G, r = row_tile * p.tile_rows + wave * 32 + i;
     const int len = span_of(p.prefix[0], 0, p.max_len).prefix, tiles = (len + TT - 1) / TT;
     const int u0 = split * p.chunk, u1 = min(tiles, u0 + p.chunk);
     if (u0 >= tiles && split > 0) return;              // (the join does not ask for it; the first split is always there)
 
-    u32x4 q[RB][KS];
+    u32x4 q[KS];
     const uint32_t sign = p.scale < 0.0f ? 0x80008000u : 0u;    // a negative scale turns the queries round
-#pragma unroll
-    for (int t = 0; t < RB; ++t) {
-        const int r = row0 + t * 32 + i, node = min(r, rows - 1) / G, hq = head * G + min(r, rows - 1) % G;
+    {
+        const int node = min(r, rows - 1) / G, hq = head * G + min(r, rows - 1) % G;
         const E *src = reinterpret_cast<const E *>(p.q.data) + ((int64_t)(node / p.per) * p.q.sent + (int64_t)(node % p.per) * p.q.token + (int64_t)hq * p.q.head);
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
             const int d = k * 16 + h * 8;
             u32x4 v = u32x4{0, 0, 0, 0};
             if (r < rows && d < p.D && p.scale != 0.0f) v = *reinterpret_cast<const u32x4 *>(src + d);
-            q[t][k] = v ^ sign;
+            q[k] = v ^ sign;
         }
     }
     const float sl2 = p.scale != 0.0f ? fabsf(p.scale) * kLog2e : 1.0f;
@@ -116,15 +116,10 @@ __global__ __launch_bounds__(256, RB == 2 && DP == 128 ? 1 : 2) void dba_common_
         if (lane == 0) s_live[buf][wave] = !there ? 0 : len - pos >= 16 ? 0xFFFFu : (1u << (len - pos)) - 1;
     };
 
-    f32x16 o[RB][DB];
-    float m[RB], l[RB];
+    f32x16 o[DB];
+    float m = -INFINITY, l = 0.0f;
 #pragma unroll
-    for (int t = 0; t < RB; ++t) {
-        m[t] = -INFINITY;
-        l[t] = 0.0f;
-#pragma unroll
-        for (int d = 0; d < DB; ++d) o[t][d] = f32x16{};
-    }
+    for (int d = 0; d < DB; ++d) o[d] = f32x16{};
     int key_at[KS];
 #pragma unroll
     for (int k = 0; k < KS; ++k) key_at[k] = i * A::ROW + ((k * 2 + h) ^ A::key_swap(i)) * 16;     // (tokens 32 on have the same places)
@@ -147,73 +142,66 @@ __global__ __launch_bounds__(256, RB == 2 && DP == 128 ? 1 : 2) void dba_common_
         }
         if (u + 1 < u1) ask_tile(u + 1, buf ^ 1, page_next);
         // S^T
-        f32x16 s[2][RB];
+        f32x16 s[2];
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
                 const u32x4 kf = *reinterpret_cast<const u32x4 *>(s_mem + key_at[k] + (kb + b * 32 * A::ROW));
-#pragma unroll
-                for (int t = 0; t < RB; ++t) s[b][t] = mfma16<FMT>(kf, q[t][k], k == 0 ? f32x16{} : s[b][t]);
+                s[b] = mfma16<FMT>(kf, q[k], k == 0 ? f32x16{} : s[b]);
             }
         // softmax, one row a lane and a half
-#pragma unroll
-        for (int t = 0; t < RB; ++t) {
-            if (__builtin_expect(!all, 0)) {
-#pragma unroll
-                for (int b = 0; b < 2; ++b)
-#pragma unroll
-                    for (int x = 0; x < 16; ++x)
-                        if (!((live >> (b * 32 + x / 4 * 8 + h * 4 + x % 4)) & 1)) s[b][t][x] = -INFINITY;
-            }
-            const float seed = fmaxf(s[0][t][0], s[1][t][0]);
-            float top = max_of_3(seed, s[0][t][1], s[1][t][1]), top1 = max_of_3(seed, s[0][t][2], s[1][t][2]);
-#pragma unroll
-            for (int x = 3; x < 15; x += 2) {
-                top = max_of_3(top, s[0][t][x], s[1][t][x]);
-                top1 = max_of_3(top1, s[0][t][x + 1], s[1][t][x + 1]);
-            }
-            top = max_of_3(top, s[0][t][15], s[1][t][15]);
-            top = fmaxf(top, top1);
-            top = fmaxf(top, __uint_as_float(xor32_u32(__float_as_uint(top))));
-            top = fmaf(top, sl2, -kWeightBits<FMT>);
-            if (__any(top > m[t] + kWeightRoom<FMT>)) {
-                const float m1 = top > m[t] + kWeightRoom<FMT> ? top : m[t];
-                const float keep = m1 == m[t] ? 1.0f : __builtin_amdgcn_exp2f(m[t] - m1);
-                m[t] = m1;
-                l[t] *= keep;
-#pragma unroll
-                for (int d = 0; d < DB; ++d) o[t][d] *= keep;
-            }
-            const float base = m[t] == -INFINITY ? 0.0f : m[t];
-            float sum[2] = {0.0f, 0.0f};
+        if (__builtin_expect(!all, 0)) {
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
-                for (int x = 0; x < 16; ++x) {
-                    s[b][t][x] = __builtin_amdgcn_exp2f(fmaf(s[b][t][x], sl2, -base));
-                    sum[x & 1] += s[b][t][x];
-                }
-            l[t] += sum[0] + sum[1];
+                for (int x = 0; x < 16; ++x)
+                    if (!((live >> (b * 32 + x / 4 * 8 + h * 4 + x % 4)) & 1)) s[b][x] = -INFINITY;
         }
+        const float seed = fmaxf(s[0][0], s[1][0]);
+        float top = max_of_3(seed, s[0][1], s[1][1]), top1 = max_of_3(seed, s[0][2], s[1][2]);
+#pragma unroll
+        for (int x = 3; x < 15; x += 2) {
+            top = max_of_3(top, s[0][x], s[1][x]);
+            top1 = max_of_3(top1, s[0][x + 1], s[1][x + 1]);
+        }
+        top = max_of_3(top, s[0][15], s[1][15]);
+        top = fmaxf(top, top1);
+        top = fmaxf(top, __uint_as_float(xor32_u32(__float_as_uint(top))));
+        top = fmaf(top, sl2, -kWeightBits<FMT>);
+        if (__any(top > m + kWeightRoom<FMT>)) {
+            const float m1 = top > m + kWeightRoom<FMT> ? top : m;
+            const float keep = m1 == m ? 1.0f : __builtin_amdgcn_exp2f(m - m1);
+            m = m1;
+            l *= keep;
+#pragma unroll
+            for (int d = 0; d < DB; ++d) o[d] *= keep;
+        }
+        const float base = m == -INFINITY ? 0.0f : m;
+        float sum[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int x = 0; x < 16; ++x) {
+                s[b][x] = __builtin_amdgcn_exp2f(fmaf(s[b][x], sl2, -base));
+                sum[x & 1] += s[b][x];
+            }
+        l += sum[0] + sum[1];
         // O^T += V^T P^T
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
-                u32x4 w[RB];
+                u32x4 w;
 #pragma unroll
-                for (int t = 0; t < RB; ++t)
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) w[t][x] = pack2<FMT>(s[b][t][y * 8 + 2 * x], s[b][t][y * 8 + 2 * x + 1]);
+                for (int x = 0; x < 4; ++x) w[x] = pack2<FMT>(s[b][y * 8 + 2 * x], s[b][y * 8 + 2 * x + 1]);
 #pragma unroll
                 for (int d = 0; d < DB; ++d) {
                     typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
                     struct { i16x4 lo, hi; } v;
                     v.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(s_mem + value_at[d] + (kb + (b * 32 + y * 16) * A::ROW)));
                     v.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(s_mem + value_at[d] + (kb + (b * 32 + y * 16 + 8) * A::ROW)));
-#pragma unroll
-                    for (int t = 0; t < RB; ++t) o[t][d] = mfma16<FMT>(__builtin_bit_cast(u32x4, v), w[t], o[t][d]);
+                    o[d] = mfma16<FMT>(__builtin_bit_cast(u32x4, v), w, o[d]);
                 }
             }
     };
@@ -230,20 +218,16 @@ __global__ __launch_bounds__(256, RB == 2 && DP == 128 ? 1 : 2) void dba_common_
 
     // this part's results: [rows, D] and the statistics
     const size_t part = ((size_t)head * p.splits + split) * rows;
+    l += __uint_as_float(xor32_u32(__float_as_uint(l)));
+    if (r >= rows) return;
+    if (h == 0) *reinterpret_cast<float2 *>(p.part_ml + (part + r) * 2) = make_float2(m, l);
 #pragma unroll
-    for (int t = 0; t < RB; ++t) {
-        const int r = row0 + t * 32 + i;
-        const float ll = l[t] + __uint_as_float(xor32_u32(__float_as_uint(l[t])));
-        if (r >= rows) continue;
-        if (h == 0) *reinterpret_cast<float2 *>(p.part_ml + (part + r) * 2) = make_float2(m[t], ll);
+    for (int d = 0; d < DB; ++d)
 #pragma unroll
-        for (int d = 0; d < DB; ++d)
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                const int e = d * 32 + x * 8 + h * 4;
-                if (e < p.D) *reinterpret_cast<f32x4 *>(p.part_o + (part + r) * p.D + e) = f32x4{o[t][d][x * 4], o[t][d][x * 4 + 1], o[t][d][x * 4 + 2], o[t][d][x * 4 + 3]};
-            }
-    }
+        for (int x = 0; x < 4; ++x) {
+            const int e = d * 32 + x * 8 + h * 4;
+            if (e < p.D) *reinterpret_cast<f32x4 *>(p.part_o + (part + r) * p.D + e) = f32x4{o[d][x * 4], o[d][x * 4 + 1], o[d][x * 4 + 2], o[d][x * 4 + 3]};
+        }
 }
 
 }  // namespace dba

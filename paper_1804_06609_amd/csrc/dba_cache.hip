@@ -69,7 +69,7 @@ const char *shared_fault(int B, int n, int q_heads, const dba_cache *cache, int 
     return nullptr;
 }
 
-// Many rows over common tokens: how many rows a wave, and how many parts of the token axis.  A part costs about kPartTiles tiles to begin with and to write and join;
+// Many rows over common tokens: how many parts of the token axis.  A part costs about kPartTiles tiles to begin with and to write and join;
 // workgroups come in rounds.
 constexpr int kPartTiles = 3;
 
@@ -80,9 +80,8 @@ AttendPlan common_plan(int nodes, int q_heads, const dba_cache &c, int max_share
     const int rows = nodes * (q_heads / c.heads);
     a.dense = true;
     a.side = 1;
-    a.QT = 1;
     a.tile = 64;
-    a.tile_rows = 128 * a.QT;
+    a.tile_rows = 128;
     a.row_tiles = (rows + a.tile_rows - 1) / a.tile_rows;
     const int tiles = (int)(((int64_t)max_shared + 63) / 64), resident = 512;
     const int64_t units = (int64_t)a.row_tiles * c.heads;

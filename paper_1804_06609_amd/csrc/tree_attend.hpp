@@ -846,7 +846,7 @@ struct AttendPlan {
     int side;                          // heads of a workgroup whose waves have tiles of their own: 1 or 2
     bool shared;                       // the waves have rows of their own (ROWS)
     int tile, tile_rows, row_tiles, splits, chunk;
-    bool dense = false;                // rows that all see all tokens, and many of them: dba_common_kernel, QT times 32 rows a wave
+    bool dense = false;                // rows that all see all tokens, and many of them: dba_common_kernel
 };
 
 template <int FMT> hipError_t attend_launch(const AttendParams &p, const AttendPlan &plan, int B, hipStream_t stream);

@@ -55,15 +55,15 @@ hipError_t attend_launch(const AttendParams &p, const AttendPlan &plan, int B, h
                   dim3(256), 0, stream, p, plan.tile, __builtin_ctz((unsigned)plan.tile_rows));
 }
 
-template <int FMT, int DP, int RB>
+template <int FMT, int DP>
 hipError_t common_one(const AttendParams &p, hipStream_t stream)
 {
-    constexpr int lds = CommonShape<DP, RB>::LDS;
+    constexpr int lds = CommonShape<DP>::LDS;
     if constexpr (lds > 65536) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&dba_common_kernel<FMT, DP, RB>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&dba_common_kernel<FMT, DP>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
         if (e != hipSuccess) return e;
     }
-    return launch(dba_common_kernel<FMT, DP, RB>, dim3((unsigned)p.groups * (unsigned)p.row_tiles), dim3(256), lds, stream, p);
+    return launch(dba_common_kernel<FMT, DP>, dim3((unsigned)p.groups * (unsigned)p.row_tiles), dim3(256), lds, stream, p);
 }
 
 // Both kinds of parts, and their join.
@@ -74,8 +74,7 @@ hipError_t shared_launch(const SharedParams &p, const AttendPlan &own, const Att
     if (!common.dense) {
         e = attend_widths<FMT, true>(p.common, common, stream);
     } else if constexpr (FMT != 0) {
-        e = common.DP == 64 ? common.QT == 2 ? common_one<FMT, 64, 2>(p.common, stream) : common_one<FMT, 64, 1>(p.common, stream)
-                            : common.QT == 2 ? common_one<FMT, 128, 2>(p.common, stream) : common_one<FMT, 128, 1>(p.common, stream);
+        e = common.DP == 64 ? common_one<FMT, 64>(p.common, stream) : common_one<FMT, 128>(p.common, stream);
     }
     if (e == hipSuccess) e = attend_widths<FMT, true>(p.own, own, stream);
     if (e != hipSuccess) return e;
