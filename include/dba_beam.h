@@ -193,7 +193,7 @@ DBA_API int dba_shared_attend(int B, int n, int q_heads, const dba_heads *q, con
  *   count_dev    device [B] int32; NULL: n everywhere
  *   max_len      1 to max_pages * page_size, at most width
  *   score_dev, out_dev  device [B, 1 or heads, width] fp32 with strides between sentences and heads, last axis dense; width <= 2^28.  out_dev may be
- *                score_dev (same strides), and else has no byte in common with it, q, lse_dev or mask_dev
+ *                score_dev (same strides), and else has no byte in common with it; nor has it with q, lse_dev, mask_dev or the cache
  *   workspace_dev  device, 256-byte aligned, at least dba_cache_weigh_workspace_bytes bytes (which may be 0); none of these lies in it
  */
 DBA_API size_t dba_cache_weigh_workspace_bytes(int B, int n, int q_heads, const dba_cache *cache, int by_head, int max_len);

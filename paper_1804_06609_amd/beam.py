@@ -513,6 +513,7 @@ def evict(score: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, tab
         new_score = _empty_like(score, memory_format=_CONTIGUOUS)
     new_prefix = prefix.new_empty((B,))
     by_head = heads == k_pages.shape[2]
+    keep, sinks, recent = (min(x, 2**31 - 1) for x in (keep, sinks, recent))       # (more than there are tokens)
     if max_len is None:
         max_len = min(table.shape[1] * k_pages.shape[1], width)
     nbytes = lib.dba_cache_evict_workspace_bytes(B, cache, by_head, keep, max_len)

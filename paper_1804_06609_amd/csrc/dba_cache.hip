@@ -346,8 +346,8 @@ DBA_API int dba_cache_weigh(int B, int n, int q_heads, const dba_heads *q, const
     if (!to.nested()) return set_error(DBA_EINVAL, "%s: rows of out_dev overlap", who);
     if (!in_place && meet(to, was)) return set_error(DBA_EINVAL, "%s: out_dev overlaps a part of score_dev", who);
     if (meet(to, places_of(*q, B, n, q_heads, *cache)) || meet(to, Places(lse_dev, (int64_t)B * n * q_heads * 4)) ||
-        (mask_dev && meet(to, Places(mask_dev, (int64_t)B * n * mask_words * 8))))
-        return set_error(DBA_EINVAL, "%s: out_dev lies in q, lse_dev or mask_dev", who);
+        (mask_dev && meet(to, Places(mask_dev, (int64_t)B * n * mask_words * 8))) || meet(to, places_of(cache->k, *cache)))
+        return set_error(DBA_EINVAL, "%s: out_dev lies in q, lse_dev, mask_dev or the cache", who);
     const size_t need = dba_cache_weigh_workspace_bytes(B, n, q_heads, cache, by_head, max_len);
     if (need) {
         if (!workspace_dev || misaligned(workspace_dev, 256)) return set_error(DBA_EINVAL, "%s: workspace_dev must be 256-byte aligned", who);
@@ -451,8 +451,11 @@ DBA_API int dba_cache_evict(int B, const dba_cache *cache, const int32_t *new_ta
     if (!places_of(cache->k, *cache).nested()) return set_error(DBA_EINVAL, "%s: tokens of the cache overlap", who);
     if (!to.nested()) return set_error(DBA_EINVAL, "%s: rows of new_score_dev overlap", who);
     if (meet(to, stay) || meet(to, room) || meet(stay, room)) return set_error(DBA_EINVAL, "%s: results or the workspace overlap", who);
+    const Places keys = places_of(cache->k, *cache), values = places_of(cache->v, *cache);
     for (const Places &x : small)
         if (meet(x, to) || meet(x, stay) || meet(x, room)) return set_error(DBA_EINVAL, "%s: a result or the workspace overlaps what is read", who);
+    for (const Places &x : {to, stay, room, was})
+        if (meet(x, keys) || meet(x, values)) return set_error(DBA_EINVAL, "%s: scores, a result or the workspace lie in the cache", who);
     EvictParams p;
     p.from = p.to = paged_of(*cache);
     p.to.table = new_table_dev;

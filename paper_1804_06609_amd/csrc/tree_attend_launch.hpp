@@ -59,7 +59,7 @@ template <int FMT, int DP>
 hipError_t common_one(const AttendParams &p, hipStream_t stream)
 {
     constexpr int lds = CommonShape<DP>::LDS;
-    if constexpr (lds > 65536) {
+    if constexpr (lds >= 65536) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&dba_common_kernel<FMT, DP>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
         if (e != hipSuccess) return e;
     }

@@ -113,7 +113,7 @@ def test_weigh_refuses_a_cache(kw, frag):
     (dict(tree=None), "mask"), (dict(words=-1), "mask"), (dict(max_len=0), "max_len"), (dict(max_len=129), "max_len"), (dict(scale=float("nan")), "scale"),
     (dict(score=None), "NULL"), (dict(out=None), "NULL"), (dict(score=K + 2), "4 bytes"), (dict(oh=-1), "negative"), (dict(width=127), "width"), (dict(width=(1 << 28) + 1), "width"),
     (dict(out=K, oh=200), "two sets"), (dict(out=K, os_=2048), "two sets"), (dict(out=K + 4), "overlaps"), (dict(oh=199), "rows"), (dict(out=Q), "lies in"), (dict(out=AT), "lies in"),
-    (dict(lse=V + 400), "lies in"), (dict(mask=V + 1024), "lies in"), (dict(q=_heads(data=None)), "NULL"),
+    (dict(lse=V + 400), "lies in"), (dict(mask=V + 1024), "lies in"), (dict(q=_heads(data=None)), "NULL"), (dict(cache=_cache(k=V - 4096)), "the cache"),
 ])
 def test_weigh_refuses(kw, frag):
     _refused(_weigh(**kw), frag)
@@ -151,7 +151,8 @@ def test_evict_refuses_a_cache(kw, frag):
     (dict(pages=1 << 27, stride=1 << 27), "new_max_pages"), (dict(sinks=-1), "sinks"), (dict(recent=-1), "recent"), (dict(width=127), "width"), (dict(width=(1 << 28) + 1), "width"),
     (dict(ws=None), "256"), (dict(ws=FAR + 64), "256"), (dict(cache=_cache(token_stride=64)), "overlap"), (dict(nh=199), "rows"), (dict(new=K), "what is read"), (dict(new=K + 4), "what is read"),
     (dict(new_prefix=V + 4), "overlap"), (dict(new_prefix=AT + 4), "what is read"), (dict(new_prefix=AT + 4096), "what is read"), (dict(ws=K), "what is read"), (dict(ws=V), "overlap"),
-    (dict(budget=O), "what is read"), (dict(new_prefix=FAR), "overlap"),
+    (dict(budget=O), "what is read"), (dict(new_prefix=FAR), "overlap"), (dict(cache=_cache(k=V - 4096)), "in the cache"), (dict(cache=_cache(v=K)), "in the cache"),
+    (dict(cache=_cache(v=FAR)), "in the cache"), (dict(cache=_cache(k=O - 64)), "in the cache"),
 ])
 def test_evict_refuses(kw, frag):
     _refused(_evict(**kw), frag)

@@ -103,6 +103,42 @@ def test_append(beam, dtype, interleaved, B, n, Hq, Hkv, D, rot, page, norm, wid
         assert (kc[~touched] == 7).all() and (vc[~touched] == 7).all()
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("B,n,Hq,Hkv,D,rot,norm,axes", [(4, 1027, 6, 2, 64, 32, "head", 3), (3, 1366, 3, 3, 80, 80, "all", 0), (70, 60, 9, 1, 16, 16, "none", 2)])
+def test_append_of_many_tokens(beam, dtype, interleaved, B, n, Hq, Hkv, D, rot, norm, axes):  # noqa: F811
+    """Several tokens a workgroup; counts that end inside one, and those of no token."""
+    g, page = gen(n), 32
+    k_pages, v_pages, table = a_cache(5, B, n + 40, Hkv, D, page, dtype, fill=7.0)
+    k, v, q = (torch.randn(B, n, h, D, generator=g).to(dtype) for h in (Hkv, Hkv, Hq))
+    first, count = torch.randint(0, 40, (B,), generator=g).int(), torch.randint(1, n + 1, (B,), generator=g).int()
+    count[0], count[1], count[2] = -2**31, n, 3
+    inv = (10000.0 ** (-torch.arange(0, rot, 2).double() / rot)).float()
+    eps = None if norm == "none" else 1e-5
+    qw, kw = [None, None] if norm == "none" else [(torch.rand((D,) if norm == "all" else (h, D), generator=g) + 0.5).to(dtype) for h in (Hq, Hkv)]
+    axis = torch.randint(0, axes, (rot // 2,), generator=g).int() if axes else None
+    position = torch.randint(0, 50000, (B, n, axes), generator=g).int() if axes else None
+    q_dev = q.cuda()
+    more = dict(position=None if position is None else position.cuda(), inv_freq=inv.cuda(), interleaved=interleaved, axis=None if axis is None else axis.cuda(), eps=eps,
+                q_weight=None if qw is None else qw.cuda(), k_weight=None if kw is None else kw.cuda())
+    beam.append(*cuda(k, v), k_pages, v_pages, *cuda(table, first, count), q=q_dev, q_out=q_dev, **more)
+    kc, vc, touched = k_pages.cpu().double(), v_pages.cpu().double(), torch.zeros(k_pages.shape[:2], dtype=torch.bool)
+    for b in range(B):
+        m = max(0, int(count[b]))
+        pos = position[b] if axes else first[b] + torch.arange(n)
+        want_k, tol_k = normed_rotated(k[b], kw, eps, pos, axis, inv, interleaved)
+        want_q, tol_q = normed_rotated(q[b], qw, eps, pos, axis, inv, interleaved)
+        t = int(first[b]) + torch.arange(m)
+        at = table[b, t // page].long(), t % page
+        touched[at] = True
+        assert ((kc[at] - want_k[:m]).abs() <= U[dtype] * want_k[:m].abs() + tol_k[:m] * (1 + U[dtype]) + LEAST[dtype]).all()
+        assert torch.equal(vc[at], v[b, :m].double())
+        got = q_dev[b].cpu().double()
+        assert ((got[:m] - want_q[:m]).abs() <= U[dtype] * want_q[:m].abs() + tol_q[:m] * (1 + U[dtype]) + LEAST[dtype]).all()
+        assert (got[m:] == 0).all()
+    assert (kc[~touched] == 7).all() and (vc[~touched] == 7).all()
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_append_norms_of_any_size(beam, dtype):  # noqa: F811
     """Squares pass fp32's range at both ends; what is not finite stays with its head."""
@@ -221,6 +257,9 @@ SHAPES = [
     (9, 11, 16, 2, 128, 16, 517, [30] * 9, [11] * 9),
     (3, 70, 4, 2, 256, 16, 90, [30, 2, 0], [70] * 3),
     (4, 1, 3, 1, 24, 2, 5, [0, 1, 2, 3], [1, 0, 2, 1]),
+    (9, 10, 8, 1, 40, 16, 205, [3] * 9, [10] * 9),
+    (40, 5, 3, 3, 64, 64, 77, [1] * 40, [5] * 40),
+    (17, 2, 8, 2, 96, 128, 640, [0] * 17, [2] * 17),
 ]
 
 
@@ -383,6 +422,9 @@ WEIGH = [
     (1, 63, 16, 2, 128, 16, [700], [63]),
     (4, 1, 3, 1, 24, 2, [0, 1, 2, 3], [1, 0, 2, 1]),
     (2, 150, 4, 2, 64, 16, [0, 37], [150, 150]),
+    (2, 25, 8, 2, 128, 16, [300, 0], [100, 25]),
+    (1, 32, 8, 2, 64, 32, [1500], [32]),
+    (3, 40, 9, 3, 40, 8, [70, 0, 200], [64, 128, 40]),
     (2, 90, 3, 1, 256, 16, [0, 300], [90, 200]),
 ]
 
