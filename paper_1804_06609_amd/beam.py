@@ -482,7 +482,7 @@ def weigh(score: torch.Tensor, q: torch.Tensor, lse: torch.Tensor, k_pages: torc
     if max_len is None:
         max_len = min(table.shape[1] * k_pages.shape[1], rows[2])
     by_head = rows[1] == kv_heads
-    nbytes = 0 if by_head else lib.dba_cache_weigh_workspace_bytes(B, n, heads, cache, by_head, max_len)
+    nbytes = lib.dba_cache_weigh_workspace_bytes(B, n, heads, cache, by_head, max_len)
     ws, at = _workspace(nbytes, q)
     _b._check(lib.dba_cache_weigh(B, n, heads, _heads("q", q, shape, dtype, device), lse.data_ptr(), cache, _ints("prefix", prefix, (B,), device),
                                   _ints("tree", tree, (B,), device), bits, words, _ints("count", count, (B,), device), max_len,

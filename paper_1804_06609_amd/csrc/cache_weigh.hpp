@@ -11,12 +11,13 @@ struct WeighParams {
     const float *lse;                  // [B, n, q_heads]
     const int32_t *prefix, *tree, *count;
     const unsigned long long *mask;
-    const float *score;                // [B, 1 or heads, ..]; of one for all heads, nullptr: sums are left for another launch
-    float *out;                        // [B, 1 or heads, ..], or those sums [B, heads, max_len]
+    const float *score;                // [B, 1 or heads, ..]; nullptr: sums are left for another launch
+    float *out;                        // [B, 1 or heads, ..], or those sums [B, heads, splits, max_len]
     int64_t score_sent, score_head, out_sent, out_head;
     int n, q_heads, heads, D, mask_words, max_len;
     int width;                         // tokens that out has; those that nobody asks about are taken over
     int chunk;                         // of few rows: tokens of a workgroup
+    int splits, split_rows;            // of many: workgroups along them, rows of each
     float scale;
 };
 
@@ -99,6 +100,7 @@ struct WeighShape {
 // a token's sum is four additions a lane and, at the very end, two exchanges.  Each token belongs to one wave, which adds up in the order of the
 // rows: nothing is added atomically, and results do not vary.
 //
+// Rows are split where there are few tokens; sums of splits are added up in their order by another launch.
 // Bound: the exponentials and what is around them.
 template <int FMT, int DP, bool FULL>
 __global__ __launch_bounds__(256, 2) void dba_weigh_kernel(WeighParams p)
@@ -111,18 +113,18 @@ __global__ __launch_bounds__(256, 2) void dba_weigh_kernel(WeighParams p)
     __shared__ unsigned long long s_seen[W::RQ][4];     // which of a wave's tokens a row sees
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int c = lane & 15, g = lane >> 4;
-    const int b = (int)blockIdx.z, head = (int)blockIdx.y;
+    const int b = (int)blockIdx.z, head = (int)blockIdx.y / p.splits, split = (int)blockIdx.y - head * p.splits;
     const int t0 = (int)blockIdx.x * W::TG, mine = t0 + wave * W::TW;
     const int G = p.q_heads / p.heads;
     const NodeOf of = {G, 1.0f / (float)G};
     const int tree_all = p.tree ? max(p.tree[b], 0) : 0;
     const Span span = span_of(p.prefix[b], tree_all, p.max_len);
     const int n = p.count ? min(max(p.count[b], 0), p.n) : p.n;
-    const int rows = n * G;
+    const int r0 = split * p.split_rows, rows = min(n * G, r0 + p.split_rows);     // this workgroup's
     const WeighMask mask = {p.mask ? p.mask + (int64_t)b * p.n * p.mask_words : nullptr, p.mask_words, span.prefix, span.end, tree_all - p.n};
     // of a chain, the first node that sees any of these tokens
-    const int node0 = p.mask ? 0 : (int)max((int64_t)0, min((int64_t)n, (int64_t)t0 - span.prefix - tree_all + p.n));
-    const int first = node0 * G / W::RQ * W::RQ;
+    const int node0 = p.mask || t0 < span.prefix ? 0 : (int)max((int64_t)0, min((int64_t)n, (int64_t)t0 - span.prefix - tree_all + p.n));
+    const int first = max(r0, node0 * G / W::RQ * W::RQ);
     float acc[NT];
     bool there[NT];
 #pragma unroll
@@ -212,7 +214,7 @@ __global__ __launch_bounds__(256, 2) void dba_weigh_kernel(WeighParams p)
             }
         }
     }
-    const int64_t from = (int64_t)b * p.score_sent + (int64_t)head * p.score_head, to = (int64_t)b * p.out_sent + (int64_t)head * p.out_head;
+    const int64_t from = (int64_t)b * p.score_sent + (int64_t)head * p.score_head, to = (int64_t)b * p.out_sent + (int64_t)blockIdx.y * p.out_head;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         const float sum = sum_over_groups(acc[t]);
@@ -401,18 +403,18 @@ __global__ __launch_bounds__(256, (DP == 256 || FMT == 0 ? 2 : 4)) void dba_weig
     }
 }
 
-// One score for all heads: their sums, added up in the order of the heads.
-__global__ __launch_bounds__(256) void dba_weigh_join_kernel(WeighParams p, const float *sums)
+// Sums of heads (one score for all: parts are those of all heads) or of a head's rows, added up in their order.
+__global__ __launch_bounds__(256) void dba_weigh_join_kernel(WeighParams p, const float *sums, int parts)
 {
-    const int b = (int)blockIdx.y, t = (int)blockIdx.x * 256 + (int)threadIdx.x;
+    const int b = (int)blockIdx.z, row = (int)blockIdx.y, t = (int)blockIdx.x * 256 + (int)threadIdx.x;
     if (t >= p.width) return;
     const Span span = span_of(p.prefix[b], p.tree ? p.tree[b] : 0, p.max_len);
     const bool there = t < span.end && token_offset(p.cache, b, t) >= 0;
     if (!there && p.out == p.score) return;
     float sum = 0.0f;
     if (there)
-        for (int h = 0; h < p.heads; ++h) sum += sums[((int64_t)b * p.heads + h) * p.max_len + t];
-    p.out[(int64_t)b * p.out_sent + t] = p.score[(int64_t)b * p.score_sent + t] + sum;
+        for (int x = 0; x < parts; ++x) sum += sums[(((int64_t)b * gridDim.y + row) * parts + x) * p.max_len + t];
+    p.out[(int64_t)b * p.out_sent + (int64_t)row * p.out_head + t] = p.score[(int64_t)b * p.score_sent + (int64_t)row * p.score_head + t] + sum;
 }
 
 }  // namespace dba

@@ -125,23 +125,58 @@ void lay_out(AttendParams &p, const AttendPlan &plan, int B, const dba_cache &c)
 // ---- weighing -------------------------------------------------------------------------------------------------------
 
 // Up to WeighFew::MOST rows a head the waves go through tokens, else through rows.  Of the former a workgroup has as few tokens as fill the GPU
-// (kWeighGroups workgroups), but two tiles a wave at least, and sums that fit into LDS.
-constexpr int kWeighGroups = 3072, kWeighChunk = 2048;
+// (kWeighGroups workgroups), but two tiles a wave at least, and sums that fit into LDS.  Of the latter rows are split where tokens alone leave GPU empty, two
+// turns of rows in LDS at least to a workgroup (one sentence of 300 tokens, 2400 rows: 18 us a call instead of 108; one of 4000 tokens, 16000 rows for each of 8 heads: 324 instead of 979).
+constexpr int kWeighGroups = 3072, kWeighChunk = 2048, kWeighRowGroups = 512;
+
+struct WeighPlan {
+    bool few;
+    int chunk, splits, split_rows;
+};
+
+template <int FMT, int DP>
+WeighPlan weigh_plan_of(int B, int heads, int rows, int tokens)
+{
+    typedef WeighShape<FMT, DP> W;
+    typedef WeighFew<FMT, DP> F;
+    static_assert(F::MOST % 16 == 0, "rows come in sixteens");
+    WeighPlan w;
+    w.few = rows <= F::MOST;
+    w.splits = 1;
+    w.split_rows = rows;
+    const int64_t pairs = (int64_t)B * heads;
+    if (w.few) {
+        constexpr int turn = 4 * F::TF;
+        const int64_t groups = std::max<int64_t>(1, kWeighGroups / pairs), even = (tokens + groups - 1) / groups;
+        w.chunk = (int)std::min<int64_t>(kWeighChunk / turn * turn, std::max<int64_t>(2 * turn, (even + turn - 1) / turn * turn));
+    } else {
+        w.chunk = W::TG;
+        const int64_t groups = pairs * ((tokens + W::TG - 1) / W::TG), turns = (rows + W::RQ - 1) / W::RQ;
+        const int64_t per = std::max<int64_t>(2, turns / std::max<int64_t>(1, kWeighRowGroups / groups));       // turns of a workgroup
+        w.splits = (int)((turns + per - 1) / per);
+        w.split_rows = (int)(per * W::RQ);
+    }
+    return w;
+}
+WeighPlan weigh_plan(int B, const dba_cache &c, int rows, int tokens)
+{
+    const auto plan = c.format == DBA_LOGP_F32 ? c.head_dim <= 64 ? weigh_plan_of<0, 64> : c.head_dim <= 128 ? weigh_plan_of<0, 128> : weigh_plan_of<0, 256>
+                                               : c.head_dim <= 64 ? weigh_plan_of<1, 64> : c.head_dim <= 128 ? weigh_plan_of<1, 128> : weigh_plan_of<1, 256>;
+    return plan(B, c.heads, rows, tokens);
+}
 
 template <int FMT, int DP, bool FULL>
 hipError_t weigh_one(WeighParams p, int B, int tokens, hipStream_t stream)
 {
     const int rows = p.n * (p.q_heads / p.heads);
-    if (rows <= WeighFew<FMT, DP>::MOST) {
-        constexpr int turn = 4 * WeighFew<FMT, DP>::TF;
-        const int64_t groups = std::max<int64_t>(1, kWeighGroups / ((int64_t)B * p.heads)), even = (tokens + groups - 1) / groups;
-        p.chunk = (int)std::min<int64_t>(kWeighChunk / turn * turn, std::max<int64_t>(2 * turn, (even + turn - 1) / turn * turn));
-        const auto kernel = rows <= 64 || WeighFew<FMT, DP>::MOST <= 64 ? dba_weigh_few_kernel<FMT, DP, FULL, 1> : dba_weigh_few_kernel<FMT, DP, FULL, WeighFew<FMT, DP>::MOST <= 64 ? 1 : 2>;
-        return launch(kernel, dim3((unsigned)((tokens + p.chunk - 1) / p.chunk), (unsigned)p.heads, (unsigned)B), dim3(256),
-                      (size_t)WeighFew<FMT, DP>::lds(rows, p.chunk), stream, p);
-    }
-    const unsigned blocks = (unsigned)((tokens + WeighShape<FMT, DP>::TG - 1) / WeighShape<FMT, DP>::TG);
-    return launch(dba_weigh_kernel<FMT, DP, FULL>, dim3(blocks, (unsigned)p.heads, (unsigned)B), dim3(256), 0, stream, p);
+    const WeighPlan w = weigh_plan_of<FMT, DP>(B, p.heads, rows, p.max_len);        // (laid out for max_len, as the workspace is)
+    p.chunk = w.chunk;
+    p.splits = w.splits;
+    p.split_rows = w.split_rows;
+    const dim3 grid((unsigned)((tokens + w.chunk - 1) / w.chunk), (unsigned)(p.heads * w.splits), (unsigned)B);
+    if (!w.few) return launch(dba_weigh_kernel<FMT, DP, FULL>, grid, dim3(256), 0, stream, p);
+    const auto kernel = rows <= 64 || WeighFew<FMT, DP>::MOST <= 64 ? dba_weigh_few_kernel<FMT, DP, FULL, 1> : dba_weigh_few_kernel<FMT, DP, FULL, WeighFew<FMT, DP>::MOST <= 64 ? 1 : 2>;
+    return launch(kernel, grid, dim3(256), (size_t)WeighFew<FMT, DP>::lds(rows, w.chunk), stream, p);
 }
 template <int FMT>
 hipError_t weigh_launch(const WeighParams &p, int B, int tokens, hipStream_t stream)
@@ -321,8 +356,9 @@ DBA_API int dba_shared_attend(int B, int n, int q_heads, const dba_heads *q, con
 
 DBA_API size_t dba_cache_weigh_workspace_bytes(int B, int n, int q_heads, const dba_cache *cache, int by_head, int max_len)
 {
-    if (attend_fault(B, n, q_heads, cache, max_len) || max_len > kMostTokens || by_head || cache->heads == 1) return 0;
-    return align256((size_t)B * cache->heads * max_len * 4);
+    if (attend_fault(B, n, q_heads, cache, max_len) || max_len > kMostTokens) return 0;
+    const int splits = weigh_plan(B, *cache, n * (q_heads / cache->heads), max_len).splits;
+    return splits == 1 && (by_head || cache->heads == 1) ? 0 : align256((size_t)B * cache->heads * splits * max_len * 4);
 }
 
 DBA_API int dba_cache_weigh(int B, int n, int q_heads, const dba_heads *q, const float *lse_dev, const dba_cache *cache, const int32_t *prefix_dev,
@@ -382,14 +418,16 @@ DBA_API int dba_cache_weigh(int B, int n, int q_heads, const dba_heads *q, const
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     const auto go = cache->format == DBA_LOGP_F32 ? weigh_launch<0> : cache->format == DBA_LOGP_F16 ? weigh_launch<1> : weigh_launch<2>;
     if (!need) return launched(who, go(p, B, in_place ? max_len : width, stream));
+    const int splits = weigh_plan(B, *cache, n * (q_heads / cache->heads), max_len).splits;
     WeighParams sums = p;
     sums.score = nullptr;
     sums.out = static_cast<float *>(workspace_dev);
-    sums.out_sent = (int64_t)cache->heads * max_len;
+    sums.out_sent = (int64_t)cache->heads * splits * max_len;
     sums.out_head = max_len;
     sums.width = max_len;
     hipError_t e = go(sums, B, max_len, stream);
-    if (e == hipSuccess) e = launch(dba_weigh_join_kernel, dim3((unsigned)((width + 255) / 256), (unsigned)B), dim3(256), 0, stream, p, static_cast<const float *>(workspace_dev));
+    if (e == hipSuccess) e = launch(dba_weigh_join_kernel, dim3((unsigned)((width + 255) / 256), (unsigned)heads_s, (unsigned)B), dim3(256), 0, stream, p,
+                                     static_cast<const float *>(workspace_dev), cache->heads / heads_s * splits);
     return launched(who, e);
 }
 

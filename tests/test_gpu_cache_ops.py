@@ -425,6 +425,8 @@ WEIGH = [
     (2, 25, 8, 2, 128, 16, [300, 0], [100, 25]),
     (1, 32, 8, 2, 64, 32, [1500], [32]),
     (3, 40, 9, 3, 40, 8, [70, 0, 200], [64, 128, 40]),
+    (1, 300, 8, 2, 64, 16, [100], [300]),
+    (2, 200, 6, 1, 256, 16, [0, 5], [200, 7]),
     (2, 90, 3, 1, 256, 16, [0, 300], [90, 200]),
 ]
 
