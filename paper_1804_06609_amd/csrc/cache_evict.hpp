@@ -60,32 +60,36 @@ __device__ __forceinline__ uint32_t evict_key(const EvictParams &p, const Choice
     return s != s ? 1u : ord_from_float(s);
 }
 
-// By a whole workgroup of W waves, every thread with the same result.
-template <int W>
-__device__ __forceinline__ Choice evict_choice(const EvictParams &p, int b, uint32_t (&s_wave)[W])
+// there: of the P tokens, so many are; safe: of the first and last ones, which go before all others, so many.
+__device__ __forceinline__ Choice choice_of(const EvictParams &p, int b, int P, int there, int safe)
 {
     Choice c;
-    c.P = span_of(p.prefix[b], 0, p.max_len).prefix;
-    // tokens that are there
-    const int t = (int)threadIdx.x, pages = c.P > 0 ? ((c.P - 1) >> p.from.page_shift) + 1 : 0;
-    uint32_t mine = 0;
-    for (int g = t; g < pages; g += 64 * W) {
-        const int first = g << p.from.page_shift;
-        if (evict_present(p, b, first)) mine += (uint32_t)min(1 << p.from.page_shift, c.P - first);
-    }
-    const int there = (int)sum_of_all<W>(mine, s_wave);
-    c.all = there == c.P;
+    c.P = P;
+    c.all = there == P;
     c.stay = min(p.budget ? min(p.keep, max(p.budget[b], 0)) : p.keep, there);
-    // the first and the last ones go before all others
-    int safe = (int)min((int64_t)c.P, (int64_t)min(p.sinks, c.P) + min(p.recent, c.P));
-    if (!c.all) {
-        mine = 0;
-        for (int x = t; x < c.P; x += 64 * W) mine += evict_safe(p, c, x) && evict_present(p, b, x);
-        safe = (int)sum_of_all<W>(mine, s_wave);
-    }
     c.among_safe = safe >= c.stay;
     c.need = (uint32_t)(c.among_safe ? c.stay : c.stay - safe);
     return c;
+}
+
+// Counts those, by a whole workgroup of W waves, every thread with the same result.
+template <int W>
+__device__ __forceinline__ int2 evict_counts(const EvictParams &p, int b, int P, uint32_t (&s_wave)[W])
+{
+    const int t = (int)threadIdx.x, pages = P > 0 ? ((P - 1) >> p.from.page_shift) + 1 : 0;
+    uint32_t mine = 0;
+    for (int g = t; g < pages; g += 64 * W) {
+        const int first = g << p.from.page_shift;
+        if (evict_present(p, b, first)) mine += (uint32_t)min(1 << p.from.page_shift, P - first);
+    }
+    const int there = (int)sum_of_all<W>(mine, s_wave);
+    int safe = (int)min((int64_t)P, (int64_t)min(p.sinks, P) + min(p.recent, P));
+    if (there != P) {
+        mine = 0;
+        for (int x = t; x < P; x += 64 * W) mine += (x < p.sinks || x >= P - p.recent) && evict_present(p, b, x);
+        safe = (int)sum_of_all<W>(mine, s_wave);
+    }
+    return make_int2(there, safe);
 }
 
 // The images are found digit by digit: 11, 11 and 10 bits.
@@ -179,7 +183,8 @@ __global__ __launch_bounds__(64 * W) void dba_evict_choose_kernel(EvictParams p)
     float s[NK];
 #pragma unroll
     for (int x = 0; x < NK; ++x) s[x] = x < reach && base + x * 64 < P ? score[base + x * 64] : 0.0f;      // (asked for before all else)
-    const Choice c = evict_choice<W>(p, b, s_wave[0]);
+    const int2 counts = evict_counts<W>(p, b, P, s_wave[0]);
+    const Choice c = choice_of(p, b, P, counts.x, counts.y);
     if (head == 0 && t == 0) p.new_prefix[b] = c.stay;
     if (c.stay == 0) return;
     uint32_t key[NK];
@@ -242,6 +247,7 @@ constexpr int kEvictFew = 4096;        // tokens of the first digit that are kep
 struct EvictLong {
     uint32_t *hist;                    // [B, heads_s, parts, kDigits]
     uint32_t *found;                   // [B, heads_s, 2]: the bar
+    int2 *counts;                      // [B]
     int parts;
 };
 
@@ -250,8 +256,13 @@ __global__ __launch_bounds__(64 * kEvictWaves) void dba_evict_count_kernel(Evict
     __shared__ uint32_t s_hist[kDigits], s_wave[kEvictWaves];
     const int t = (int)threadIdx.x, b = (int)blockIdx.z, head = (int)blockIdx.y, first = (int)blockIdx.x * kEvictPart;
     const float *const score = p.score + ((int64_t)b * p.score_sent + (int64_t)head * p.score_head);
-    const Choice c = evict_choice<kEvictWaves>(p, b, s_wave);
-    if (head == 0 && blockIdx.x == 0 && t == 0) p.new_prefix[b] = c.stay;
+    const int P = span_of(p.prefix[b], 0, p.max_len).prefix;
+    const int2 counts = evict_counts<kEvictWaves>(p, b, P, s_wave);
+    const Choice c = choice_of(p, b, P, counts.x, counts.y);
+    if (head == 0 && blockIdx.x == 0 && t == 0) {
+        p.new_prefix[b] = c.stay;
+        l.counts[b] = counts;
+    }
     for (int x = t; x < kDigits; x += 64 * kEvictWaves) s_hist[x] = 0;
     __syncthreads();
 #pragma unroll
@@ -270,7 +281,7 @@ __global__ __launch_bounds__(64 * kEvictWaves) void dba_evict_bar_kernel(EvictPa
     __shared__ uint32_t s_hist[kDigits], s_key[kEvictFew], s_wave[kEvictWaves], s_found[3], s_few;
     const int t = (int)threadIdx.x, b = (int)blockIdx.y, head = (int)blockIdx.x;
     const float *const score = p.score + ((int64_t)b * p.score_sent + (int64_t)head * p.score_head);
-    const Choice c = evict_choice<kEvictWaves>(p, b, s_wave);
+    const Choice c = choice_of(p, b, span_of(p.prefix[b], 0, p.max_len).prefix, l.counts[b].x, l.counts[b].y);
     if (c.stay == 0) return;
     constexpr int PER = kDigits / (64 * kEvictWaves);
     uint32_t n[PER] = {}, known = 0, need = c.need, few = 0;      // few: of the first digit, so many in s_key
@@ -296,27 +307,50 @@ __global__ __launch_bounds__(64 * kEvictWaves) void dba_evict_bar_kernel(EvictPa
             for (int x = t; x < kDigits; x += 64 * kEvictWaves) s_hist[x] = 0;
             if (t == 0) s_few = 0;
             __syncthreads();
+            // (the images of what is looked for are those of the scores between these two; a NaN's is alone in the digit 0)
+            const uint32_t lowest = known << (d.shift + d.bits);
+            const float least = float_from_ord(max(lowest, ord_from_float(-INFINITY))), most = float_from_ord(min(lowest | ((1u << (d.shift + d.bits)) - 1), ord_from_float(INFINITY)));
+            const bool gather = pass == 1 && s_found[2] <= kEvictFew;
             constexpr int U = 16;                      // loads under way
             for (int x0 = 0; x0 < (few ? 0 : c.P); x0 += U * 64 * kEvictWaves) {
                 float s[U];
 #pragma unroll
                 for (int x = 0; x < U; ++x) s[x] = score[min(x0 + x * 64 * kEvictWaves + t, c.P - 1)];
+                uint32_t hits = 0, key[U];
 #pragma unroll
                 for (int x = 0; x < U; ++x) {
+                    const bool in = known == 0 ? s[x] != s[x] : (s[x] >= least) & (s[x] <= most);
                     const int at = x0 + x * 64 * kEvictWaves + t;
-                    const uint32_t key = s[x] != s[x] ? 1u : ord_from_float(s[x]);
-                    bool in = at < c.P && key >> (d.shift + d.bits) == known;
-                    if (!__any(in)) continue;
-                    if (in) in = evict_key(p, c, b, at, s[x]) != 0;
-                    count_digit(s_hist, in, key >> d.shift & ((1u << d.bits) - 1));
-                    if (in && pass == 1 && s_found[2] <= kEvictFew) s_key[atomicAdd(&s_few, 1u)] = key;
+                    // (evict_key without a branch; zeros of either sign are one image)
+                    const bool safe = (at < p.sinks) | (at >= c.P - p.recent);
+                    const uint32_t image = known == 0 ? 1u : ord_from_float(s[x]);
+                    key[x] = (in & (at < c.P) & (safe == c.among_safe) & (image >> (d.shift + d.bits) == known)) ? image : 0;
+                    if (!c.all && key[x] && !evict_present(p, b, at)) key[x] = 0;
+                    hits += key[x] != 0;
+                }
+                if (gather) {                          // a place for each, with one atomic a wave
+                    const uint32_t up = wave_sum_up_to(hits);
+                    uint32_t place = 0;
+                    if (lane_id() == 63 && up) place = atomicAdd(&s_few, up);
+                    place = (uint32_t)__builtin_amdgcn_readlane((int)place, 63) + up - hits;
+#pragma unroll
+                    for (int x = 0; x < U; ++x)
+                        if (key[x]) s_key[place++] = key[x];
+                } else {
+#pragma unroll
+                    for (int x = 0; x < U; ++x) count_digit(s_hist, key[x] != 0, key[x] >> d.shift & ((1u << d.bits) - 1));
                 }
             }
+            if (gather) {
+                __syncthreads();
+                few = s_few;
+            }
             if (few)
-                for (uint32_t x = t; x < ((few + 63) & ~63u); x += 64 * kEvictWaves)
-                    count_digit(s_hist, x < few && s_key[x] >> (d.shift + d.bits) == known, s_key[min(x, few - 1)] >> d.shift & ((1u << d.bits) - 1));
+                for (uint32_t x = t; x < ((few + 63) & ~63u); x += 64 * kEvictWaves) {
+                    const uint32_t key = s_key[min(x, few - 1)];
+                    count_digit(s_hist, x < few && key >> (d.shift + d.bits) == known, key >> d.shift & ((1u << d.bits) - 1));
+                }
             __syncthreads();
-            if (pass == 1) few = s_few;
 #pragma unroll
             for (int x = 0; x < PER; ++x) n[x] = s_hist[kDigits - 1 - PER * t - x];
         }
@@ -340,7 +374,7 @@ __global__ __launch_bounds__(64 * kEvictWaves) void dba_evict_list_kernel(EvictP
     __shared__ uint32_t s_wave[2][kEvictWaves];
     const int lane = lane_id(), t = (int)threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6), b = (int)blockIdx.z, head = (int)blockIdx.y, first = (int)blockIdx.x * kEvictPart;
     const float *const score = p.score + ((int64_t)b * p.score_sent + (int64_t)head * p.score_head);
-    const Choice c = evict_choice<kEvictWaves>(p, b, s_wave[0]);
+    const Choice c = choice_of(p, b, span_of(p.prefix[b], 0, p.max_len).prefix, l.counts[b].x, l.counts[b].y);
     if (c.stay == 0 || first >= c.P) return;
     const Bar bar = {l.found[((int64_t)b * p.heads_s + head) * 2], l.found[((int64_t)b * p.heads_s + head) * 2 + 1]};
     // what lies before this part is counted once more, which is less than a launch for it
@@ -354,9 +388,11 @@ __global__ __launch_bounds__(64 * kEvictWaves) void dba_evict_list_kernel(EvictP
         for (int x = 0; x < U; ++x) {
             const int at = x0 + x * 64 * kEvictWaves + t;
             const uint32_t image = s[x] != s[x] ? 1u : ord_from_float(s[x]);
-            const bool safe = evict_safe(p, c, at), asked = safe == c.among_safe, here = at < first && (c.all || evict_present(p, b, min(at, first - 1)));
-            before_sure += here && (asked ? image > bar.least : !c.among_safe);
-            before_tied += here && asked && image == bar.least;
+            const bool safe = (at < p.sinks) | (at >= c.P - p.recent), asked = safe == c.among_safe;
+            bool here = at < first;
+            if (!c.all) here = here && evict_present(p, b, at);
+            before_sure += here & (asked ? image > bar.least : !c.among_safe);
+            before_tied += here & asked & (image == bar.least);
         }
     }
     before_sure = sum_of_all<kEvictWaves>(before_sure, s_wave[0]);

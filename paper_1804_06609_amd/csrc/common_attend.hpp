@@ -131,6 +131,7 @@ __global__ __launch_bounds__(256, 2) void dba_common_kernel(AttendParams p)
 
     auto work = [&](int u, auto buf_of, int page_next) {
         constexpr int buf = decltype(buf_of)::value;
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // this wave's loads into LDS, which a barrier does not wait for
         __syncthreads();                               // the tile has come, and nobody reads the last one any more
         constexpr int kb = buf * 2 * A::TILE;
         const unsigned long long live = (unsigned long long)(s_live[buf][0] | s_live[buf][1] << 16) | (unsigned long long)(s_live[buf][2] | s_live[buf][3] << 16) << 32;

@@ -583,6 +583,27 @@ def test_evict_pages_that_are_not_there(beam):  # noqa: F811
             check_evict(beam, torch.bfloat16, 3, 2, 16, 8, [70, 30, 95], [9, 5, 11], by_head, keep, 4, 12, spoil=spoil)
 
 
+@pytest.mark.parametrize("P", [4000, 18000])
+def test_evict_scores_around_nothing(beam, P):  # noqa: F811
+    """Zeros of either sign are equal, and lie between the smallest numbers; infinities are greater than the greatest."""
+    g = gen(P)
+    small = (torch.rand(P + 8, generator=g) - 0.5) * 1e-40
+    small[::3], small[1::3] = 0.0, -0.0
+    large = (torch.rand(P + 8, generator=g) - 0.5) * 6e38
+    large[::4], large[1::4] = INF, -INF
+    score = torch.stack([small, -small.abs(), large, -large.abs()])[None]
+    for keep in (P // 5, P // 2, P - P // 6):
+        check_evict(beam, torch.float16, 1, 4, 8, 64, [P], [0], True, keep, 0, 0, score=score)
+
+
+def test_evict_long_rows_with_pages_that_are_not_there(beam):  # noqa: F811
+    def spoil(table, new_table):
+        table[0, 5:9], table[0, 100], table[1, ::2] = -1, 2**31 - 1, -1
+    for by_head in (True, False):
+        for keep, recent in ((3000, 40), (9000, 9000), (17999, 0)):
+            check_evict(beam, torch.float16, 2, 2, 8, 64, [18000, 17000], [70, 5], by_head, keep, 400, recent, spoil=spoil)
+
+
 @pytest.mark.parametrize("P,keep", [(66000, 30000), (140000, 5)])
 def test_evict_of_long_sentences(beam, P, keep):  # noqa: F811
     score = torch.randn(1, 1, P + 64, generator=gen(1)).round(decimals=2)
