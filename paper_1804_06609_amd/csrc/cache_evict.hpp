@@ -239,7 +239,7 @@ __global__ __launch_bounds__(64 * W) void dba_evict_choose_kernel(EvictParams p)
 }
 
 // Longer rows in three launches, with a workgroup for each kEvictPart tokens: counts of the first digit; the bar, from those counts and the tokens of that digit; the list.
-// (One choice of 16384 of 65000 tokens, 4 sentences: 5.5 + 33 + 19 us; one workgroup took 103.)
+// (One choice of 16384 of 65000 tokens, 4 sentences: 5.5 + 24 + 18 us; one workgroup took 103.)
 constexpr int kEvictWaves = 16, kEvictPart = 4096, kEvictPer = kEvictPart / (64 * kEvictWaves);
 
 constexpr int kEvictFew = 4096;        // tokens of the first digit that are kept rather than looked for once more

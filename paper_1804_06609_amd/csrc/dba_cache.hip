@@ -127,7 +127,7 @@ void lay_out(AttendParams &p, const AttendPlan &plan, int B, const dba_cache &c)
 // Up to WeighFew::MOST rows a head the waves go through tokens, else through rows.  Of the former a workgroup has as few tokens as fill the GPU
 // (kWeighGroups workgroups), but two tiles a wave at least, and sums that fit into LDS.  Of the latter rows are split where tokens alone leave GPU empty, two
 // turns of rows in LDS at least to a workgroup (one sentence of 300 tokens, 2400 rows: 18 us a call instead of 108; one of 4000 tokens, 16000 rows for each of 8 heads: 324 instead of 979).
-constexpr int kWeighGroups = 3072, kWeighChunk = 2048, kWeighRowGroups = 512;
+constexpr int kWeighGroups = 3200, kWeighChunk = 2048, kWeighRowGroups = 512;
 
 struct WeighPlan {
     bool few;

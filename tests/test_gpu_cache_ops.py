@@ -622,7 +622,7 @@ def test_offsets_beyond_32_bits(beam):  # noqa: F811
         k_pages[p].normal_(generator=g)
     small = torch.stack([k_pages[p] for p in last])
     q = torch.randn(3, 2, 8, D, generator=gen(1)).bfloat16().cuda()
-    score = torch.rand(1, H, 3072, generator=gen(2)).cuda()
+    score = torch.rand(1, H, 3000, generator=gen(2)).cuda()
     results = []
     for pool, ids in ((k_pages, last), (small, range(5))):
         ids = ints(*ids)
