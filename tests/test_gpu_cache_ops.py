@@ -163,6 +163,30 @@ def test_append_norms_of_any_size(beam, dtype):  # noqa: F811
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("wide", [False, True])
+def test_append_of_keys_alone_and_weights_of_one_side(beam, dtype, wide):  # noqa: F811
+    B, n, H, D = 2, 5, 3, 64
+    k_pages, v_pages, table = a_cache(1, B, 32, H, D, 8, dtype)
+    qkv = torch.randn(B, n, 3 * H, D, generator=gen(1)).to(dtype)
+    q, k, v = qkv.chunk(3, dim=2)
+    dev, first = qkv.cuda().chunk(3, dim=2), ints(0, 9)
+    w = (torch.rand(H, D, generator=gen(2)) + 0.5).to(torch.float32 if wide else dtype)
+    none, inv = torch.zeros(n), torch.zeros(0)
+    for weights in ((None, None), (w, None), (None, w)):
+        for with_q in (True, False):
+            more = dict(eps=1e-6, q_weight=None if weights[0] is None or not with_q else w.cuda(), k_weight=None if weights[1] is None else w.cuda())
+            got = beam.append(dev[1], dev[2], k_pages, v_pages, *cuda(table, first), q=dev[0] if with_q else None, **more)
+            assert (got is None) == (not with_q)
+            for b in range(B):
+                t = int(first[b]) + torch.arange(n)
+                at = table[b, t // 8].long().cuda(), (t % 8).cuda()
+                for have, x, weight in ((k_pages[at], k, weights[1]),) + (((got[b], q, weights[0]),) if with_q else ()):
+                    want, tol = normed_rotated(x[b], weight, 1e-6, none, None, inv, False)
+                    assert ((have.cpu().double() - want).abs() <= U[dtype] * want.abs() + tol * (1 + U[dtype]) + LEAST[dtype]).all()
+                assert torch.equal(v_pages[at].cpu(), v[b])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 def test_append_without_norms_or_axes_to_speak_of_is_append(beam, dtype):  # noqa: F811
     """Each is 4 u32 (|x0| + |x1|) and a rounding from the definition at most (as in test_gpu_beam_ops.py; the angles are the same)."""
     k_pages, v_pages, table = a_cache(1, 2, 64, 2, 64, 8, dtype)
