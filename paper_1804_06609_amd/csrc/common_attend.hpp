@@ -46,11 +46,15 @@ struct CommonShape {
 
 // As in dba_attend_kernel both products are transposed and the weights stay in registers: S^T = K Q^T leaves a lane with 16 tokens of one row for each 32 of them, which in
 // their order are what O^T = V^T P^T takes, V^T coming out of LDS through the transposing read.  The path of a tile that is all there has no branch but the one around
-// new maxima, and 170 instructions of the VALU beside 32 matrix ones.
+// new maxima.
 //
-// Bound: LDS, whose reads take 64 bytes a clock (a counter of its busy clocks says nine tenths of the time; 8192 rows of 128 over 8000 tokens, 4 heads: 173 us, 0.77
-// PFLOP/s).  64 rows a wave would halve what is read of it, but a wave alone on its SIMD has nothing to fill the waits with (209 us), and two have not the registers: with a half of
-// each tile's tokens for either, 35 spilled ones make every tile wait for the next one's loads (267 us).
+// Weights are rounded to 16 bits for the matrix units, and what that leaves of them goes through a second product with the same values: outputs are then as far from the exact ones as their own
+// rounding (1.66e-3 in bf16, 2.07e-4 in fp16) and no further, as they would be without it (2.3e-3, 2.9e-4).  It costs half as many matrix instructions again and 48 others a tile, and nothing of LDS: 8192
+// rows of 128 over 8000 tokens, 4 heads: 224 us instead of 173 to 181; 5120 over 1500, 8 heads: 77 instead of 65.
+//
+// Bound: no unit alone.  In the first of these the matrix units are at work for 49 % of the clocks, the VALU for 39, LDS, whose reads take 64 bytes a clock, for 68; with two waves a SIMD the first two hardly
+// overlap (0.60 PFLOP/s, each product counted once).  64 rows a wave would halve what is read of LDS, but have not the registers (when the kernel had one product and 173 us: a wave alone on its SIMD 209, two with
+// a half of each tile's tokens for either, whose 35 spilled registers make every tile wait for the next one's loads, 267).
 template <int FMT, int DP>
 __global__ __launch_bounds__(256, 2) void dba_common_kernel(AttendParams p)
 {
@@ -193,9 +197,13 @@ __global__ __launch_bounds__(256, 2) void dba_common_kernel(AttendParams p)
         for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
-                u32x4 w;
+                u32x4 w, rest;                         // weights in 16 bits, and what that leaves of them
 #pragma unroll
-                for (int x = 0; x < 4; ++x) w[x] = pack2<FMT>(s[b][y * 8 + 2 * x], s[b][y * 8 + 2 * x + 1]);
+                for (int x = 0; x < 4; ++x) {
+                    const float w0 = s[b][y * 8 + 2 * x], w1 = s[b][y * 8 + 2 * x + 1];
+                    w[x] = pack2<FMT>(w0, w1);
+                    rest[x] = rest2<FMT>(w0, w1, w[x]);
+                }
 #pragma unroll
                 for (int d = 0; d < DB; ++d) {
                     typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
@@ -203,6 +211,7 @@ __global__ __launch_bounds__(256, 2) void dba_common_kernel(AttendParams p)
                     v.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(s_mem + value_at[d] + (kb + (b * 32 + y * 16) * A::ROW)));
                     v.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(s_mem + value_at[d] + (kb + (b * 32 + y * 16 + 8) * A::ROW)));
                     o[d] = mfma16<FMT>(__builtin_bit_cast(u32x4, v), w, o[d]);
+                    o[d] = mfma16<FMT>(__builtin_bit_cast(u32x4, v), rest, o[d]);
                 }
             }
     };

@@ -92,6 +92,25 @@ __device__ __forceinline__ uint32_t pack2(float a, float b)
     }
 }
 
+// What is left of a and b where pack2 has made `both` of them, packed alike.  The differences are exact; an instruction each, which takes its half of `both` as it is.
+// (In assembly for fp16.  Whatever wrote a and b has been waited for by the instruction that made `both`.)
+template <int FMT>
+__device__ __forceinline__ uint32_t rest2(float a, float b, uint32_t both)
+{
+    if constexpr (FMT == 1) {
+        float x, y;
+        asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[0,0,0] op_sel_hi:[1,0,0]" : "=v"(x) : "v"(both), "v"(a));
+        asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(y) : "v"(both), "v"(b));
+        return pack2<FMT>(x, y);
+    } else {
+        typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+        uint32_t low = 0x0000BF80u, high = 0xBF800000u;     // (-1, 0) and (0, -1); kept from the compiler, which makes the first an inline constant that is read as another number
+        asm("" : "+s"(low), "+s"(high));
+        const b2 v = __builtin_bit_cast(b2, both);
+        return pack2<FMT>(__builtin_amdgcn_fdot2_f32_bf16(v, __builtin_bit_cast(b2, low), a, false), __builtin_amdgcn_fdot2_f32_bf16(v, __builtin_bit_cast(b2, high), b, false));
+    }
+}
+
 template <int FMT>
 __device__ __forceinline__ float low_half(uint32_t w)
 {
@@ -242,13 +261,15 @@ struct AttendShape {
 // 225 -> 140 us when this was chosen).  There the parts of the token axis vary slowest, so that what is left of short sentences comes last; where
 // tokens are read once they vary fastest (4 sentences of 50000 and more: 186 instead of 199 us).
 //
-// PARTS: results are always left as parts, for another join; and the nodes of several sentences may be taken for those of one.
+// PARTS: results are always left as parts, for another join; and the nodes of several sentences may be taken for those of one.  What the rounding leaves of weights goes through a second
+// product whatever the form (64 sentences of 80 rows of 128, 8 heads, over 900 to 1500 tokens: 121 us instead of 101; 128 of 64 rows over 110 to 160, 4 heads: 26.5 either way).
 template <int FMT, int DP, int QT, bool ROWS, int SIDE, bool PARTS = false>
 __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) void dba_attend_kernel(AttendParams p)
 {
     typedef AttendShape<FMT, DP, QT, ROWS> A;
     typedef typename Elem<FMT>::type E;
     constexpr int KS = A::KS, DT = A::DT, NT = A::NT, CT = A::CT, TT = A::TT, FC = Frag<FMT>::C, NE = 16 / A::ES;
+    constexpr bool REST = A::REST || (PARTS && FMT != 0);
     extern __shared__ __align__(16) unsigned char s_mem[];
     __shared__ float s_ml[4][16 * QT][2];
     __shared__ unsigned long long s_live[2][4];
@@ -525,7 +546,8 @@ __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) vo
                         const float w0 = s[t + i / 2][j][i % 2 * 2], w1 = s[t + i / 2][j][i % 2 * 2 + 1];
                         const uint32_t both = pack2<FMT>(w0, w1);
                         w[j].c[0][i] = both;
-                        if constexpr (A::REST) rest[j].c[0][i] = pack2<FMT>(w0 - low_half<FMT>(both), w1 - high_half<FMT>(both));
+                        if constexpr (REST && PARTS) rest[j].c[0][i] = rest2<FMT>(w0, w1, both);
+                        else if constexpr (REST) rest[j].c[0][i] = pack2<FMT>(w0 - low_half<FMT>(both), w1 - high_half<FMT>(both));
                     }
 #pragma unroll
                 for (int d = 0; d < DT; ++d) {
@@ -539,7 +561,7 @@ __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) vo
 #pragma unroll
                     for (int j = 0; j < QT; ++j) {
                         o[j][d] = mfma32<FMT>(vf, w[j], o[j][d]);
-                        if constexpr (A::REST) o[j][d] = mfma32<FMT>(vf, rest[j], o[j][d]);
+                        if constexpr (REST) o[j][d] = mfma32<FMT>(vf, rest[j], o[j][d]);
                     }
                 }
             }
