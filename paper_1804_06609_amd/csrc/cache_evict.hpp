@@ -423,6 +423,7 @@ __global__ __launch_bounds__(64 * kEvictWaves) void dba_evict_list_kernel(EvictP
 }
 
 constexpr int kMoveThreads = 256, kMoveItems = 4;      // chunks of keys, and of values, that a thread has under way
+constexpr int kMoveScores = 8;                         // scores of a thread, where a row is much wider than what is moved
 
 // Token j of the new pages is the list's j-th, or behind those the tree's (j - stay)-th.  Bound: memory; each thread moves 16 bytes of keys and of values at
 // a time, which of a token lie side by side.  Nothing that is moved is asked for again, so it goes past the caches (64 x 1200 tokens of 8 heads of 128 in bf16, a choice for
@@ -495,9 +496,12 @@ __global__ __launch_bounds__(kMoveThreads) void dba_evict_move_kernel(EvictParam
         }
     }
     if (!p.new_score) return;
-    const uint64_t scores = (uint64_t)p.heads_s * (uint32_t)p.width;
-    for (uint64_t x = (uint64_t)blockIdx.x * kMoveThreads + t; x < scores; x += (uint64_t)gridDim.x * kMoveThreads) {
-        const int h = (int)(x / (uint32_t)p.width), j = (int)(x - (uint64_t)h * (uint32_t)p.width);
+    // (h, j) of heads_s rows of `width`, one behind the other: no division a score
+    const uint32_t width = (uint32_t)p.width, start = blockIdx.x * kMoveThreads + (uint32_t)t, stride = gridDim.x * kMoveThreads;
+    uint32_t h = start / width, j0 = start - h * width;
+    const uint32_t rows_on = stride / width, on = stride - rows_on * width;
+    for (; h < (uint32_t)p.heads_s; h += rows_on + (j0 + on >= width), j0 = j0 + on >= width ? j0 + on - width : j0 + on) {
+        const int j = (int)j0;
         const float *const score = p.score + ((int64_t)b * p.score_sent + (int64_t)h * p.score_head);
         float s = 0.0f;
         if (j < total) s = score[j < stay ? list[(int64_t)h * p.cap + j] : span.prefix + (j - stay)];

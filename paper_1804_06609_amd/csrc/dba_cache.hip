@@ -538,10 +538,11 @@ DBA_API int dba_cache_evict(int B, const dba_cache *cache, const int32_t *new_ta
         if (e == hipSuccess) e = launch(dba_evict_list_kernel, parts, threads, 0, stream, p, l);
     }
     if (e == hipSuccess) {
-        // (without a tree no more than keep tokens are moved)
+        // (without a tree no more than keep tokens are moved; scores are written for all of a row)
         const int64_t items = (int64_t)(tree_dev ? max_len : p.cap) * p.heads * p.chunks, turn = kMoveThreads * kMoveItems;
-        const int64_t most = std::max<int64_t>(1, 8192 / B);
-        e = launch(dba_evict_move_kernel, dim3((unsigned)std::min((items + turn - 1) / turn, most), (unsigned)B), dim3(kMoveThreads), 0, stream, p);
+        const int64_t scores = new_score_dev ? (int64_t)heads_s * width : 0, score_turn = kMoveThreads * kMoveScores;
+        const int64_t most = std::max<int64_t>(1, 8192 / B), wanted = std::max((items + turn - 1) / turn, (scores + score_turn - 1) / score_turn);
+        e = launch(dba_evict_move_kernel, dim3((unsigned)std::min(wanted, most), (unsigned)B), dim3(kMoveThreads), 0, stream, p);
     }
     return launched(who, e);
 }
