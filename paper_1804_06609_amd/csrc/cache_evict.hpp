@@ -72,24 +72,21 @@ __device__ __forceinline__ Choice choice_of(const EvictParams &p, int b, int P, 
     return c;
 }
 
-// Counts those, by a whole workgroup of W waves, every thread with the same result.
+// Counts those, by a whole workgroup of W waves, every thread with the same result.  A page is there with all of its tokens, so pages are what is gone through.
 template <int W>
 __device__ __forceinline__ int2 evict_counts(const EvictParams &p, int b, int P, uint32_t (&s_wave)[W])
 {
     const int t = (int)threadIdx.x, pages = P > 0 ? ((P - 1) >> p.from.page_shift) + 1 : 0;
-    uint32_t mine = 0;
+    const int sinks = min(p.sinks, P), rest = max(P - p.recent, sinks);        // places before the one and from the other on are safe
+    uint32_t mine = 0, mine_safe = 0;
     for (int g = t; g < pages; g += 64 * W) {
-        const int first = g << p.from.page_shift;
-        if (evict_present(p, b, first)) mine += (uint32_t)min(1 << p.from.page_shift, P - first);
+        const int first = g << p.from.page_shift, last = first + min(1 << p.from.page_shift, P - first);
+        if (!evict_present(p, b, first)) continue;
+        mine += (uint32_t)(last - first);
+        mine_safe += (uint32_t)(max(min(last, sinks) - first, 0) + max(last - max(first, rest), 0));
     }
     const int there = (int)sum_of_all<W>(mine, s_wave);
-    int safe = (int)min((int64_t)P, (int64_t)min(p.sinks, P) + min(p.recent, P));
-    if (there != P) {
-        mine = 0;
-        for (int x = t; x < P; x += 64 * W) mine += (x < p.sinks || x >= P - p.recent) && evict_present(p, b, x);
-        safe = (int)sum_of_all<W>(mine, s_wave);
-    }
-    return make_int2(there, safe);
+    return make_int2(there, there == P ? sinks + P - rest : (int)sum_of_all<W>(mine_safe, s_wave));
 }
 
 // The images are found digit by digit: 11, 11 and 10 bits.
@@ -238,8 +235,10 @@ __global__ __launch_bounds__(64 * W) void dba_evict_choose_kernel(EvictParams p)
         if (x < reach) list_wave(p, c, bar, b, list, base + x * 64, base + x * 64 < P, key[x], s0, e0);
 }
 
-// Longer rows in three launches, with a workgroup for each kEvictPart tokens: counts of the first digit; the bar, from those counts and the tokens of that digit; the list.
-// (One choice of 16384 of 65000 tokens, 4 sentences: 5.5 + 24 + 18 us; one workgroup took 103.)
+// Longer rows in launches with a workgroup for each kEvictPart tokens: what is there of a sentence; counts of the first digit; the bar, from those counts and the tokens of that digit, by one
+// workgroup a row; how many stay of each part; the list.  Each goes over a row's scores, or a sentence's pages, once, and the last over the counts of the parts before its own.
+// (One choice of 16384 of 65000 tokens, 4 sentences: 4.6 + 4.8 + 24 + 4.6 + 6.2 us; one workgroup took 103.  8 choices of 64 of a million tokens 0.37 ms, of four million 1.36; where each
+// part counted all scores before it 1.33 and 14.4, and with an absent page among 16 tokens each, which each part looked for, 3.1 and 43.7 instead of 0.42 and 1.51.)
 constexpr int kEvictWaves = 16, kEvictPart = 4096, kEvictPer = kEvictPart / (64 * kEvictWaves);
 
 constexpr int kEvictFew = 4096;        // tokens of the first digit that are kept rather than looked for once more
@@ -248,21 +247,34 @@ struct EvictLong {
     uint32_t *hist;                    // [B, heads_s, parts, kDigits]
     uint32_t *found;                   // [B, heads_s, 2]: the bar
     int2 *counts;                      // [B]
+    uint2 *tally;                      // [B, heads_s, parts]: sure to stay, and equal to the bar
     int parts;
 };
 
-__global__ __launch_bounds__(64 * kEvictWaves) void dba_evict_count_kernel(EvictParams p, EvictLong l)
+__global__ __launch_bounds__(64 * kEvictWaves) void dba_evict_there_kernel(EvictParams p, EvictLong l)
 {
-    __shared__ uint32_t s_hist[kDigits], s_wave[kEvictWaves];
-    const int t = (int)threadIdx.x, b = (int)blockIdx.z, head = (int)blockIdx.y, first = (int)blockIdx.x * kEvictPart;
-    const float *const score = p.score + ((int64_t)b * p.score_sent + (int64_t)head * p.score_head);
-    const int P = span_of(p.prefix[b], 0, p.max_len).prefix;
+    __shared__ uint32_t s_wave[kEvictWaves];
+    const int b = (int)blockIdx.x, P = span_of(p.prefix[b], 0, p.max_len).prefix;
     const int2 counts = evict_counts<kEvictWaves>(p, b, P, s_wave);
-    const Choice c = choice_of(p, b, P, counts.x, counts.y);
-    if (head == 0 && blockIdx.x == 0 && t == 0) {
-        p.new_prefix[b] = c.stay;
+    if (threadIdx.x == 0) {
+        p.new_prefix[b] = choice_of(p, b, P, counts.x, counts.y).stay;
         l.counts[b] = counts;
     }
+}
+
+// The choice of a long row, once its sentence's tokens have been counted.
+__device__ __forceinline__ Choice choice_of(const EvictParams &p, const EvictLong &l, int b)
+{
+    return choice_of(p, b, span_of(p.prefix[b], 0, p.max_len).prefix, l.counts[b].x, l.counts[b].y);
+}
+
+__global__ __launch_bounds__(64 * kEvictWaves) void dba_evict_count_kernel(EvictParams p, EvictLong l)
+{
+    __shared__ uint32_t s_hist[kDigits];
+    const int t = (int)threadIdx.x, b = (int)blockIdx.z, head = (int)blockIdx.y, first = (int)blockIdx.x * kEvictPart;
+    const float *const score = p.score + ((int64_t)b * p.score_sent + (int64_t)head * p.score_head);
+    const Choice c = choice_of(p, l, b);
+    if (first >= c.P) return;                          // (nobody asks for it)
     for (int x = t; x < kDigits; x += 64 * kEvictWaves) s_hist[x] = 0;
     __syncthreads();
 #pragma unroll
@@ -281,7 +293,7 @@ __global__ __launch_bounds__(64 * kEvictWaves) void dba_evict_bar_kernel(EvictPa
     __shared__ uint32_t s_hist[kDigits], s_key[kEvictFew], s_wave[kEvictWaves], s_found[3], s_few;
     const int t = (int)threadIdx.x, b = (int)blockIdx.y, head = (int)blockIdx.x;
     const float *const score = p.score + ((int64_t)b * p.score_sent + (int64_t)head * p.score_head);
-    const Choice c = choice_of(p, b, span_of(p.prefix[b], 0, p.max_len).prefix, l.counts[b].x, l.counts[b].y);
+    const Choice c = choice_of(p, l, b);
     if (c.stay == 0) return;
     constexpr int PER = kDigits / (64 * kEvictWaves);
     uint32_t n[PER] = {}, known = 0, need = c.need, few = 0;      // few: of the first digit, so many in s_key
@@ -369,47 +381,69 @@ __global__ __launch_bounds__(64 * kEvictWaves) void dba_evict_bar_kernel(EvictPa
     }
 }
 
+// How many of a wave's stretch of this part are sure to stay, and equal to the bar: each a whole wave's number.  key: their images.
+__device__ __forceinline__ uint2 evict_stretch(const EvictParams &p, const Choice &c, const Bar &bar, int b, const float *score, int base, uint32_t (&key)[kEvictPer])
+{
+    uint2 n = make_uint2(0, 0);
+#pragma unroll
+    for (int x = 0; x < kEvictPer; ++x) {
+        const int at = base + x * 64;
+        key[x] = at < c.P ? evict_key(p, c, b, at, score[at]) : 0;
+        const uint2 one = at < c.P ? count_of(p, c, bar, b, at, key[x]) : make_uint2(0, 0);
+        n.x += (uint32_t)__popcll(__ballot(one.x));
+        n.y += (uint32_t)__popcll(__ballot(one.y));
+    }
+    return n;
+}
+
+__global__ __launch_bounds__(64 * kEvictWaves) void dba_evict_tally_kernel(EvictParams p, EvictLong l)
+{
+    __shared__ uint32_t s_wave[2][kEvictWaves];
+    const int lane = lane_id(), t = (int)threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6), b = (int)blockIdx.z, head = (int)blockIdx.y, first = (int)blockIdx.x * kEvictPart;
+    const float *const score = p.score + ((int64_t)b * p.score_sent + (int64_t)head * p.score_head);
+    const Choice c = choice_of(p, l, b);
+    if (c.stay == 0 || first >= c.P) return;
+    const int64_t row = (int64_t)b * p.heads_s + head;
+    const Bar bar = {l.found[row * 2], l.found[row * 2 + 1]};
+    uint32_t key[kEvictPer];
+    const uint2 n = evict_stretch(p, c, bar, b, score, first + wave * kEvictPer * 64 + lane, key);
+    if (lane == 0) {
+        s_wave[0][wave] = n.x;
+        s_wave[1][wave] = n.y;
+    }
+    __syncthreads();
+    if (t) return;
+    uint2 all = make_uint2(0, 0);
+    for (int w = 0; w < kEvictWaves; ++w) {
+        all.x += s_wave[0][w];
+        all.y += s_wave[1][w];
+    }
+    l.tally[row * l.parts + blockIdx.x] = all;
+}
+
 __global__ __launch_bounds__(64 * kEvictWaves) void dba_evict_list_kernel(EvictParams p, EvictLong l)
 {
     __shared__ uint32_t s_wave[2][kEvictWaves];
     const int lane = lane_id(), t = (int)threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6), b = (int)blockIdx.z, head = (int)blockIdx.y, first = (int)blockIdx.x * kEvictPart;
     const float *const score = p.score + ((int64_t)b * p.score_sent + (int64_t)head * p.score_head);
-    const Choice c = choice_of(p, b, span_of(p.prefix[b], 0, p.max_len).prefix, l.counts[b].x, l.counts[b].y);
+    const Choice c = choice_of(p, l, b);
     if (c.stay == 0 || first >= c.P) return;
-    const Bar bar = {l.found[((int64_t)b * p.heads_s + head) * 2], l.found[((int64_t)b * p.heads_s + head) * 2 + 1]};
-    // what lies before this part is counted once more, which is less than a launch for it
+    const int64_t row = (int64_t)b * p.heads_s + head;
+    const Bar bar = {l.found[row * 2], l.found[row * 2 + 1]};
     uint32_t before_sure = 0, before_tied = 0;
-    constexpr int U = 16;
-    for (int x0 = 0; x0 < first; x0 += U * 64 * kEvictWaves) {
-        float s[U];
-#pragma unroll
-        for (int x = 0; x < U; ++x) s[x] = score[min(x0 + x * 64 * kEvictWaves + t, first - 1)];
-#pragma unroll
-        for (int x = 0; x < U; ++x) {
-            const int at = x0 + x * 64 * kEvictWaves + t;
-            const uint32_t image = s[x] != s[x] ? 1u : ord_from_float(s[x]);
-            const bool safe = (at < p.sinks) | (at >= c.P - p.recent), asked = safe == c.among_safe;
-            bool here = at < first;
-            if (!c.all) here = here && evict_present(p, b, at);
-            before_sure += here & (asked ? image > bar.least : !c.among_safe);
-            before_tied += here & asked & (image == bar.least);
-        }
+    for (int x = t; x < (int)blockIdx.x; x += 64 * kEvictWaves) {
+        const uint2 n = l.tally[row * l.parts + x];
+        before_sure += n.x;
+        before_tied += n.y;
     }
+    const int base = first + wave * kEvictPer * 64 + lane;
+    uint32_t key[kEvictPer];
+    const uint2 n = evict_stretch(p, c, bar, b, score, base, key);
     before_sure = sum_of_all<kEvictWaves>(before_sure, s_wave[0]);
     before_tied = sum_of_all<kEvictWaves>(before_tied, s_wave[1]);
-    const int base = first + wave * kEvictPer * 64 + lane;
-    uint32_t key[kEvictPer], n_sure = 0, n_tied = 0;
-#pragma unroll
-    for (int x = 0; x < kEvictPer; ++x) {
-        const int at = base + x * 64;
-        key[x] = at < c.P ? evict_key(p, c, b, at, score[at]) : 0;
-        const uint2 n = at < c.P ? count_of(p, c, bar, b, at, key[x]) : make_uint2(0, 0);
-        n_sure += (uint32_t)__popcll(__ballot(n.x));
-        n_tied += (uint32_t)__popcll(__ballot(n.y));
-    }
     if (lane == 0) {
-        s_wave[0][wave] = n_sure;
-        s_wave[1][wave] = n_tied;
+        s_wave[0][wave] = n.x;
+        s_wave[1][wave] = n.y;
     }
     __syncthreads();
     uint32_t s0 = before_sure, e0 = before_tied;

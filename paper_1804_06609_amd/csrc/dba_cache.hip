@@ -431,10 +431,10 @@ DBA_API int dba_cache_weigh(int B, int n, int q_heads, const dba_heads *q, const
     return launched(who, e);
 }
 
-// The workspace: lists, and for long rows counts of digits and bars.
+// The workspace: lists, and for long rows counts of digits, bars, and what is there and stays.
 struct EvictPlan {
     int parts;                         // 0: rows are short
-    size_t hist_at, found_at, counts_at, total;
+    size_t hist_at, found_at, counts_at, tally_at, total;
 };
 constexpr int kShortRow = 16384;
 
@@ -446,7 +446,8 @@ static EvictPlan evict_plan(int B, int heads_s, int keep, int max_len)
     e.hist_at = align256(rows * std::min(keep, max_len) * 4);
     e.found_at = e.hist_at + align256(rows * e.parts * kDigits * 4);
     e.counts_at = e.found_at + (e.parts ? align256(rows * 8) : 0);
-    e.total = e.counts_at + (e.parts ? align256((size_t)B * 8) : 0);
+    e.tally_at = e.counts_at + (e.parts ? align256((size_t)B * 8) : 0);
+    e.total = e.tally_at + align256(rows * e.parts * 8);
     return e;
 }
 
@@ -531,10 +532,13 @@ DBA_API int dba_cache_evict(int B, const dba_cache *cache, const int32_t *new_ta
         e = launch(kernel, dim3((unsigned)heads_s, (unsigned)B), dim3(max_len <= 1024 ? 256u : max_len <= 4096 ? 512u : 1024u), 0, stream, p);
     } else {
         unsigned char *const ws = static_cast<unsigned char *>(workspace_dev);
-        const EvictLong l = {reinterpret_cast<uint32_t *>(ws + plan.hist_at), reinterpret_cast<uint32_t *>(ws + plan.found_at), reinterpret_cast<int2 *>(ws + plan.counts_at), plan.parts};
+        const EvictLong l = {reinterpret_cast<uint32_t *>(ws + plan.hist_at), reinterpret_cast<uint32_t *>(ws + plan.found_at), reinterpret_cast<int2 *>(ws + plan.counts_at),
+                             reinterpret_cast<uint2 *>(ws + plan.tally_at), plan.parts};
         const dim3 parts((unsigned)plan.parts, (unsigned)heads_s, (unsigned)B), threads(64 * kEvictWaves);
-        e = launch(dba_evict_count_kernel, parts, threads, 0, stream, p, l);
+        e = launch(dba_evict_there_kernel, dim3((unsigned)B), threads, 0, stream, p, l);
+        if (e == hipSuccess) e = launch(dba_evict_count_kernel, parts, threads, 0, stream, p, l);
         if (e == hipSuccess) e = launch(dba_evict_bar_kernel, dim3((unsigned)heads_s, (unsigned)B), threads, 0, stream, p, l);
+        if (e == hipSuccess) e = launch(dba_evict_tally_kernel, parts, threads, 0, stream, p, l);
         if (e == hipSuccess) e = launch(dba_evict_list_kernel, parts, threads, 0, stream, p, l);
     }
     if (e == hipSuccess) {

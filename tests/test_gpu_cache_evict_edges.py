@@ -39,3 +39,40 @@ def test_evict_to_few_tokens_of_a_wide_row_takes_no_longer_than_to_many(beam, P,
     did it alone."""
     few, many = (evict_ms(beam, P, width, 8, 64, 64, keep) for keep in (64, 2900))
     assert few < 1.3 * many, (few, many)
+
+
+@pytest.mark.parametrize("page,absent", [(256, ()), (16, (0, 77, -1))])
+def test_evict_from_four_times_the_tokens_takes_about_four_times_the_time(beam, page, absent):  # noqa: F811
+    """The choice goes over a row's scores, and a sentence's pages, a fixed number of times: 0.37 and 1.36 ms (0.42 and 1.51 with absent pages); 1.33 and 14.4 (3.1 and 43.7) where
+    each part of a row counted all before it."""
+    one, four = (evict_ms(beam, P, P + 64, 8, 8, page, 64, absent) for P in (1 << 20, 1 << 22))
+    assert four < 6.0 * one, (one, four)
+
+
+@pytest.mark.parametrize("P,keep,sinks,recent,holes", [(1 << 20, 500000, 4, 1000, False), (1300001, 70, 60, 20, True), (700000, 300000, 200000, 400000, True), (2500000, 2400000, 0, 0, False)])
+def test_evict_of_millions(beam, P, keep, sinks, recent, holes):  # noqa: F811
+    """Two rows of a sentence: one with many equal scores, one without."""
+    page, g = 64, gen(P)
+    n = -(-P // page)
+    score = torch.stack((torch.randint(0, 50, (P,), generator=g).float(), torch.rand(P, generator=g)))
+    table = torch.randperm(n, generator=g).int()
+    if holes:
+        table[torch.randint(0, n, (n // 50,), generator=g)] = -1
+        table[0] = -9
+    there = (table >= 0).repeat_interleave(page)[:P]
+    t = torch.arange(P)
+    stay = min(keep, int(there.sum()))
+    new_n = -(-stay // page)
+    k_pages = torch.zeros((n + new_n, page, 2, 8), dtype=torch.float16, device="cuda")
+    k_pages[:n] = (torch.arange(n * page, device="cuda") % 2039).reshape(n, page, 1, 1).half()          # places of the pool, which half holds
+    new_table = torch.arange(n, n + new_n, dtype=torch.int32)
+    stays, new_score = beam.evict(score.cuda()[None], k_pages, k_pages.clone(), *cuda(table[None], new_table[None], ints(P)), keep=keep, sinks=sinks, recent=recent)
+    assert stays.tolist() == [stay]
+    pool = (table.long().repeat_interleave(page)[:P] * page + t % page) % 2039
+    for h in range(2):
+        safe = (t < sinks) | (t >= P - recent)
+        order = torch.argsort(score[h], descending=True, stable=True)
+        order = order[torch.argsort((~safe[order]).int(), stable=True)]
+        kept = order[there[order]][:stay].sort().values
+        assert torch.equal(new_score[0, h, :stay].cpu(), score[h][kept]) and (new_score[0, h, stay:] == 0).all()
+        assert torch.equal(k_pages[n:, :, h, 0].flatten()[:stay].cpu().long(), pool[kept])
