@@ -147,8 +147,9 @@ DBA_API int dba_tree_attend(int B, int n, int q_heads, const dba_heads *q, const
 /*
  * dba_cache_append with queries and keys normed by head before they are rotated, and with positions of several axes.  With norms
  *     y = x / sqrt(mean x^2 + eps) * weight
- * over the head_dim elements of each head of q and of k (an L2 norm is this one with weights of head_dim ** -0.5); the rotation turns y, all in fp32, squares
- * added up in 64 bits, and the result is rounded once.  Without norms (NULL) the formula is dba_cache_append's.
+ * over the head_dim elements of each head of q and of k (an L2 norm is this one with weights of head_dim ** -0.5); the rotation turns y, and the result is rounded once.  y is fp32, the squares
+ * and their sum too; where a head's sum leaves 1e-30 .. 1e36 (fp16's does not) they are added up once more without a power of two, which is taken out of the elements first.  So y is off by at most
+ * 12 * 2^-24 of itself, or by fp32's least normal number, in heads of any size.  Without norms (NULL) the formula is dba_cache_append's.
  *   norms        host, may be NULL
  *   position_dev device [B, n, axes] int32; NULL (axis_dev is NULL then): first[b] + i
  *   axis_dev     device [rot_dim / 2] int32: pair j turns by position[.., axis[j]] * inv_freq[j], and not at all where axis[j] lies outside [0, axes);
