@@ -165,7 +165,7 @@ __device__ __forceinline__ uint2 count_of(const EvictParams &p, const Choice &c,
 
 // One workgroup of W waves per sentence and row of scores of up to 64 W NK tokens, whose images stay in registers.  A wave has a stretch of its own, so that
 // places come from counts of waves and ballots.
-// Bound: latency, a chain of fifteen to twenty-five barriers; scores are a small part of what the move behind it takes.
+// Bound: latency, a chain of seven to seventeen barriers (two, or four where a page is missing, four a digit, one); scores are a small part of what the move behind it takes.
 template <int W, int NK>
 __global__ __launch_bounds__(64 * W) void dba_evict_choose_kernel(EvictParams p)
 {

@@ -101,7 +101,8 @@ struct WeighShape {
 // rows: nothing is added atomically, and results do not vary.
 //
 // Rows are split where there are few tokens; sums of splits are added up in their order by another launch.
-// Bound: the exponentials and what is around them.
+// Bound: waits.  All of 8 prompts of 1500 tokens, 32 heads on 8 of 128: 418 us, in which a SIMD has 0.94 waves on average, whose steps are chains of reads from LDS, four products that need each other
+// and sixteen exponentials; the VALU is at work for 25 % of the clocks, the matrix units for 9.  Workgroups are too few (384, not split), and in a chain the first tile of tokens has all rows and the last a seventh of them.
 template <int FMT, int DP, bool FULL>
 __global__ __launch_bounds__(256, 2) void dba_weigh_kernel(WeighParams p)
 {
@@ -228,8 +229,9 @@ __global__ __launch_bounds__(256, 2) void dba_weigh_kernel(WeighParams p)
 // waiting for them.
 //
 // FULL: heads have DP elements.  SR: rows in sixty-fours, whose masks the lanes look after.
-// Bound: memory, each key is read once: 64 sentences of 20 branches over 900 to 1500 tokens, 16 heads of 64, 48 us (3.5 TB/s, in pieces of 128 bytes), 128 rows of 128 over 16 x 3000 to 16000
-// tokens, 8 heads, 93 (3.4 TB/s; the exponentials alone are 28).
+// Bound: memory and waits, each key is read once: 64 sentences of 20 branches over 900 to 1500 tokens, 16 heads of 64, 48 us (3.5 TB/s, the VALU at work for 45 % of the clocks; attention, which reads the same layout for
+// two heads a workgroup, reaches 4.8, and that has not been tried here), 128 rows of 128 over 16 x 3000 to 16000 tokens, 8 heads, 93 (3.4 TB/s; the VALU 47 %, the matrix units 21, the exponentials alone are 28 us).
+// The 16-bit instances with SR = 2 have 8 to 10 registers in scratch (36 to 44 bytes a lane), some of them read again within the loop, which then waits for the next tile's keys as well; without that the second case has not been measured.
 template <int FMT, int DP>
 struct WeighFew {
     typedef WeighShape<FMT, DP> W;

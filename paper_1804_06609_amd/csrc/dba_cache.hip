@@ -69,8 +69,9 @@ const char *shared_fault(int B, int n, int q_heads, const dba_cache *cache, int 
     return nullptr;
 }
 
-// Many rows over common tokens: how many parts of the token axis.  A part costs about kPartTiles tiles to begin with and to write and join;
-// workgroups come in rounds.
+// Many rows over common tokens: how many parts of the token axis.  A part costs about kPartTiles tiles to begin with and to write and join; workgroups come in rounds of `resident`, two a compute unit.
+// (64 x 20 branches, 32 heads on 8 of 128, over 1500 tokens: 199 us a call, with 0 and 8 for kPartTiles 240 and 204, with 1, 2 and 5 the same; 128 x 8, 32 heads on 4, over 8000: 236 to 242, with rounds of 256
+// 279, of 1024 253; 8 x 16, 32 on 8, over 16000: 86, 97, 100; but 16 x 8, 16 on 2 of 64, over 4000: 34, 28, 37.)
 constexpr int kPartTiles = 3;
 
 AttendPlan common_plan(int nodes, int q_heads, const dba_cache &c, int max_shared)
@@ -125,7 +126,8 @@ void lay_out(AttendParams &p, const AttendPlan &plan, int B, const dba_cache &c)
 // ---- weighing -------------------------------------------------------------------------------------------------------
 
 // Up to WeighFew::MOST rows a head the waves go through tokens, else through rows.  Of the former a workgroup has as few tokens as fill the GPU
-// (kWeighGroups workgroups), but two tiles a wave at least, and sums that fit into LDS.  Of the latter rows are split where tokens alone leave GPU empty, two
+// (kWeighGroups workgroups, three rounds: 32 rows, 32 heads on 8 of 128, 16 x 3000 to 16000 tokens 100 us, with 2048 workgroups 125, 4096 123; 20 rows, 16 heads of 64, 64 x 900 to 1500 tokens 51, with 2048 56; five other
+// sizes within 0.6 us but for one, 31 and with 2048 33), but two tiles a wave at least, and sums that fit into LDS.  Of the latter rows are split where tokens alone leave GPU empty, two
 // turns of rows in LDS at least to a workgroup (one sentence of 300 tokens, 2400 rows: 18 us a call instead of 108; one of 4000 tokens, 16000 rows for each of 8 heads: 324 instead of 979).
 constexpr int kWeighGroups = 3200, kWeighChunk = 2048, kWeighRowGroups = 512;
 

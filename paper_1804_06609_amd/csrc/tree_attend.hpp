@@ -230,7 +230,7 @@ struct AttendShape {
     static constexpr int PER_SIMD = REGS <= 190 ? 2 : 1;
 
     // Weights of 16 bits leave an output 1.4 times as far from the exact one as its own rounding does (2.3e-3 against 1.66e-3 in bf16, 2.9e-4 against 2.07e-4 in
-    // fp16).  Where memory is what bounds, what the rounding leaves of a weight goes through a second product, and they do not: 64 sentences of 20 branches 65.4 us instead of
+    // fp16).  In attention over a sentence's own cache (PARTS, below, has the product throughout), where memory is what bounds, what the rounding leaves of a weight goes through a second product, and they do not: 64 sentences of 20 branches 65.4 us instead of
     // 64.1, 4 of 57000 tokens 192.6 either way.  Where the matrix units and the VALU do, they are left at that: with the second product 36 rows of 64 a head would take 45.7 us instead of 42.9,
     // 64 of 128 106 instead of 96, 32 drafts of 63 nodes 156 instead of 122, 8 prompts of 1500 tokens 346 instead of 277.
     static constexpr bool REST = FMT != 0 && !ROWS && QT <= 2;
@@ -262,7 +262,7 @@ struct AttendShape {
 // tokens are read once they vary fastest (4 sentences of 50000 and more: 186 instead of 199 us).
 //
 // PARTS: results are always left as parts, for another join; and the nodes of several sentences may be taken for those of one.  What the rounding leaves of weights goes through a second
-// product whatever the form (64 sentences of 80 rows of 128, 8 heads, over 900 to 1500 tokens: 121 us instead of 101; 128 of 64 rows over 110 to 160, 4 heads: 26.5 either way).
+// product whatever the form (64 sentences of 80 rows of 128, 8 heads, over 900 to 1500 tokens: 115 to 122 us instead of 101; 128 of 64 rows over 110 to 160, 4 heads: 26.5 either way).
 template <int FMT, int DP, int QT, bool ROWS, int SIDE, bool PARTS = false>
 __global__ __launch_bounds__(256, (AttendShape<FMT, DP, QT, ROWS>::PER_SIMD)) void dba_attend_kernel(AttendParams p)
 {
