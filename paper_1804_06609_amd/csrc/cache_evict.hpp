@@ -236,7 +236,7 @@ __global__ __launch_bounds__(64 * W) void dba_evict_choose_kernel(EvictParams p)
 }
 
 // Longer rows in launches with a workgroup for each kEvictPart tokens: what is there of a sentence; counts of the first digit; the bar, from those counts and the tokens of that digit, by one
-// workgroup a row; how many stay of each part; the list.  Each goes over a row's scores, or a sentence's pages, once, and the last over the counts of the parts before its own.
+// workgroup a row; how many stay of each part; the list.  Scores are read five times at most and a sentence's pages once; a part of the list adds up the numbers of those before it.
 // (One choice of 16384 of 65000 tokens, 4 sentences: 4.6 + 4.8 + 24 + 4.6 + 6.2 us; one workgroup took 103.  8 choices of 64 of a million tokens 0.37 ms, of four million 1.36; where each
 // part counted all scores before it 1.33 and 14.4, and with an absent page among 16 tokens each, which each part looked for, 3.1 and 43.7 instead of 0.42 and 1.51.)
 constexpr int kEvictWaves = 16, kEvictPart = 4096, kEvictPer = kEvictPart / (64 * kEvictWaves);

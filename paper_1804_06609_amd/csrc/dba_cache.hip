@@ -126,7 +126,7 @@ void lay_out(AttendParams &p, const AttendPlan &plan, int B, const dba_cache &c)
 // ---- weighing -------------------------------------------------------------------------------------------------------
 
 // Up to WeighFew::MOST rows a head the waves go through tokens, else through rows.  Of the former a workgroup has as few tokens as fill the GPU
-// (kWeighGroups workgroups, three rounds: 32 rows, 32 heads on 8 of 128, 16 x 3000 to 16000 tokens 100 us, with 2048 workgroups 125, 4096 123; 20 rows, 16 heads of 64, 64 x 900 to 1500 tokens 51, with 2048 56; five other
+// (kWeighGroups workgroups, about three rounds: 32 rows, 32 heads on 8 of 128, 16 x 3000 to 16000 tokens 100 us, with 2048 workgroups 125, 4096 123; 20 rows, 16 heads of 64, 64 x 900 to 1500 tokens 51, with 2048 56; five other
 // sizes within 0.6 us but for one, 31 and with 2048 33), but two tiles a wave at least, and sums that fit into LDS.  Of the latter rows are split where tokens alone leave GPU empty, two
 // turns of rows in LDS at least to a workgroup (one sentence of 300 tokens, 2400 rows: 18 us a call instead of 108; one of 4000 tokens, 16000 rows for each of 8 heads: 324 instead of 979).
 constexpr int kWeighGroups = 3200, kWeighChunk = 2048, kWeighRowGroups = 512;
